@@ -303,6 +303,165 @@ int codegemm_gemm_static(const codegemm_desc *desc, const codegemm_plan *plan,
 int codegemm_dequant_gemm(const codegemm_desc *desc, const void *x, const uint8_t *codes,
                           const void *codebooks, const void *scales, void *y, void *stream);
 
+/*
+ * What lies between the q, k, v projections of a decoder block and its output
+ * projection: the new tokens' keys and values go into a paged cache, rotated and
+ * (where the model does so) normalised on the way; single tokens attend to the
+ * cache, the tokens of prompts to each other.
+ *
+ * A cache of one layer (host struct; the caller owns the buffers behind its
+ * device pointers and may change their contents between calls).  A page holds
+ * page_size tokens of one sequence, position p of sequence i lies in place
+ * p % page_size of page page_table[i][p / page_size]; no page may be in two
+ * places that are written.
+ *     k         [num_pages][kv_heads][page_size][head_dim]
+ *     v         [num_pages][kv_heads][page_size/16][head_dim][16]   (16 tokens innermost, so
+ *               that 16 tokens' values of one dimension are one load of the matrix operand)
+ *     k_scales, v_scales  [num_pages][kv_heads][page_size/scale_block] fp32 (8-bit types)
+ * A cached value is its element for CODEGEMM_KV_FP16 and element * scale for
+ * CODEGEMM_KV_INT8 (-127..127) and CODEGEMM_KV_FP8 (e4m3: 3 bits of mantissa,
+ * largest value 448), scale_block consecutive tokens of a page sharing a scale.
+ * Places that hold no token of a sequence may hold anything, NaN too.
+ * A page number outside 0..num_pages-1 stands for no page: nothing is written
+ * there, and its tokens are not attended to and read as zeros.  The same holds for
+ * positions from max_pages * page_size on.
+ */
+enum {
+    CODEGEMM_KV_FP16 = 0,
+    CODEGEMM_KV_INT8 = 1,
+    CODEGEMM_KV_FP8 = 2
+};
+
+typedef struct codegemm_kv_cache {
+    int32_t kv_heads;           /* 1..1024                                         */
+    int32_t head_dim;           /* D: a multiple of 16, 16..256                    */
+    int32_t num_pages;          /* 1..2^30                                         */
+    int32_t page_size;          /* tokens: 16, 32, 64, 128 or 256                  */
+    int32_t dtype;              /* CODEGEMM_KV_*                                   */
+    int32_t scale_block;        /* tokens that share a scale: 1, 2, 4 .. page_size */
+                                /* (not read for CODEGEMM_KV_FP16)                 */
+    int32_t num_seqs;           /* rows of page_table, 1..65535                    */
+    int32_t max_pages;          /* entries of a row, max_pages * page_size <= 2^30 */
+    void *k, *v;                /* device */
+    float *k_scales, *v_scales; /* device; NULL for CODEGEMM_KV_FP16 */
+    const int32_t *page_table;  /* device, [num_seqs][max_pages] */
+    const int32_t *kv_lens;     /* device, [num_seqs]: tokens of each sequence, those of this step among them */
+} codegemm_kv_cache;
+
+/* Bytes of k (and of v), and of k_scales (and of v_scales; 0 for CODEGEMM_KV_FP16).
+ * 0 for an invalid cache; the pointers are not looked at. */
+size_t codegemm_kv_pool_bytes(const codegemm_kv_cache *cache);
+size_t codegemm_kv_scales_bytes(const codegemm_kv_cache *cache);
+
+enum {
+    CODEGEMM_ROPE_INTERLEAVED = 1   /* pairs (2i, 2i+1) instead of (i, i + R/2) */
+};
+
+/* The new tokens of a step (host struct). */
+typedef struct codegemm_append_desc {
+    int32_t tokens;             /* T: rows of q, k and v, of all sequences, 1..2^24           */
+    int32_t q_heads;            /* 0 (q and q_out NULL) .. 1024                               */
+    int32_t rotary_dim;         /* R: leading dimensions that turn, a multiple of 16 up to    */
+                                /* head_dim; 0: none                                          */
+    int32_t rope_positions;     /* rows of the rope table, >= 1 when R > 0                    */
+    int32_t flags;              /* CODEGEMM_ROPE_*                                            */
+    float norm_eps;             /* >= 0; of the norms, if any                                 */
+    int32_t q_stride, k_stride, v_stride;   /* elements between tokens, multiples of 8 up to  */
+    int32_t q_out_stride, k_out_stride;     /* 2^20 (they may be columns of one fused         */
+                                            /* projection's output); 0: heads * head_dim      */
+} codegemm_append_desc;
+
+/*
+ * Writes the step's keys and values into the cache.  The new tokens of sequence i
+ * are rows cu_seqlens[i] .. cu_seqlens[i+1]-1 of q [T][q_heads][D], k and v
+ * [T][kv_heads][D] (fp16), n_i of them, and take the positions
+ * kv_lens[i] - n_i .. kv_lens[i] - 1; rows at negative positions write nothing to
+ * the cache and get zeros in q_out and k_out (an idle slot of a captured graph:
+ * kv_lens 0).  cu_seqlens [num_seqs + 1] int32, ascending from 0 to T; NULL: one
+ * token each, T = num_seqs.
+ * Per head, in fp32, with one rounding at the end:
+ *   q_norm, k_norm [D] fp16 (NULL: no norm): x_d *= w_d / sqrt(mean(x^2) + eps);
+ *   rope [rope_positions][R/2][2] fp32 (NULL for R = 0), the caller's cos and sin
+ *     of every position and pair, with whatever scaling for long contexts:
+ *     (a, b) -> (a cos - b sin, b cos + a sin); positions past the table take its
+ *     last row;
+ *   q_out [T][q_heads][D], k_out [T][kv_heads][D] fp16: the result, for the
+ *     attention (k_out may be NULL; q_out may be q and k_out k, with their strides);
+ *   the cache: fp16, or codes round(x / s).  s is the largest |x| of the block's
+ *     new tokens over 127 (448), and not below the scale that its earlier tokens
+ *     have; where it is above, their codes c become round(c * s_old / s).  A block
+ *     whose first token is new starts afresh.  A block that gets a NaN or an
+ *     infinity has a NaN scale from then on: all its values read as NaN.
+ */
+int codegemm_kv_append(const codegemm_kv_cache *cache, const codegemm_append_desc *desc,
+                       const int32_t *cu_seqlens, const void *q, const void *k, const void *v,
+                       const void *q_norm, const void *k_norm, const float *rope,
+                       void *q_out, void *k_out, void *stream);
+
+/*
+ * Cached keys and values as contiguous fp16: rows cu_rows[i] .. cu_rows[i+1]-1 of
+ * k_out and v_out [rows][kv_heads][D] are positions first[i], first[i]+1, .. of
+ * sequence i (first NULL: 0), zeros where a position is negative, not below
+ * kv_lens[i] or has no page.  rows 1..2^24; cu_rows [num_seqs + 1] int32,
+ * ascending from 0 to rows.  Either output may be NULL.  For the prompt attention
+ * of tokens that follow a cached prefix, which takes contiguous keys and values.
+ */
+int codegemm_kv_gather(const codegemm_kv_cache *cache, int32_t rows, const int32_t *cu_rows,
+                       const int32_t *first, void *k_out, void *v_out, void *stream);
+
+enum {
+    CODEGEMM_ATTN_CAUSAL = 1        /* codegemm_attn_prompt: keys up to the query's own position */
+};
+
+/* An attention call (host struct). */
+typedef struct codegemm_attn_desc {
+    int32_t q_heads;            /* a multiple of kv_heads, 1..1024; query heads r * h .. r * h + r - 1  */
+    int32_t kv_heads;           /* share key head h, r = q_heads / kv_heads                             */
+    int32_t head_dim;           /* D: a multiple of 16, 16..256                                         */
+    int32_t num_seqs;           /* 1..65535                                                             */
+    int32_t total_q;            /* rows of q, 1..2^24; codegemm_attn_decode: num_seqs                   */
+    int32_t total_kv;           /* rows of k and v, 0..2^24 (codegemm_attn_decode: not read)            */
+    int32_t max_kv;             /* keys of the longest sequence as far as the host knows, >= 1: chooses */
+                                /* how keys are split; longer ones are right all the same               */
+    int32_t window;             /* 0, or keys that a query sees: the last `window` up to its position   */
+    int32_t flags;              /* CODEGEMM_ATTN_*                                                      */
+    float scale;                /* of the scores, finite (usually 1 / sqrt(D))                          */
+    int32_t q_stride, k_stride, v_stride, out_stride;   /* elements between tokens, multiples of 8 up   */
+                                                        /* to 2^20; 0: heads * head_dim                 */
+} codegemm_attn_desc;
+
+/*
+ * One query token per sequence against the cache:
+ *     out[i][h] = sum_t softmax_t(scale * q[i][h] . k_t) * v_t
+ * over the positions t < kv_lens[i] (with a window W: t >= kv_lens[i] - W) of
+ * sequence i that have a page; zeros where there are none.  q, out
+ * [num_seqs][q_heads][D] fp16.  Products of fp16 (8-bit codes are exact in fp16)
+ * summed in fp32, weights rounded to fp16 for their product with v, one rounding of
+ * the result.  Long sequences are split over workgroups and joined in a fixed
+ * order: results are bit-reproducible.  workspace: as for codegemm_gemm
+ * (codegemm_workspace_init once; shared with the linear layers on one stream).
+ * kv_heads, head_dim and num_seqs of desc are those of the cache.
+ */
+size_t codegemm_attn_decode_workspace_bytes(const codegemm_kv_cache *cache, const codegemm_attn_desc *desc);
+int codegemm_attn_decode(const codegemm_kv_cache *cache, const codegemm_attn_desc *desc,
+                         const void *q, void *out, void *workspace, size_t workspace_bytes,
+                         void *stream);
+
+/*
+ * Packed sequences: queries cu_q[i] .. cu_q[i+1]-1 (n of them) of q
+ * [total_q][q_heads][D] attend to keys cu_kv[i] .. cu_kv[i+1]-1 (n_kv) of k and v
+ * [total_kv][kv_heads][D], fp16; cu_q and cu_kv [num_seqs + 1] int32, ascending
+ * from 0 to total_q and total_kv (cu_kv NULL: cu_q).  Query j stands at position
+ * p = n_kv - n + j and sees the keys t with t <= p (CODEGEMM_ATTN_CAUSAL; all of
+ * them otherwise) and t > p - window (window > 0); out [total_q][q_heads][D] is
+ * zero where it sees none.  Keys and values that a query does not see do not reach
+ * its result, whatever they hold.  Sums as for codegemm_attn_decode.
+ */
+size_t codegemm_attn_prompt_workspace_bytes(const codegemm_attn_desc *desc);
+int codegemm_attn_prompt(const codegemm_attn_desc *desc, const void *q, const void *k, const void *v,
+                         const int32_t *cu_q, const int32_t *cu_kv, void *out,
+                         void *workspace, size_t workspace_bytes, void *stream);
+
 /* Static, NUL-terminated description of a status code.  Host only. */
 const char *codegemm_status_string(int status);
 

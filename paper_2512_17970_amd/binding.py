@@ -23,6 +23,9 @@ _lib: Optional[ctypes.CDLL] = None
 
 FLAG_Y_FP32 = 1
 PSUM_FP32, PSUM_FP16 = 0, 1
+KV_FP16, KV_INT8, KV_FP8 = 0, 1, 2
+ROPE_INTERLEAVED = 1
+ATTN_CAUSAL = 1
 
 EXPORTS = [
     "codegemm_default_plan", "codegemm_workspace_bytes", "codegemm_packed_codes_bytes",
@@ -32,6 +35,8 @@ EXPORTS = [
     "codegemm_psumbook_build", "codegemm_gemm", "codegemm_dequant_gemm", "codegemm_status_string",
     "codegemm_gemm_static", "codegemm_static_workspace_limit",
     "codegemm_gemm_grouped", "codegemm_grouped_workspace_bytes",
+    "codegemm_kv_pool_bytes", "codegemm_kv_scales_bytes", "codegemm_kv_append", "codegemm_kv_gather",
+    "codegemm_attn_decode", "codegemm_attn_decode_workspace_bytes", "codegemm_attn_prompt", "codegemm_attn_prompt_workspace_bytes",
 ]
 
 
@@ -78,6 +83,47 @@ class GroupMember(ctypes.Structure):
     _fields_ = [("out_features", ctypes.c_int32), ("reserved", ctypes.c_int32),
                 ("packed_codes", ctypes.c_void_p), ("codebooks", ctypes.c_void_p),
                 ("scales", ctypes.c_void_p), ("y", ctypes.c_void_p)]
+
+
+class KvCache(ctypes.Structure):
+    """codegemm_kv_cache of include/codegemm.h: a layer's paged cache.  Holds addresses only; the caller keeps the tensors."""
+    _fields_ = [("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("num_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("scale_block", ctypes.c_int32), ("num_seqs", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+                ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scales", ctypes.c_void_p), ("v_scales", ctypes.c_void_p),
+                ("page_table", ctypes.c_void_p), ("kv_lens", ctypes.c_void_p)]
+
+    @classmethod
+    def make(cls, k, v, k_scales, v_scales, page_table, kv_lens, *, kv_heads: int, head_dim: int, num_pages: int, page_size: int,
+             dtype: int = KV_FP16, scale_block: int = 1, num_seqs: int, max_pages: int):
+        return cls(kv_heads, head_dim, num_pages, page_size, dtype, scale_block, num_seqs, max_pages,
+                   _ptr(k), _ptr(v), _ptr(k_scales), _ptr(v_scales), _ptr(page_table), _ptr(kv_lens))
+
+
+class AppendDesc(ctypes.Structure):
+    """codegemm_append_desc"""
+    _fields_ = [("tokens", ctypes.c_int32), ("q_heads", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("rope_positions", ctypes.c_int32),
+                ("flags", ctypes.c_int32), ("norm_eps", ctypes.c_float), ("q_stride", ctypes.c_int32), ("k_stride", ctypes.c_int32),
+                ("v_stride", ctypes.c_int32), ("q_out_stride", ctypes.c_int32), ("k_out_stride", ctypes.c_int32)]
+
+    @classmethod
+    def make(cls, tokens: int, q_heads: int, *, rotary_dim: int = 0, rope_positions: int = 0, interleaved: bool = False, norm_eps: float = 0.0,
+             q_stride: int = 0, k_stride: int = 0, v_stride: int = 0, q_out_stride: int = 0, k_out_stride: int = 0):
+        return cls(tokens, q_heads, rotary_dim, rope_positions, ROPE_INTERLEAVED if interleaved else 0, norm_eps,
+                   q_stride, k_stride, v_stride, q_out_stride, k_out_stride)
+
+
+class AttnDesc(ctypes.Structure):
+    """codegemm_attn_desc"""
+    _fields_ = [("q_heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("num_seqs", ctypes.c_int32),
+                ("total_q", ctypes.c_int32), ("total_kv", ctypes.c_int32), ("max_kv", ctypes.c_int32), ("window", ctypes.c_int32),
+                ("flags", ctypes.c_int32), ("scale", ctypes.c_float), ("q_stride", ctypes.c_int32), ("k_stride", ctypes.c_int32),
+                ("v_stride", ctypes.c_int32), ("out_stride", ctypes.c_int32)]
+
+    @classmethod
+    def make(cls, q_heads: int, kv_heads: int, head_dim: int, *, num_seqs: int, total_q: int, total_kv: int = 0, max_kv: int, scale: float,
+             window: int = 0, causal: bool = False, q_stride: int = 0, k_stride: int = 0, v_stride: int = 0, out_stride: int = 0):
+        return cls(q_heads, kv_heads, head_dim, num_seqs, total_q, total_kv, max_kv, window, ATTN_CAUSAL if causal else 0, scale,
+                   q_stride, k_stride, v_stride, out_stride)
 
 
 def lib_path() -> str:
@@ -138,6 +184,22 @@ def load() -> ctypes.CDLL:
     lib.codegemm_static_workspace_limit.restype = sz
     lib.codegemm_dequant_gemm.argtypes = [dp, vp, vp, vp, vp, vp, vp]
     lib.codegemm_dequant_gemm.restype = i
+    cp, ap, tp, i32 = ctypes.POINTER(KvCache), ctypes.POINTER(AppendDesc), ctypes.POINTER(AttnDesc), ctypes.c_int32
+    for name in ("codegemm_kv_pool_bytes", "codegemm_kv_scales_bytes"):
+        getattr(lib, name).argtypes = [cp]
+        getattr(lib, name).restype = sz
+    lib.codegemm_kv_append.argtypes = [cp, ap, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.codegemm_kv_append.restype = i
+    lib.codegemm_kv_gather.argtypes = [cp, i32, vp, vp, vp, vp, vp]
+    lib.codegemm_kv_gather.restype = i
+    lib.codegemm_attn_decode_workspace_bytes.argtypes = [cp, tp]
+    lib.codegemm_attn_decode_workspace_bytes.restype = sz
+    lib.codegemm_attn_decode.argtypes = [cp, tp, vp, vp, vp, sz, vp]
+    lib.codegemm_attn_decode.restype = i
+    lib.codegemm_attn_prompt_workspace_bytes.argtypes = [tp]
+    lib.codegemm_attn_prompt_workspace_bytes.restype = sz
+    lib.codegemm_attn_prompt.argtypes = [tp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.codegemm_attn_prompt.restype = i
     lib.codegemm_status_string.argtypes = [i]
     lib.codegemm_status_string.restype = ctypes.c_char_p
     if _calls:
@@ -277,6 +339,42 @@ if _calls:
 def codegemm_dequant_gemm(desc: Desc, x, codes, codebooks, scales, y, stream: int = 0) -> None:
     _check(load().codegemm_dequant_gemm(ctypes.byref(desc), _ptr(x), _ptr(codes), _ptr(codebooks), _ptr(scales),
                                         _ptr(y), stream), "codegemm_dequant_gemm")
+
+
+def codegemm_kv_pool_bytes(cache: KvCache) -> int:
+    return int(load().codegemm_kv_pool_bytes(ctypes.byref(cache)))
+
+
+def codegemm_kv_scales_bytes(cache: KvCache) -> int:
+    return int(load().codegemm_kv_scales_bytes(ctypes.byref(cache)))
+
+
+def codegemm_kv_append(cache: KvCache, desc: AppendDesc, cu_seqlens, q, k, v, q_norm, k_norm, rope, q_out, k_out, stream: int = 0) -> None:
+    _check(load().codegemm_kv_append(ctypes.byref(cache), ctypes.byref(desc), _ptr(cu_seqlens), _ptr(q), _ptr(k), _ptr(v), _ptr(q_norm),
+                                     _ptr(k_norm), _ptr(rope), _ptr(q_out), _ptr(k_out), stream), "codegemm_kv_append")
+
+
+def codegemm_kv_gather(cache: KvCache, rows: int, cu_rows, first, k_out, v_out, stream: int = 0) -> None:
+    _check(load().codegemm_kv_gather(ctypes.byref(cache), rows, _ptr(cu_rows), _ptr(first), _ptr(k_out), _ptr(v_out), stream),
+           "codegemm_kv_gather")
+
+
+def codegemm_attn_decode_workspace_bytes(cache: KvCache, desc: AttnDesc) -> int:
+    return int(load().codegemm_attn_decode_workspace_bytes(ctypes.byref(cache), ctypes.byref(desc)))
+
+
+def codegemm_attn_decode(cache: KvCache, desc: AttnDesc, q, out, workspace, workspace_bytes: int, stream: int = 0) -> None:
+    _check(load().codegemm_attn_decode(ctypes.byref(cache), ctypes.byref(desc), _ptr(q), _ptr(out), _ptr(workspace), workspace_bytes, stream),
+           "codegemm_attn_decode")
+
+
+def codegemm_attn_prompt_workspace_bytes(desc: AttnDesc) -> int:
+    return int(load().codegemm_attn_prompt_workspace_bytes(ctypes.byref(desc)))
+
+
+def codegemm_attn_prompt(desc: AttnDesc, q, k, v, cu_q, cu_kv, out, workspace, workspace_bytes: int, stream: int = 0) -> None:
+    _check(load().codegemm_attn_prompt(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(cu_q), _ptr(cu_kv), _ptr(out), _ptr(workspace),
+                                       workspace_bytes, stream), "codegemm_attn_prompt")
 
 
 def compressed_bytes(B: int, K: int, N: int, v: int, m: int, g: int = -1) -> int:
