@@ -440,7 +440,8 @@ typedef struct codegemm_attn_desc {
  * the result.  Long sequences are split over workgroups and joined in a fixed
  * order: results are bit-reproducible.  workspace: as for codegemm_gemm
  * (codegemm_workspace_init once; shared with the linear layers on one stream).
- * kv_heads, head_dim and num_seqs of desc are those of the cache.
+ * kv_heads, head_dim and num_seqs of desc are those of the cache; num_seqs *
+ * max_pages * page_size * kv_heads * ceil(q_heads / kv_heads / 16) < 2^36.
  */
 size_t codegemm_attn_decode_workspace_bytes(const codegemm_kv_cache *cache, const codegemm_attn_desc *desc);
 int codegemm_attn_decode(const codegemm_kv_cache *cache, const codegemm_attn_desc *desc,

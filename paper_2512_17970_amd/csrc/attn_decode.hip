@@ -1,39 +1,42 @@
 // Attention of one query token per sequence over the paged cache.
 //
-// A workgroup takes a range of one sequence's keys for up to 16 query heads that share a key head.  Each of its wavefronts works on
-// its own on steps of 32 A tokens: scores as S^T = K Q^T on the matrix cores (rows: tokens, columns: query heads), the softmax's
-// running maximum and sum per column, and O^T += V^T P^T, whose right operand is what the score tiles leave in the lanes, because
-// a step's tokens are dealt out to the lanes' groups g in runs of 8 A: row 4 g + r of score tile n is token 8 A g + 4 n + r, so
-// lane group g holds 8 A consecutive tokens of P^T, and, in the value pool's layout (16 tokens innermost), the 8 A tokens of V^T that
-// go with them are one or two loads.  Keys, values and weights never pass through LDS, and no wavefront waits for another before the end.
+// An item is a sequence and up to 16 query heads that share a key head; its keys are steps of 32 tokens.  The workgroups look at all lengths
+// and cut the items into pieces such that each has about one, whatever the lengths are; the last workgroup of an item to finish joins its
+// pieces.
+//
+// Each wavefront works on its own on every fourth step: scores as S^T = K Q^T on the matrix cores (rows: tokens, columns: query heads),
+// the softmax's running maximum and sum per column, and O^T += V^T P^T.  The right operand of the second product is what the score tiles
+// leave in the lanes, because a step's tokens are dealt out to the four lane groups g in runs of 8: row 4 g + r of score tile n is
+// token 8 g + 4 n + r, so lane group g holds 8 consecutive tokens of P^T, and the value pool has them next to each other for every
+// dimension.  The memory pipeline writes keys, values and scales of the next steps into a ring in LDS (global_load .. lds), where every lane
+// finds its own operands again; no wavefront waits for another before the end of an item.
 // 8-bit codes become fp16 exactly on the way into the matrix cores; a key's scale multiplies its score, a value's scale its weight.
 #include <cmath>
+#include <type_traits>
 
 #include "attn_common.h"
 
 namespace cg {
 
-constexpr int kDecodeWaves = 4;
 constexpr int kDecodeRows = 16;             // query heads of a workgroup
-constexpr int kMaxSplits = 64;
+constexpr int kDecodeUnits = 256;           // compute units
+constexpr int kJoinSteps = 1;               // what joining pieces takes, in steps of a wavefront: an item that is longer by less stays whole
+constexpr int kRoundSteps = 10;             // .. and a second piece for the same workgroup
 constexpr float kLeastLog = -40.0f;         // of a scale's logarithm in the running maximum
 
 struct DecodeParams {
     CacheView c;
     const _Float16* q;
     _Float16* out;
-    float* part;            // [item][split][16][D + 2] of sequences in several ranges: sums, then maximum and weight
-    uint32_t* counters;
-    int cstride;
+    float* part;            // [piece of an item that has several][16 (D + 2)]: [D / 16][64 lanes][4] sums, [16] maximum and weight
+    uint32_t* counters;     // of such an item: that of its first piece
+    int slots;              // workgroups that run at once
     int r;                  // query heads of a key head
-    int tiles;              // workgroups of 16 of them
+    int tiles;              // items of 16 of them
     int q_stride, out_stride;
     int window;
-    int min_steps;          // of a range, before there is a second one
     float scale;            // times log2(e)
 };
-
-typedef float float2_t __attribute__((ext_vector_type(2)));
 
 // 8 codes to fp16, exactly.
 template <int TYPE>
@@ -56,364 +59,531 @@ __device__ __forceinline__ half8_t codes_to_half(uint32_t lo, uint32_t hi)
     }
 }
 
-// What one lane holds of a step.  K rows: 16 elements of each of 2 A tokens per 64 dimensions; V: 8 A tokens of one dimension in 16.
-template <int TYPE, int DP, int A, int SC>
-struct Step {
+typedef __attribute__((address_space(3))) u32x4_t lds_words4;
+typedef __attribute__((address_space(3))) u32x2_t lds_words2;
+typedef __attribute__((address_space(3))) float4_t lds_float4;
+typedef __attribute__((address_space(3))) float lds_float1;
+typedef __attribute__((address_space(4))) const int32_t const_int;
+
+// A step in LDS, per wavefront: keys, values, the tokens' scales.  A workgroup has a compute unit to itself, or, NARROW, half of one.
+template <int TYPE, int DP, bool NARROW>
+struct DecodeStep {
     static constexpr bool kHalf = TYPE == CODEGEMM_KV_FP16;
-    static constexpr int kTiles = 2 * A, kChunks = DP / 64, kBlocks = DP / 16;
-    uint32_t k[kTiles][kChunks][kHalf ? 8 : 4];
-    uint32_t v[kBlocks][kHalf ? 4 * A : 2 * A];
-    float ks[SC == 2 ? 4 * kTiles : 1], vs[SC == 2 ? 4 * kTiles : 1];
-    bool ok;                     // the lane group's tokens have a page
+    static constexpr int kSize = kHalf ? 2 : 1;
+    static constexpr int kTokens = 32, kRun = 8, kTiles = 2;
+    static constexpr int kPart = kTokens * DP * kSize;               // bytes of the keys, and of the values
+    static constexpr int kScaleBytes = kHalf ? 0 : 256;              // [keys, values][32] fp32
+    static constexpr int kBytes = 2 * kPart + kScaleBytes;
+    static constexpr int kRequests = 2 * kPart / 1024 + (kHalf ? 0 : 1);
+    static constexpr int kStages = 2;
+    static constexpr int kPerCu = NARROW && kBytes <= 20 * 1024 ? 2 : 1;
+    static constexpr int kWaves = (kBytes > 20 * 1024 ? 2 : kBytes > 10 * 1024 ? 4 : 8) / kPerCu;
+    static constexpr int kRing = kWaves * kStages * kBytes;
+    static constexpr int kSums = kWaves * kDecodeRows * 8;           // the wavefronts' maxima and weights
+    static constexpr int kLds = kRing + kSums + 16;
+    static constexpr int kBlocks = DP / 16 / kWaves > 0 ? DP / 16 / kWaves : 1;    // of 16 dimensions that a wavefront sums up in the end
+    static_assert(kBytes >= kDecodeRows * DP * 4, "a wavefront's sums fit into a stage");
 };
 
-// TYPE: of the cache.  DP: head_dim rounded up to 64, 128 or 256; EXACT: it is head_dim.  SC: 0 no scales, 1 one for the lane group's
-// run of tokens, 2 several.  A: 32 A tokens a step.
-template <int TYPE, int DP, int SC, bool EXACT>
-__global__ void __launch_bounds__(kDecodeWaves * kWave) attn_decode_kernel(const DecodeParams p)
+// The sum of the values up to the lane's own; all lanes' in the last lane.
+__device__ __forceinline__ unsigned wave_scan(unsigned x)
 {
-    constexpr int A = TYPE == CODEGEMM_KV_FP16 || DP == 256 || SC == 2 ? 1 : 2;
-    constexpr int kRun = 8 * A, kStep = 32 * A, kTiles = 2 * A;
-    typedef Step<TYPE, DP, A, SC> stage_t;
-    constexpr int kPitch = DP + 4;                                   // floats of a row's sums in LDS
-    __shared__ __align__(16) float merge[(kDecodeWaves / 2) * kDecodeRows * kPitch];
-    __shared__ float merge_ml[(kDecodeWaves / 2) * kDecodeRows * 2];
-    __shared__ uint32_t flag;
+    auto add = [&](auto ctrl, auto rows) { x += (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, decltype(ctrl)::value, decltype(rows)::value, 0xf, false); };
+    typedef std::integral_constant<int, 0xf> all;
+    add(std::integral_constant<int, 0x111>(), all());      // row_shr 1, 2, 4, 8
+    add(std::integral_constant<int, 0x112>(), all());
+    add(std::integral_constant<int, 0x114>(), all());
+    add(std::integral_constant<int, 0x118>(), all());
+    add(std::integral_constant<int, 0x142>(), std::integral_constant<int, 0xa>());     // row_bcast 15 into rows 1 and 3
+    add(std::integral_constant<int, 0x143>(), std::integral_constant<int, 0xc>());     // row_bcast 31 into rows 2 and 3
+    return x;
+}
+__device__ __forceinline__ unsigned wave_max(unsigned x)
+{
+    for (int o = 1; o < kWave; o <<= 1) {
+        const unsigned w = (unsigned)__shfl_xor((int)x, o);
+        x = x > w ? x : w;
+    }
+    return (unsigned)__builtin_amdgcn_readfirstlane((int)x);
+}
+__device__ __forceinline__ unsigned wave_sum(unsigned x) { return (unsigned)__builtin_amdgcn_readlane((int)wave_scan(x), kWave - 1); }
+
+// Sum, maximum over the four lanes of a column: lanes l, l ^ 16, l ^ 32, l ^ 48.
+template <class Join>
+__device__ __forceinline__ float over_groups(float x, Join join)
+{
+    const uint32_t w = __builtin_bit_cast(uint32_t, x);
+    const auto a = __builtin_amdgcn_permlane16_swap(w, w, false, false);
+    const uint32_t y = __builtin_bit_cast(uint32_t, join(__builtin_bit_cast(float, (uint32_t)a[0]), __builtin_bit_cast(float, (uint32_t)a[1])));
+    const auto b = __builtin_amdgcn_permlane32_swap(y, y, false, false);
+    return join(__builtin_bit_cast(float, (uint32_t)b[0]), __builtin_bit_cast(float, (uint32_t)b[1]));
+}
+
+// A sequence's tokens lo .. len - 1; its steps start at multiples of their length.  One without tokens has a step all the same, in
+// which nothing counts, and so gets its zeros.
+struct Span {
+    int lo, len, first, steps;
+};
+__device__ __forceinline__ Span span_of(const DecodeParams& p, int n)
+{
+    const int held = p.c.max_pages << p.c.page_shift;
+    Span s;
+    s.len = n < 0 ? 0 : n < held ? n : held;
+    s.lo = p.window > 0 && n > p.window ? n - p.window : 0;
+    s.first = s.lo & ~31;
+    s.steps = s.len > s.lo ? (s.len - s.first + 31) / 32 : 1;
+    return s;
+}
+
+// 16 bytes per lane (LANES of them), each from its own address, to LDS byte address lds + 16 lane; 4 bytes, lds + 4 lane.
+__device__ __forceinline__ void request16(uint32_t lds, const unsigned char* from)
+{
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" :: "{m0}"(lds), "v"(from) : "memory");
+}
+__device__ __forceinline__ void request4(uint32_t lds, const float* from)
+{
+    asm volatile("s_nop 0\n\tglobal_load_lds_dword %1, off" :: "{m0}"(lds), "v"(from) : "memory");
+}
+
+// TYPE: of the cache.  DP: head_dim rounded up to 64, 128 or 256; EXACT: it is head_dim.
+template <int TYPE, int DP, bool EXACT, bool NARROW>
+__global__ void __launch_bounds__((DecodeStep<TYPE, DP, NARROW>::kWaves * kWave), (DecodeStep<TYPE, DP, NARROW>::kWaves * DecodeStep<TYPE, DP, NARROW>::kPerCu > 4 ? 2 : 1))
+attn_decode_kernel(const DecodeParams p)
+{
+    typedef DecodeStep<TYPE, DP, NARROW> T;
+    constexpr int NW = T::kWaves;
+    extern __shared__ __align__(16) unsigned char smem[];
+    const uint32_t lds0 = (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) unsigned char*)smem);
+    const uint32_t ml_at = lds0 + T::kRing;
+    volatile uint32_t* flag = reinterpret_cast<volatile uint32_t*>(smem + T::kRing + T::kSums);     // whether this workgroup is an item's last
 
     const CacheView& cv = p.c;
-    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int col = lane & 15, g = lane >> 4;
-    const int split = blockIdx.x, seq = blockIdx.z, head = blockIdx.y / p.tiles, row0 = (blockIdx.y % p.tiles) * kDecodeRows;
-    const int rows = p.r - row0 < kDecodeRows ? p.r - row0 : kDecodeRows;
     const int D = EXACT ? DP : cv.D;
+    const int items = cv.Hk * p.tiles;                               // of a sequence
 
-    const int len0 = cv.lens[seq], held = cv.max_pages << cv.page_shift;
-    const int len = len0 < 0 ? 0 : len0 < held ? len0 : held;
-    const int lo = p.window > 0 && len0 > p.window ? len0 - p.window : 0;
-    const int first = lo & ~(kStep - 1);                             // steps start at multiples of their length
-    const int steps = len > lo ? (len - first + kStep - 1) / kStep : 0;
-    const int by_grid = (steps + (int)gridDim.x - 1) / (int)gridDim.x;
-    const int per = by_grid > p.min_steps ? by_grid : p.min_steps;
-    const int splits = steps > per ? (steps + per - 1) / per : 1;
-    if (split >= splits) return;
-    const int s_end = (split + 1) * per < steps ? (split + 1) * per : steps;
-
-    // Q^T: column `col`, dimensions 64 j + 16 g + 8 a .. + 7 for products 2 j + a; zeros beyond the head's rows and dimensions.
-    half8_t qf[DP / 32];
-#pragma unroll
-    for (int j = 0; j < DP / 64; ++j)
-#pragma unroll
-        for (int a = 0; a < 2; ++a) {
-            half8_t w = {0, 0, 0, 0, 0, 0, 0, 0};
-            const int d = 64 * j + 16 * g + 8 * a;
-            if (col < rows && d < D) w = *reinterpret_cast<const half8_t*>(p.q + (size_t)seq * p.q_stride + (size_t)(head * p.r + row0 + col) * D + d);
-            qf[2 * j + a] = w;
-        }
-
-    float4_t o[DP / 16];
-#pragma unroll
-    for (int b = 0; b < DP / 16; ++b) o[b] = float4_t{0, 0, 0, 0};
-    float m = -INFINITY, l = 0.0f;
-
-    // Tokens of runs that start at or past the end take the last run's place: what is loaded there is masked.
-    auto run_at = [&](int step, int x) {
-        const int t = first + step * kStep + kRun * x;
-        return t < len ? t : (len - 1) & ~(kRun - 1);
+    // The most steps of a piece: such that there are no more pieces than workgroups, if that is little more than an even share of all steps;
+    // else that share, and some workgroups have a second piece.
+    int tokens = 0;                                                  // of the lane's sequence
+    auto steps_at = [&](int i) {
+        tokens = i < cv.seqs ? cv.lens[i] : 0;
+        return i < cv.seqs ? (unsigned)span_of(p, tokens).steps : 0u;
     };
-    auto load = [&](stage_t& st, int step) {
-        const int tk = run_at(step, col >> 2), tv = run_at(step, g);
-        int pk = page_of(cv, seq, tk >> cv.page_shift), pv = page_of(cv, seq, tv >> cv.page_shift);
-        st.ok = pv >= 0;
-        pk = pk < 0 ? 0 : pk;
-        pv = pv < 0 ? 0 : pv;
-        const int in_page = (1 << cv.page_shift) - 1, sk = tk & in_page, sv = tv & in_page;
-        constexpr int kSize = stage_t::kHalf ? 2 : 1;
-        const unsigned char* kp = cv.k + (page_at(cv, pk, head) + (size_t)(sk + (col & 3)) * D) * kSize;
-#pragma unroll
-        for (int n = 0; n < kTiles; ++n)
-#pragma unroll
-            for (int j = 0; j < DP / 64; ++j) {
-                const int d = 64 * j + 16 * g;
-                const bool in = EXACT || d < D;
-                const u32x4_t* src = reinterpret_cast<const u32x4_t*>(kp + (size_t)(4 * n * D + (in ? d : 0)) * kSize);
-#pragma unroll
-                for (int h = 0; h < kSize; ++h) {
-                    const u32x4_t w = src[h];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) st.k[n][j][4 * h + e] = in ? w[e] : 0u;
-                }
-            }
-        // [16 tokens of a dimension] in the group of 16 that the run is in
-        const unsigned char* vp = cv.v + (page_at(cv, pv, head) + (size_t)(sv & ~(kTokenGroup - 1)) * D + (size_t)col * kTokenGroup + (sv & (kTokenGroup - 1))) * kSize;
-#pragma unroll
-        for (int b = 0; b < DP / 16; ++b) {
-            if (!EXACT && 16 * b >= D) {
-#pragma unroll
-                for (int e = 0; e < kRun * kSize / 4; ++e) st.v[b][e] = 0;
-                continue;
-            }
-            const unsigned char* src = vp + (size_t)b * 16 * kTokenGroup * kSize;
-            if constexpr (kRun * kSize == 8) {
-                const u32x2_t w = *reinterpret_cast<const u32x2_t*>(src);
-                st.v[b][0] = w[0];
-                st.v[b][1] = w[1];
-            } else {
-#pragma unroll
-                for (int h = 0; h < kRun * kSize / 16; ++h) {
-                    const u32x4_t w = reinterpret_cast<const u32x4_t*>(src)[h];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) st.v[b][4 * h + e] = w[e];
-                }
+    unsigned mine = steps_at(lane), sum = mine, longest = mine;
+    for (int i = kWave; i < cv.seqs; i += kWave) {
+        const unsigned n = steps_at(i + lane);
+        sum += n;
+        longest = longest > n ? longest : n;
+    }
+    longest = wave_max(longest);
+    const unsigned groups = gridDim.x, all_items = (unsigned)(cv.seqs * items), total = wave_sum(sum) * (unsigned)items;
+    unsigned share = (total + (unsigned)p.slots - 1) / (unsigned)p.slots;
+    share = share > (unsigned)NW ? share : (unsigned)NW;
+    unsigned most = longest;
+    if (all_items <= groups) {
+        const unsigned each = groups / all_items;
+        most = (longest + each - 1) / each;                          // does for any lengths
+        if (cv.seqs <= kWave) {                                      // less may do for these
+            unsigned from = share;
+            for (int i = 0; i < 5 && from < most; ++i) {
+                const unsigned mid = (from + most) / 2;
+                if (wave_sum((mine + mid - 1) / mid) * (unsigned)items <= groups) most = mid;
+                else from = mid + 1;
             }
         }
-        if constexpr (SC != 0) {
-            const float* ksp = cv.k_scales + scales_at(cv, pv, head);
-            const float* vsp = cv.v_scales + scales_at(cv, pv, head);
-            if constexpr (SC == 1) {
-                st.ks[0] = ksp[sv >> cv.block_shift];
-                st.vs[0] = vsp[sv >> cv.block_shift];
-            } else {
+        most = most > (unsigned)NW ? most : (unsigned)NW;
+    }
+    if (most > share + kRoundSteps * NW) most = share;
+    if (longest <= most + kJoinSteps * NW) most = longest;
+
+    const_int* table = (const_int*)(uintptr_t)cv.table;
+
+    // where the lane's own operands lie in a stage
+    const uint32_t ring = lds0 + (uint32_t)(wave * T::kStages * T::kBytes);
+    const uint32_t k_read = ring + lane * 16;
+    const uint32_t v_read = T::kHalf ? k_read + T::kPart : ring + T::kPart + (uint32_t)((g >> 1) * 512 + col * 16 + (g & 1) * 8);
+    const uint32_t s_read = ring + 2 * T::kPart + g * 32;
+
+    for (unsigned piece = blockIdx.x;; piece += groups) {
+        // Its sequence and item, and steps begin .. s_end - 1: the k-th of the item's `parts`.
+        int seq = -1, item = 0, begin = 0, s_end = 0, k_part = 0, parts = 1;
+        Span sp = {};
+        unsigned kept = 0;                                           // pieces of cut items before this item's: their sums are kept apart
+        for (unsigned i = 0, before = 0; i < (unsigned)cv.seqs; i += kWave) {
+            if (cv.seqs > kWave) mine = steps_at((int)i + lane);
+            const unsigned n = (mine + most - 1) / most, several = n > 1 ? n : 0;
+            const unsigned past = before + wave_scan(n) * (unsigned)items, kept_past = kept + wave_scan(several) * (unsigned)items;
+            const unsigned long long in = __ballot(piece < past);
+            if (in) {
+                const int l = __builtin_ctzll(in);
+                const unsigned of_item = (unsigned)__builtin_amdgcn_readlane((int)n, l), length = (unsigned)__builtin_amdgcn_readlane((int)mine, l);
+                const unsigned local = piece - ((unsigned)__builtin_amdgcn_readlane((int)past, l) - of_item * (unsigned)items), size = (length + of_item - 1) / of_item;
+                seq = (int)i + l;
+                sp = span_of(p, __builtin_amdgcn_readlane(tokens, l));
+                item = __builtin_amdgcn_readfirstlane((int)(local / of_item));
+                k_part = __builtin_amdgcn_readfirstlane((int)(local % of_item));
+                parts = (int)of_item;
+                begin = __builtin_amdgcn_readfirstlane(k_part * (int)size);
+                s_end = __builtin_amdgcn_readfirstlane(begin + (int)size < (int)length ? begin + (int)size : (int)length);
+                kept = (unsigned)__builtin_amdgcn_readlane((int)kept_past, l) - (unsigned)(items - item) * of_item;
+                break;
+            }
+            kept = (unsigned)__builtin_amdgcn_readlane((int)kept_past, kWave - 1);
+            before = (unsigned)__builtin_amdgcn_readlane((int)past, kWave - 1);
+        }
+        if (seq < 0) return;
+        const int head = item / p.tiles, row0 = item % p.tiles * kDecodeRows;
+        const int rows = p.r - row0 < kDecodeRows ? p.r - row0 : kDecodeRows;
+
+        int page[2];
+        // A step's pages: those of its two groups of 16 tokens (one page, where pages are longer), by scalar loads ahead of their use.
+        // Groups past the end take the last one's place: what is loaded there does not count.
+        const_int* pages = table + (size_t)seq * cv.max_pages;
+        auto find = [&](int step) {
 #pragma unroll
-                for (int n = 0; n < kTiles; ++n) {
-                    const int at = (sv + 4 * n) >> cv.block_shift;
-                    float4_t a, b;
-                    if (cv.block_shift == 0) {
-                        a = *reinterpret_cast<const float4_t*>(ksp + at);
-                        b = *reinterpret_cast<const float4_t*>(vsp + at);
-                    } else if (cv.block_shift == 1) {
-                        const float2_t c = *reinterpret_cast<const float2_t*>(ksp + at), d = *reinterpret_cast<const float2_t*>(vsp + at);
-                        a = float4_t{c[0], c[0], c[1], c[1]};
-                        b = float4_t{d[0], d[0], d[1], d[1]};
+            for (int x = 0; x < 2; ++x) {
+                int t = sp.first + step * 32 + 16 * x;
+                t = t < sp.len ? t : sp.len > 0 ? sp.len - 1 : 0;
+                page[x] = pages[t >> cv.page_shift];
+            }
+        };
+        // bit x: group x has a page
+        auto request = [&](int step, int stage) {
+            const unsigned char *kp[2], *vp[2];
+            const float *ks[2], *vs[2];
+            int ok = 0;
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                int t = sp.first + step * 32 + 16 * x;
+                t = t < sp.len ? t : sp.len > 0 ? (sp.len - 1) & ~15 : 0;
+                const bool in = (unsigned)page[x] < (unsigned)cv.pages;
+                ok |= in ? 1 << x : 0;
+                const int pg = in ? page[x] : 0, slot = t & ((1 << cv.page_shift) - 1);
+                kp[x] = cv.k + (page_at(cv, pg, head) + (size_t)slot * D) * T::kSize;
+                vp[x] = cv.v + (page_at(cv, pg, head) + (size_t)slot * D) * T::kSize;
+                if constexpr (!T::kHalf) {
+                    ks[x] = cv.k_scales + scales_at(cv, pg, head) + (slot >> cv.block_shift);
+                    vs[x] = cv.v_scales + scales_at(cv, pg, head) + (slot >> cv.block_shift);
+                }
+            }
+            const uint32_t to = ring + (uint32_t)(stage * T::kBytes);
+            // keys: lane (col, g) reads dimensions 64 j + 16 g .. + 15 of token 8 (col / 4) + 4 n + col % 4
+            const unsigned char* k = (col >= 8 ? kp[1] : kp[0]) + (size_t)((8 * ((col >> 2) & 1) + (col & 3)) * D) * T::kSize;
+#pragma unroll
+            for (int n = 0; n < T::kTiles; ++n)
+#pragma unroll
+                for (int j = 0; j < DP / 64; ++j) {
+                    const int d = 64 * j + 16 * g;
+#pragma unroll
+                    for (int h = 0; h < T::kSize; ++h)
+                        request16(to + (uint32_t)(((n * (DP / 64) + j) * T::kSize + h) * 1024), k + (4 * n * D + (EXACT || d < D ? d : 0)) * T::kSize + 16 * h);
+                }
+            if constexpr (T::kHalf) {
+                // values: lane (col, g) reads tokens 8 g .. 8 g + 7 of dimension 16 b + col
+                const unsigned char* v = (g >= 2 ? vp[1] : vp[0]) + col * 32 + (g & 1) * 16;
+#pragma unroll
+                for (int b = 0; b < DP / 16; ++b) request16(to + (uint32_t)(T::kPart + b * 1024), v + (EXACT || 16 * b < D ? b : 0) * 512);
+            } else {
+                // .. lane l reads the 16 tokens of group l / 32 of dimension 32 b + l % 32
+                const unsigned char* v = (lane >= 32 ? vp[1] : vp[0]);
+#pragma unroll
+                for (int b = 0; b < DP / 32; ++b) {
+                    const int d = 32 * b + (lane & 31);
+                    request16(to + (uint32_t)(T::kPart + b * 1024), v + (EXACT || d < D ? d : 0) * 16);
+                }
+                // scales: lane l reads that of token l % 32's key, or from 32 on value
+                const float* s = lane & 16 ? (lane & 32 ? vs[1] : ks[1]) : (lane & 32 ? vs[0] : ks[0]);
+                request4(to + 2 * T::kPart, s + ((lane & 15) >> cv.block_shift));
+            }
+            return ok;
+        };
+
+        // Q^T: column `col`, dimensions 64 j + 16 g + 8 a .. + 7 for products 2 j + a; zeros beyond the head's rows and dimensions.
+        half8_t qf[DP / 32];
+#pragma unroll
+        for (int j = 0; j < DP / 64; ++j)
+#pragma unroll
+            for (int a = 0; a < 2; ++a) {
+                half8_t w = {0, 0, 0, 0, 0, 0, 0, 0};
+                const int d = 64 * j + 16 * g + 8 * a;
+                if (col < rows && d < D) w = *reinterpret_cast<const half8_t*>(p.q + (size_t)seq * p.q_stride + (size_t)(head * p.r + row0 + col) * D + d);
+                qf[2 * j + a] = w;
+            }
+
+        float4_t o[DP / 16];
+#pragma unroll
+        for (int b = 0; b < DP / 16; ++b) o[b] = float4_t{0, 0, 0, 0};
+        float m = -INFINITY, l = 0.0f;
+
+        // WHOLE: all its tokens count
+        auto compute_as = [&](auto is_whole, int step, int stage, int ok) {
+            constexpr bool whole = decltype(is_whole)::value;
+            const uint32_t off = (uint32_t)(stage * T::kBytes);
+            float4_t s[T::kTiles];
+#pragma unroll
+            for (int n = 0; n < T::kTiles; ++n) {
+                s[n] = float4_t{0, 0, 0, 0};
+#pragma unroll
+                for (int j = 0; j < DP / 64; ++j) {
+                    const bool in = EXACT || 64 * j + 16 * g < D;
+                    half8_t kf[2];
+                    if constexpr (T::kHalf) {
+#pragma unroll
+                        for (int a = 0; a < 2; ++a) {
+                            u32x4_t w = *(const lds_words4*)(uintptr_t)(k_read + off + (uint32_t)(((n * (DP / 64) + j) * 2 + a) * 1024));
+                            if (!EXACT && !in) w = u32x4_t{0, 0, 0, 0};
+                            kf[a] = __builtin_bit_cast(half8_t, w);
+                        }
                     } else {
-                        const float c = ksp[at], d = vsp[at];
-                        a = float4_t{c, c, c, c};
-                        b = float4_t{d, d, d, d};
+                        u32x4_t w = *(const lds_words4*)(uintptr_t)(k_read + off + (uint32_t)((n * (DP / 64) + j) * 1024));
+                        if (!EXACT && !in) w = u32x4_t{0, 0, 0, 0};
+                        kf[0] = codes_to_half<TYPE>(w[0], w[1]);
+                        kf[1] = codes_to_half<TYPE>(w[2], w[3]);
                     }
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) { st.ks[4 * n + r] = a[r]; st.vs[4 * n + r] = b[r]; }
+                    s[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[0], qf[2 * j], s[n], 0, 0, 0);
+                    s[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[1], qf[2 * j + 1], s[n], 0, 0, 0);
                 }
             }
-        }
-    };
-
-    auto compute = [&](stage_t& st, int step) {
-        float4_t s[kTiles];
+            const int t0 = sp.first + step * 32, t = t0 + 8 * g;
+            // of the run's tokens, those that count
+            const int vlo = sp.lo > t ? sp.lo - t : 0, vhi = !(ok >> (g >> 1) & 1) || t >= sp.len ? 0 : sp.len - t;
+            float4_t vs[T::kTiles];
 #pragma unroll
-        for (int n = 0; n < kTiles; ++n) {
-            s[n] = float4_t{0, 0, 0, 0};
-#pragma unroll
-            for (int j = 0; j < DP / 64; ++j)
-#pragma unroll
-                for (int a = 0; a < 2; ++a) {
-                    half8_t kf;
-                    if constexpr (stage_t::kHalf) kf = __builtin_bit_cast(half8_t, u32x4_t{st.k[n][j][4 * a], st.k[n][j][4 * a + 1], st.k[n][j][4 * a + 2], st.k[n][j][4 * a + 3]});
-                    else kf = codes_to_half<TYPE>(st.k[n][j][2 * a], st.k[n][j][2 * a + 1]);
-                    s[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[2 * j + a], s[n], 0, 0, 0);
+            for (int n = 0; n < T::kTiles; ++n) {
+                if constexpr (T::kHalf) s[n] *= p.scale;
+                else {
+                    s[n] *= *(const lds_float4*)(uintptr_t)(s_read + off + (uint32_t)(16 * n)) * p.scale;
+                    vs[n] = *(const lds_float4*)(uintptr_t)(s_read + off + (uint32_t)(128 + 16 * n));
                 }
-        }
-        const int t0 = first + step * kStep, t = t0 + kRun * g;
-        const bool whole = t0 >= lo && t0 + kStep <= len && __all(st.ok);
-        float vs[SC == 2 ? 4 * kTiles : 1], lg[SC == 2 ? 4 * kTiles : 1];
+            }
+            if (!whole) {
 #pragma unroll
-        for (int i = 0; i < (SC == 2 ? 4 * kTiles : 1); ++i) vs[i] = SC ? st.vs[i] : 1.0f;
+                for (int n = 0; n < T::kTiles; ++n)
 #pragma unroll
-        for (int n = 0; n < kTiles; ++n)
+                    for (int r = 0; r < 4; ++r) {
+                        const bool seen = 4 * n + r >= vlo && 4 * n + r < vhi;
+                        s[n][r] = seen ? s[n][r] : -INFINITY;
+                        if constexpr (!T::kHalf) vs[n][r] = seen ? vs[n][r] : 0.0f;
+                    }
+            }
+            // The maximum is taken over score + log2 of the value's scale, so that weight times scale, rounded to fp16, is at most 1.
+            float most = -INFINITY;
+            if (T::kHalf || (whole && cv.block_shift >= 3)) {           // one scale for the run
 #pragma unroll
-            for (int r = 0; r < 4; ++r) s[n][r] *= (SC == 0 ? 1.0f : st.ks[SC == 2 ? 4 * n + r : 0]) * p.scale;
-        const int vlo = lo > t ? lo - t : 0, vhi = !st.ok || t >= len ? 0 : len - t;        // of the run's tokens, those that count
-        if (!whole) {
+                for (int n = 0; n < T::kTiles; ++n)
 #pragma unroll
-            for (int n = 0; n < kTiles; ++n)
+                    for (int r = 0; r < 4; ++r) most = fmaxf(most, s[n][r]);
+                if constexpr (!T::kHalf) most += fmaxf(__builtin_amdgcn_logf(vs[0][0]), kLeastLog);
+            } else if constexpr (!T::kHalf) {
+#pragma unroll
+                for (int n = 0; n < T::kTiles; ++n)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) most = fmaxf(most, s[n][r] + fmaxf(__builtin_amdgcn_logf(vs[n][r]), kLeastLog));
+            }
+            most = over_groups(most, [](float a, float b) { return fmaxf(a, b); });
+            const float m_new = fmaxf(m, most), base = m_new == -INFINITY ? 0.0f : m_new;
+            const float keep = __builtin_amdgcn_exp2f(m - base);
+            m = m_new;
+            float add = 0.0f;
+            half8_t pf;
+#pragma unroll
+            for (int n = 0; n < T::kTiles; ++n)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const bool seen = 4 * n + r >= vlo && 4 * n + r < vhi;
-                    s[n][r] = seen ? s[n][r] : -INFINITY;
-                    if (SC == 2) vs[4 * n + r] = seen ? vs[4 * n + r] : 0.0f;
+                    const float w = __builtin_amdgcn_exp2f(s[n][r] - base);
+                    add += w;
+                    pf[4 * n + r] = (_Float16)(T::kHalf ? w : w * vs[n][r]);
                 }
-            if (SC == 1) vs[0] = vhi > vlo ? vs[0] : 0.0f;
+            l = l * keep + add;
             // values that do not count are zeros: what lies there may be a NaN
+            u32x4_t mask = {~0u, ~0u, ~0u, ~0u};
+            if (!whole) {
 #pragma unroll
-            for (int i = 0; i < kRun; ++i) {
-                const bool seen = i >= vlo && i < vhi;
-#pragma unroll
-                for (int b = 0; b < DP / 16; ++b) {
-                    if constexpr (stage_t::kHalf) st.v[b][i / 2] = seen ? st.v[b][i / 2] : st.v[b][i / 2] & (i & 1 ? 0x0000ffffu : 0xffff0000u);
-                    else st.v[b][i / 4] = seen ? st.v[b][i / 4] : st.v[b][i / 4] & ~(0xffu << (8 * (i & 3)));
-                }
+                for (int i = 0; i < 8; ++i)
+                    if (!(i >= vlo && i < vhi)) {
+                        if constexpr (T::kHalf) mask[i / 2] &= i & 1 ? 0x0000ffffu : 0xffff0000u;
+                        else mask[i / 4] &= ~(0xffu << (8 * (i & 3)));
+                    }
             }
-        }
-        // The maximum is taken over score + log2 of the value's scale, so that weight times scale, rounded to fp16, is at most 1.
-        float most = -INFINITY;
-        if constexpr (SC != 0) {
+            if (!__all(keep == 1.0f)) {
 #pragma unroll
-            for (int i = 0; i < (SC == 2 ? 4 * kTiles : 1); ++i) lg[i] = fmaxf(__builtin_amdgcn_logf(vs[i]), kLeastLog);
-        }
+                for (int b = 0; b < DP / 16; ++b)
 #pragma unroll
-        for (int n = 0; n < kTiles; ++n)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) most = fmaxf(most, SC == 2 ? s[n][r] + lg[4 * n + r] : s[n][r]);
-        if (SC == 1) most += lg[0];
-        most = fmaxf(most, __shfl_xor(most, 16));
-        most = fmaxf(most, __shfl_xor(most, 32));
-        const float m_new = fmaxf(m, most), base = m_new == -INFINITY ? 0.0f : m_new;
-        const float keep = __builtin_amdgcn_exp2f(m - base);
-        m = m_new;
-        float sum = 0.0f;
-        half8_t pf[A];
-#pragma unroll
-        for (int n = 0; n < kTiles; ++n)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const float w = __builtin_amdgcn_exp2f(s[n][r] - base);
-                sum += w;
-                pf[n / 2][4 * (n & 1) + r] = (_Float16)(SC == 0 ? w : w * vs[SC == 2 ? 4 * n + r : 0]);
+                    for (int r = 0; r < 4; ++r) o[b][r] *= keep;
             }
-        l = l * keep + sum;
-#pragma unroll
-        for (int b = 0; b < DP / 16; ++b) {
-#pragma unroll
-            for (int r = 0; r < 4; ++r) o[b][r] *= keep;
-#pragma unroll
-            for (int a = 0; a < A; ++a) {
-                half8_t vf;
-                if constexpr (stage_t::kHalf) vf = __builtin_bit_cast(half8_t, u32x4_t{st.v[b][4 * a], st.v[b][4 * a + 1], st.v[b][4 * a + 2], st.v[b][4 * a + 3]});
-                else vf = codes_to_half<TYPE>(st.v[b][2 * a], st.v[b][2 * a + 1]);
-                o[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[a], o[b], 0, 0, 0);
-            }
-        }
-    };
-
-    {
-        stage_t st0, st1;
-        int s = split * per + wave;
-        if (s < s_end) load(st0, s);
-        while (s < s_end) {
-            if (s + kDecodeWaves < s_end) load(st1, s + kDecodeWaves);
-            __builtin_amdgcn_sched_barrier(0);
-            compute(st0, s);
-            s += kDecodeWaves;
-            if (s >= s_end) break;
-            if (s + kDecodeWaves < s_end) load(st0, s + kDecodeWaves);
-            __builtin_amdgcn_sched_barrier(0);
-            compute(st1, s);
-            s += kDecodeWaves;
-        }
-    }
-
-    // The lane groups' sums, then the wavefronts': the upper half hands its own to the lower half, in rounds.
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
-#pragma unroll
-    for (int half = kDecodeWaves / 2; half > 0; half >>= 1) {
-        if (wave >= half && wave < 2 * half) {
-            float* to = merge + ((wave - half) * kDecodeRows + col) * kPitch;
-#pragma unroll
-            for (int b = 0; b < DP / 16; ++b) *reinterpret_cast<float4_t*>(to + 16 * b + 4 * g) = o[b];
-            if (g == 0) {
-                merge_ml[((wave - half) * kDecodeRows + col) * 2] = m;
-                merge_ml[((wave - half) * kDecodeRows + col) * 2 + 1] = l;
-            }
-        }
-        __syncthreads();
-        if (wave < half) {
-            const float* from = merge + (wave * kDecodeRows + col) * kPitch;
-            const float m2 = merge_ml[(wave * kDecodeRows + col) * 2], l2 = merge_ml[(wave * kDecodeRows + col) * 2 + 1];
-            const float m_new = fmaxf(m, m2), base = m_new == -INFINITY ? 0.0f : m_new;
-            const float a = __builtin_amdgcn_exp2f(m - base), c = __builtin_amdgcn_exp2f(m2 - base);
-            m = m_new;
-            l = l * a + l2 * c;
 #pragma unroll
             for (int b = 0; b < DP / 16; ++b) {
-                const float4_t w = *reinterpret_cast<const float4_t*>(from + 16 * b + 4 * g);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) o[b][r] = o[b][r] * a + w[r] * c;
+                half8_t vf;
+                if constexpr (T::kHalf) {
+                    u32x4_t w = *(const lds_words4*)(uintptr_t)(v_read + off + (uint32_t)(b * 1024));
+                    if (!whole) w &= mask;
+                    vf = __builtin_bit_cast(half8_t, w);
+                } else {
+                    u32x2_t w = *(const lds_words2*)(uintptr_t)(v_read + off + (uint32_t)((b >> 1) * 1024 + (b & 1) * 256));
+                    if (!whole) w &= u32x2_t{mask[0], mask[1]};
+                    vf = codes_to_half<TYPE>(w[0], w[1]);
+                }
+                o[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf, o[b], 0, 0, 0);
             }
+        };
+
+        auto compute = [&](int step, int stage, int ok) {
+            const int t0 = sp.first + step * 32;
+            if (t0 >= sp.lo && t0 + 32 <= sp.len && ok == 3) compute_as(std::true_type(), step, stage, ok);
+            else compute_as(std::false_type(), step, stage, ok);
+        };
+
+        // The wavefront's steps: two stages, each asked for again as soon as it has been read.
+        {
+            int s = begin + wave, stage = 0, ok = 0, next = 0;
+            if (s < s_end) {
+                find(s);
+                ok = request(s, 0);
+            }
+            if (s + NW < s_end) {
+                find(s + NW);
+                next = request(s + NW, 1);
+            }
+            if (s + 2 * NW < s_end) find(s + 2 * NW);
+            // The queries are here before the loop: in it, the compiler's wait for them would be one for every request.
+#pragma unroll
+            for (int i = 0; i < DP / 32; ++i) asm volatile("" : "+v"(qf[i]));
+            for (; s < s_end; s += NW) {
+                if (s + NW < s_end) asm volatile("s_waitcnt vmcnt(%0)" :: "n"(T::kRequests) : "memory");
+                else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                compute(s, stage, ok);
+                ok = next;
+                if (s + 2 * NW < s_end) {
+                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // the stage has been read
+                    next = request(s + 2 * NW, stage);
+                    if (s + 3 * NW < s_end) find(s + 3 * NW);
+                }
+                stage ^= 1;
+            }
+        }
+        l = over_groups(l, [](float a, float b) { return a + b; });
+
+        // Every wavefront leaves its sums in its own first stage, then takes some blocks of 16 dimensions and adds up all wavefronts' sums of
+        // them, each lane those of its own place.
+#pragma unroll
+        for (int b = 0; b < DP / 16; ++b) *(lds_float4*)(uintptr_t)(ring + (uint32_t)(b * 1024 + lane * 16)) = o[b];
+        if (g == 0) {
+            *(lds_float1*)(uintptr_t)(ml_at + (uint32_t)((wave * kDecodeRows + col) * 8)) = m;
+            *(lds_float1*)(uintptr_t)(ml_at + (uint32_t)((wave * kDecodeRows + col) * 8 + 4)) = l;
         }
         __syncthreads();
-    }
-
-    _Float16* out = p.out + (size_t)seq * p.out_stride + (size_t)(head * p.r + row0) * D;
-    if (splits == 1) {
-        if (wave == 0 && col < rows) {
-            const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+        float top = -INFINITY, weight = 0.0f, by[NW];
+        {
+            float ls[NW];
 #pragma unroll
-            for (int b = 0; b < DP / 16; ++b)
-                if (EXACT || 16 * b < D)
-                    *reinterpret_cast<half4_t*>(out + (size_t)col * D + 16 * b + 4 * g) =
-                        half4_t{(_Float16)(o[b][0] * inv), (_Float16)(o[b][1] * inv), (_Float16)(o[b][2] * inv), (_Float16)(o[b][3] * inv)};
-        }
-        return;
-    }
-
-    // Several ranges: all data that crosses workgroups is moved by device-scope accesses, acknowledged before the ticket is taken; the
-    // last workgroup of the sequence's heads adds the ranges in order and leaves the counter at zero.
-    const size_t item = (size_t)seq * gridDim.y + blockIdx.y;
-    float* part = p.part + item * gridDim.x * (kDecodeRows * (size_t)(D + 2));
-    if (wave == 0 && col < rows) {
-        float* to = part + ((size_t)split * kDecodeRows + col) * (D + 2);
-        auto put = [&](float* at, float a, float b) {
-            const unsigned long long w = (unsigned long long)__builtin_bit_cast(uint32_t, b) << 32 | __builtin_bit_cast(uint32_t, a);
-            __hip_atomic_store(reinterpret_cast<unsigned long long*>(at), w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        };
-#pragma unroll
-        for (int b = 0; b < DP / 16; ++b)
-            if (EXACT || 16 * b < D) {
-                put(to + 16 * b + 4 * g, o[b][0], o[b][1]);
-                put(to + 16 * b + 4 * g + 2, o[b][2], o[b][3]);
+            for (int w = 0; w < NW; ++w) {
+                by[w] = *(const lds_float1*)(uintptr_t)(ml_at + (uint32_t)((w * kDecodeRows + col) * 8));
+                ls[w] = *(const lds_float1*)(uintptr_t)(ml_at + (uint32_t)((w * kDecodeRows + col) * 8 + 4));
+                top = fmaxf(top, by[w]);
             }
-        if (g == 0) put(to + D, m, l);
-    }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (tid == 0) {
-        uint32_t* ctr = p.counters + item * p.cstride;
-        const bool last = __hip_atomic_fetch_add(ctr, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(splits - 1);
-        if (last) __hip_atomic_store(ctr, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        flag = last ? 1u : 0u;
-    }
-    __syncthreads();
-    if (flag == 0u) return;
-    auto get = [&](const float* at) {
-        return __hip_atomic_load(reinterpret_cast<const unsigned long long*>(at), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    };
-    auto low = [](unsigned long long w) { return __builtin_bit_cast(float, (uint32_t)w); };
-    auto high = [](unsigned long long w) { return __builtin_bit_cast(float, (uint32_t)(w >> 32)); };
-    static_assert(kMaxSplits * 2 <= (kDecodeWaves / 2) * (64 + 4), "the ranges' weights fit where the wavefronts' sums were");
-    float* ml = merge;                                                // [split][16][2]
-    for (int i = tid; i < splits * kDecodeRows; i += kDecodeWaves * kWave) {
-        unsigned long long w = 0;
-        if (i % kDecodeRows < rows) w = get(part + (size_t)i * (D + 2) + D);
-        ml[2 * i] = low(w);
-        ml[2 * i + 1] = high(w);
-    }
-    __syncthreads();
-    if (tid < rows) {
-        float most = -INFINITY, sum = 0.0f;
-        for (int i = 0; i < splits; ++i) most = fmaxf(most, ml[2 * (i * kDecodeRows + tid)]);
-        const float base = most == -INFINITY ? 0.0f : most;
-        for (int i = 0; i < splits; ++i) {
-            const float w = __builtin_amdgcn_exp2f(ml[2 * (i * kDecodeRows + tid)] - base);
-            sum += w * ml[2 * (i * kDecodeRows + tid) + 1];
-            ml[2 * (i * kDecodeRows + tid)] = w;
+            const float base = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+            for (int w = 0; w < NW; ++w) {
+                by[w] = __builtin_amdgcn_exp2f(by[w] - base);
+                weight += by[w] * ls[w];
+            }
         }
-        merge_ml[tid] = sum == 0.0f ? 0.0f : 1.0f / sum;
-    }
-    __syncthreads();
-    for (int i = tid; i < rows * (D / 2); i += kDecodeWaves * kWave) {
-        const int row = i / (D / 2), d = i % (D / 2) * 2;
-        const float* from = part + (size_t)row * (D + 2) + d;
-        float a = 0.0f, b = 0.0f;
-#pragma unroll 8
-        for (int k = 0; k < splits; ++k) {
-            const unsigned long long w = get(from + (size_t)k * kDecodeRows * (D + 2));
-            const float by = ml[2 * (k * kDecodeRows + row)];
-            a += by * low(w);
-            b += by * high(w);
+        float4_t mine_o[T::kBlocks];
+#pragma unroll
+        for (int i = 0; i < T::kBlocks; ++i) {
+            const int b = wave * T::kBlocks + i;
+            mine_o[i] = float4_t{0, 0, 0, 0};
+            if (16 * b >= DP) continue;
+#pragma unroll
+            for (int w = 0; w < NW; ++w) {
+                const float4_t x = *(const lds_float4*)(uintptr_t)(lds0 + (uint32_t)(w * T::kStages * T::kBytes + b * 1024 + lane * 16));
+#pragma unroll
+                for (int r = 0; r < 4; ++r) mine_o[i][r] = __builtin_fmaf(by[w], x[r], mine_o[i][r]);
+            }
         }
-        const float inv = merge_ml[row];
-        *reinterpret_cast<half2_t*>(out + (size_t)row * D + d) = half2_t{(_Float16)(a * inv), (_Float16)(b * inv)};
+        auto store = [&](int b, const float4_t& x, float inv) {
+            _Float16* out = p.out + (size_t)seq * p.out_stride + (size_t)(head * p.r + row0 + col) * D + 16 * b + 4 * g;
+            if (col < rows && 16 * b < D) *reinterpret_cast<half4_t*>(out) = half4_t{(_Float16)(x[0] * inv), (_Float16)(x[1] * inv), (_Float16)(x[2] * inv), (_Float16)(x[3] * inv)};
+        };
+        if (parts == 1) {
+            const float inv = weight == 0.0f ? 0.0f : 1.0f / weight;
+#pragma unroll
+            for (int i = 0; i < T::kBlocks; ++i) store(wave * T::kBlocks + i, mine_o[i], inv);
+        } else {
+            // All data that crosses workgroups is moved by device-scope accesses, acknowledged before the ticket is taken; the last workgroup of
+            // the item adds the pieces in order and leaves the counter at zero.
+            const size_t each = (size_t)kDecodeRows * (D + 2);
+            const float* first = p.part + (size_t)kept * each;
+            float* to = p.part + (size_t)(kept + (unsigned)k_part) * each;
+            auto put = [&](float* at, float a, float b) {
+                const unsigned long long w = (unsigned long long)__builtin_bit_cast(uint32_t, b) << 32 | __builtin_bit_cast(uint32_t, a);
+                __hip_atomic_store(reinterpret_cast<unsigned long long*>(at), w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            };
+            if (col < rows) {
+#pragma unroll
+                for (int i = 0; i < T::kBlocks; ++i) {
+                    const int b = wave * T::kBlocks + i;
+                    if (16 * b >= D) continue;
+                    put(to + (b * kWave + lane) * 4, mine_o[i][0], mine_o[i][1]);
+                    put(to + (b * kWave + lane) * 4 + 2, mine_o[i][2], mine_o[i][3]);
+                }
+                if (wave == 0 && g == 0) put(to + kDecodeRows * D + 2 * col, top, weight);
+            }
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();
+            if (tid == 0) {
+                uint32_t* ctr = p.counters + (size_t)kept * kCounterAreaWords / (4 * kDecodeUnits);
+                const bool last = __hip_atomic_fetch_add(ctr, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(parts - 1);
+                if (last) __hip_atomic_store(ctr, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                *flag = last ? 1u : 0u;
+            }
+            __syncthreads();
+            if (*flag != 0u && col < rows) {
+                auto get = [&](const float* from) {
+                    return __hip_atomic_load(reinterpret_cast<const unsigned long long*>(from), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                };
+                auto low = [](unsigned long long w) { return __builtin_bit_cast(float, (uint32_t)w); };
+                auto high = [](unsigned long long w) { return __builtin_bit_cast(float, (uint32_t)(w >> 32)); };
+                for (int b = wave; 16 * b < D; b += NW) {
+                    float4_t x = {0, 0, 0, 0};
+                    float upto = -INFINITY, all = 0.0f;
+                    for (int k0 = 0; k0 < parts; k0 += 8) {
+                        unsigned long long w[8], ml[8], v[8];
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            const float* from = first + (size_t)(k0 + k < parts ? k0 + k : k0) * each;
+                            ml[k] = get(from + kDecodeRows * D + 2 * col);
+                            w[k] = get(from + (b * kWave + lane) * 4);
+                            v[k] = get(from + (b * kWave + lane) * 4 + 2);
+                        }
+                        float m_new = upto;
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) m_new = fmaxf(m_new, low(ml[k]));
+                        const float base = m_new == -INFINITY ? 0.0f : m_new, keep = __builtin_amdgcn_exp2f(upto - base);
+                        upto = m_new;
+                        all *= keep;
+                        x *= keep;
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            if (k0 + k >= parts) continue;
+                            const float f = __builtin_amdgcn_exp2f(low(ml[k]) - base);
+                            all += f * high(ml[k]);
+                            x[0] += f * low(w[k]);
+                            x[1] += f * high(w[k]);
+                            x[2] += f * low(v[k]);
+                            x[3] += f * high(v[k]);
+                        }
+                    }
+                    store(b, x, all == 0.0f ? 0.0f : 1.0f / all);
+                }
+            }
+        }
+        __syncthreads();                                              // the sums' places and the flag are free again
     }
 }
+
+int set_max_lds(const void* fn, size_t bytes);
 
 int check_attn(const codegemm_attn_desc* d)
 {
@@ -431,7 +601,8 @@ int check_attn(const codegemm_attn_desc* d)
 namespace {
 
 struct DecodePlan {
-    int r, tiles, splits, step, min_steps, cstride;
+    int r, tiles, groups;
+    bool narrow;
     size_t bytes;        // of workspace
 };
 
@@ -443,38 +614,49 @@ int decode_plan(const codegemm_kv_cache* cache, const codegemm_attn_desc* d, Dec
     if (d->kv_heads != cache->kv_heads || d->head_dim != cache->head_dim || d->num_seqs != cache->num_seqs || d->total_q != d->num_seqs) return CODEGEMM_INVALID_ARG;
     p->r = d->q_heads / d->kv_heads;
     p->tiles = ceil_div(p->r, kDecodeRows);
-    const bool half = cache->dtype == CODEGEMM_KV_FP16;
-    p->step = half || d->head_dim > 128 || cache->scale_block < kTokenGroup ? 32 : 64;
-    // Keys in ranges until the workgroups fill the chip twice, but no range under two steps for each wavefront.
-    const int items = d->num_seqs * d->kv_heads * p->tiles;
+    // A workgroup counts all steps there are in 32 bits.
+    if ((long long)cache->num_seqs * (((long long)cache->max_pages * cache->page_size + 31) / 32) * d->kv_heads * p->tiles >= 1ll << 31) return CODEGEMM_UNSUPPORTED;
+    // Up to as many items as there are compute units, a unit works on one: a workgroup each, or for all the pieces of 4 steps that there may be as
+    // far as the host knows (any number is right).  More items: two at a time.
+    const long long items = (long long)d->num_seqs * d->kv_heads * p->tiles;
     const int keys = d->window > 0 && d->window < d->max_kv ? d->window : d->max_kv;
-    const int steps = ceil_div(keys, p->step) + 1;
-    p->min_steps = 2 * kDecodeWaves;
-    int splits = items >= 512 ? 1 : ceil_div(512, items);
-    if (splits > ceil_div(steps, p->min_steps)) splits = ceil_div(steps, p->min_steps);
-    if (splits > kMaxSplits) splits = kMaxSplits;
-    if (items > kCounterAreaWords) splits = 1;
-    p->splits = splits;
-    p->cstride = items * kCounterStride <= kCounterAreaWords ? kCounterStride : items > 0 && items <= kCounterAreaWords ? kCounterAreaWords / items : 0;
-    p->bytes = (size_t)kCounterAreaWords * sizeof(uint32_t) + kPairAreaBytes;
-    if (splits > 1) p->bytes += (size_t)items * splits * kDecodeRows * (d->head_dim + 2) * sizeof(float);
+    const long long pieces = (ceil_div(keys, 32) + 1ll) / 4 * items + items;
+    p->narrow = items > kDecodeUnits;
+    const int slots = p->narrow ? 2 * kDecodeUnits : kDecodeUnits;
+    p->groups = (int)(items > slots ? items : pieces < slots ? pieces : slots);
+    // A cut item of x shares has at most 2 x pieces, and there are as many shares as workgroups that run at once.
+    p->bytes = (size_t)kCounterAreaWords * sizeof(uint32_t) + kPairAreaBytes + 2 * (size_t)(p->groups < slots ? p->groups : slots) * kDecodeRows * (d->head_dim + 2) * sizeof(float);
     return CODEGEMM_OK;
 }
 
-template <int TYPE, int DP, int SC>
-void launch_decode(const DecodeParams& p, dim3 grid, hipStream_t s)
+template <int TYPE, int DP, bool EXACT, bool NARROW>
+int launch_decode_one(DecodeParams& p, int groups, hipStream_t s)
 {
-    const dim3 threads(kDecodeWaves * kWave);
-    if (p.c.D == DP) hipLaunchKernelGGL((attn_decode_kernel<TYPE, DP, SC, true>), grid, threads, 0, s, p);
-    else hipLaunchKernelGGL((attn_decode_kernel<TYPE, DP, SC, false>), grid, threads, 0, s, p);
+    typedef DecodeStep<TYPE, DP, NARROW> T;
+    static_assert(T::kLds * T::kPerCu <= kMaxLds, "LDS");
+    auto fn = attn_decode_kernel<TYPE, DP, EXACT, NARROW>;
+    const int st = set_max_lds(reinterpret_cast<const void*>(fn), T::kLds);
+    if (st) return st;
+    p.slots = groups < kDecodeUnits * T::kPerCu ? groups : kDecodeUnits * T::kPerCu;
+    hipLaunchKernelGGL(fn, dim3((unsigned)groups), dim3(T::kWaves * kWave), T::kLds, s, p);
+    return hipGetLastError() == hipSuccess ? CODEGEMM_OK : CODEGEMM_LAUNCH_FAILED;
 }
 
-template <int TYPE, int SC>
-void launch_decode_of(const DecodeParams& p, dim3 grid, hipStream_t s)
+template <int TYPE, int DP>
+int launch_decode(DecodeParams& p, bool narrow, int groups, hipStream_t s)
 {
-    if (p.c.D <= 64) launch_decode<TYPE, 64, SC>(p, grid, s);
-    else if (p.c.D <= 128) launch_decode<TYPE, 128, SC>(p, grid, s);
-    else launch_decode<TYPE, 256, SC>(p, grid, s);
+    if constexpr (DecodeStep<TYPE, DP, true>::kPerCu == 2) {
+        if (narrow) return p.c.D == DP ? launch_decode_one<TYPE, DP, true, true>(p, groups, s) : launch_decode_one<TYPE, DP, false, true>(p, groups, s);
+    }
+    return p.c.D == DP ? launch_decode_one<TYPE, DP, true, false>(p, groups, s) : launch_decode_one<TYPE, DP, false, false>(p, groups, s);
+}
+
+template <int TYPE>
+int launch_decode_of(DecodeParams& p, bool narrow, int groups, hipStream_t s)
+{
+    if (p.c.D <= 64) return launch_decode<TYPE, 64>(p, narrow, groups, s);
+    if (p.c.D <= 128) return launch_decode<TYPE, 128>(p, narrow, groups, s);
+    return launch_decode<TYPE, 256>(p, narrow, groups, s);
 }
 
 }  // namespace
@@ -503,19 +685,14 @@ extern "C" int codegemm_attn_decode(const codegemm_kv_cache* cache, const codege
     p.out = static_cast<_Float16*>(out);
     p.counters = static_cast<uint32_t*>(workspace);
     p.part = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + (size_t)kCounterAreaWords * sizeof(uint32_t) + kPairAreaBytes);
-    p.cstride = plan.cstride;
     p.r = plan.r;
     p.tiles = plan.tiles;
     p.q_stride = row_stride(desc->q_stride, desc->q_heads * desc->head_dim);
     p.out_stride = row_stride(desc->out_stride, desc->q_heads * desc->head_dim);
     p.window = desc->window;
-    p.min_steps = plan.min_steps;
     p.scale = (float)(desc->scale * 1.4426950408889634);
-    const dim3 grid((unsigned)plan.splits, (unsigned)(desc->kv_heads * plan.tiles), (unsigned)desc->num_seqs);
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const bool single = cache->scale_block >= kTokenGroup;
-    if (cache->dtype == CODEGEMM_KV_FP16) launch_decode_of<CODEGEMM_KV_FP16, 0>(p, grid, s);
-    else if (cache->dtype == CODEGEMM_KV_INT8) single ? launch_decode_of<CODEGEMM_KV_INT8, 1>(p, grid, s) : launch_decode_of<CODEGEMM_KV_INT8, 2>(p, grid, s);
-    else single ? launch_decode_of<CODEGEMM_KV_FP8, 1>(p, grid, s) : launch_decode_of<CODEGEMM_KV_FP8, 2>(p, grid, s);
-    return hipGetLastError() == hipSuccess ? CODEGEMM_OK : CODEGEMM_LAUNCH_FAILED;
+    if (cache->dtype == CODEGEMM_KV_FP16) return launch_decode_of<CODEGEMM_KV_FP16>(p, plan.narrow, plan.groups, s);
+    if (cache->dtype == CODEGEMM_KV_INT8) return launch_decode_of<CODEGEMM_KV_INT8>(p, plan.narrow, plan.groups, s);
+    return launch_decode_of<CODEGEMM_KV_FP8>(p, plan.narrow, plan.groups, s);
 }

@@ -153,12 +153,13 @@ def test_attention_arguments_that_are_refused():
         assert call() == INVALID
 
 
-def test_decode_workspace_grows_with_the_ranges():
-    """Fixed areas, and [item][range][16][D + 2] sums where keys are split: few sequences are, many are not."""
-    fixed = 65536 + (2 << 20)
-    many = cache(num_seqs=600, max_pages=100)
-    assert cg.codegemm_attn_decode_workspace_bytes(many, attn(num_seqs=600, total_q=600, max_kv=3000)) == fixed
-    one = cache(num_seqs=1, max_pages=4000)
-    short, long = (cg.codegemm_attn_decode_workspace_bytes(one, attn(num_seqs=1, total_q=1, max_kv=n)) for n in (100, 100000))
-    assert short == fixed and (long - fixed) % (2 * 16 * 66 * 4) == 0 and long > fixed
-    assert cg.codegemm_attn_decode_workspace_bytes(one, attn(num_seqs=1, total_q=1, max_kv=100000, window=100)) < long
+def test_decode_workspace():
+    """Fixed areas, and [16][D + 2] sums for two pieces of an item for every workgroup that runs at once: 256, 512 where there are more items, fewer
+    where there is less to do."""
+    fixed, each = 65536 + (2 << 20), 2 * 16 * 66 * 4
+    need = lambda seqs, keys, **kw: cg.codegemm_attn_decode_workspace_bytes(cache(num_seqs=seqs, max_pages=4000), attn(num_seqs=seqs, total_q=seqs, max_kv=keys, **kw))  # noqa: E731
+    assert need(600, 3000) == fixed + 512 * each and need(129, 10) == fixed + 258 * each
+    assert need(1, 100000) == need(128, 3000) == fixed + 256 * each
+    assert fixed + 2 * each <= need(1, 100) < need(1, 3000) < fixed + 256 * each
+    assert need(1, 100000, window=100) == need(1, 100)
+    assert need(1, 100000, window=1 << 30) == fixed + 256 * each
