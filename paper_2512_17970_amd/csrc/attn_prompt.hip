@@ -4,7 +4,11 @@
 // BN.  S^T = K Q^T (rows: keys, columns: queries) in 32x32x16 products, so a lane holds all its scores for one query, and what the
 // running maximum and sum of the softmax need from other lanes is one exchange with the other half of the wavefront.  P^T goes from the
 // score tiles into the right operand of O^T += V^T P^T as it lies; V^T comes out of LDS transposed (ds_read_tr16).  Keys and values
-// come into LDS by the memory pipeline (buffer_load .. lds), one tile ahead.
+// come into LDS by the memory pipeline (buffer_load .. lds), one tile ahead.  A wavefront goes on in blocks of 32 keys, three at a time: the
+// scores of one and the product of another's weights with its values on the matrix cores, the weights of the one between by vector
+// instructions; none waits for the others.  (Matrix and vector instructions of one wavefront overlap; those of two disturb each other.)
+// The running maximum follows the scores only where one is over 2^8 times its weight above it (fp16 holds up to 2^16), so that the sums are
+// seldom rescaled.
 //
 // Tiles in which some query of the workgroup does not see some key come first.  A value that a query does not see has weight 0 there,
 // which leaves its sum alone unless the value is a NaN or an infinity; so the sums are looked at once after these tiles, and where they are
@@ -23,8 +27,18 @@ struct PromptParams {
     int window, causal;
     int negate;             // a negative scale: of -q
     float scale;            // its size, times log2(e)
-    int units;              // query tiles, at most
+    int splits;             // workgroups of a tile of queries and head, at most
+    float* part;            // [item][split][NW][DP / 8][64 lanes][4] sums, [NW][64] maximum and weight
+    uint32_t* counters;     // of an item
 };
+
+// Where there are fewer than kPromptItems tiles of queries and heads, as many workgroups as run at once share the keys of each, and the last of them
+// to end adds the parts up, in order.  A part is worth it from kLeastTiles tiles of keys on: 16 queries behind 8000 keys, 64 heads: 90 -> 30 us;
+// 512 of them, 32 heads: 109 -> 69; a prompt of 500, 32 heads, in parts of 3 tiles: 18.4 -> 22.7.
+constexpr int kPromptItems = 256, kLeastTiles = 8;
+constexpr int prompt_groups(int dp) { return dp == 256 ? 256 : 512; }
+
+constexpr int kLdsReads = 0x100, kProducts = 0x8;       // groups of instructions, for the scheduler
 
 typedef __attribute__((address_space(3))) half8_t lds_h8;
 typedef short short4_t __attribute__((ext_vector_type(4)));
@@ -35,8 +49,7 @@ typedef __attribute__((address_space(3))) unsigned char lds_byte;
 __device__ __forceinline__ u32x4_t tile_words(const void* base, uint32_t bytes)
 {
     const uint64_t a = reinterpret_cast<uint64_t>(base);
-    u32x4_t words = {(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)a), (uint32_t)__builtin_amdgcn_readfirstlane((int)((uint32_t)(a >> 32) & 0xffffu)),
-                     (uint32_t)__builtin_amdgcn_readfirstlane((int)bytes), 0x00020000u};
+    u32x4_t words = {(uint32_t)a, (uint32_t)(a >> 32) & 0xffffu, bytes, 0x00020000u};
     asm volatile("s_nop 4" : "+s"(words));
     return words;
 }
@@ -50,49 +63,59 @@ __device__ __forceinline__ void tile_to_lds(uint32_t lds, int voff, u32x4_t word
 template <int DP, int NW>
 struct PromptTile {
     static constexpr int kRows = 32 * NW;                 // queries of a workgroup
-    static constexpr int kKeys = DP == 256 ? 32 : 64;     // BN
+    static constexpr int kKeys = 64;                      // BN
     static constexpr int kUnits = DP / 8;                 // 16-byte units of a row
     static constexpr int kBytes = kKeys * DP * 2;         // of a tile of keys, or of values
     static constexpr int kLoads = kBytes / 1024 / NW;     // a wavefront's requests for one of them
-    static constexpr int kLds = 4 * kBytes + 16;          // two tiles of each, and a flag
-    // Unit u of row `row` lies in place u ^ turn(row): the 8 (16) lanes of a read that the LDS serves together take the same
-    // unit of 8 rows (4 halves of 2 units of 4 rows) and find it in different banks.
-    __host__ __device__ static constexpr int turn_k(int row) { return row & (kUnits - 1); }
-    __host__ __device__ static constexpr int turn_v(int row) { return kUnits == 8 ? row & 6 : 2 * (row & 7); }
+    static constexpr int kLds = 4 * kBytes;               // two tiles of each
+    // Unit u of row `row` lies in place u ^ turn(row): the 16 lanes that the LDS serves together take the same unit of 16 rows of keys, the 32 take
+    // 4 units of 4 rows of values, and find them in different banks (256 bytes of them).
+    __host__ __device__ static constexpr int turn_k(int row) { return kUnits == 8 ? (row >> 1) & 7 : row & 15; }
+    __host__ __device__ static constexpr int turn_v(int row) { return kUnits == 8 ? 4 * ((row >> 1) & 1) : 4 * (row & 3); }
+    static constexpr int kRowsPerLoad = 64 / kUnits;      // rows of a request
+    // requests after which the turns repeat: rows 16 apart for keys, 4 for values
+    static constexpr int kTurnsK = 16 / kRowsPerLoad < kLoads ? 16 / kRowsPerLoad : kLoads;
+    static constexpr int kTurnsV = kRowsPerLoad >= 4 ? 1 : 4 / kRowsPerLoad;
 };
 
 template <int DP, int NW, bool EXACT>
 __global__ void __launch_bounds__(NW * kWave, DP == 256 ? 1 : 2) attn_prompt_kernel(const PromptParams p)
 {
     typedef PromptTile<DP, NW> T;
-    constexpr int BM = T::kRows, BN = T::kKeys, KB = BN / 32, DB = DP / 32;
+    constexpr int BM = T::kRows, BN = T::kKeys, DB = DP / 32;
     extern __shared__ __align__(16) unsigned char smem[];
     const uint32_t lds0 = (uint32_t)reinterpret_cast<uintptr_t>((lds_byte*)smem);
-    volatile uint32_t* flag = reinterpret_cast<volatile uint32_t*>(smem + 4 * T::kBytes);
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int qc = lane & 31, h = lane >> 5;
     const int D = EXACT ? DP : p.D;
 
     // Workgroups that follow each other land on the 8 XCDs in turn: where the heads divide evenly, an XCD keeps to its own, so
-    // that a key head's tiles are read through one L2.  A sequence's last tile, the longest, comes first.
-    int head, unit;
+    // that a key head's tiles are read through one L2.
+    int head, unit, split;
     {
         const int id = blockIdx.x;
         if (p.Hq % 8 == 0) {
-            const int per = p.Hq / 8, at = id / 8;
-            head = id % 8 * per + at % per;
-            unit = at / per;
+            const int per = p.Hq / 8;
+            unit = id / 8;
+            head = id % 8 * per + unit % per;
+            unit /= per;
         } else {
             head = id % p.Hq;
             unit = id / p.Hq;
         }
+        split = unit % p.splits;
+        unit /= p.splits;
     }
-    const int seq = last_at_most(p.seqs, unit, [&](int i) { return p.cu_q[i] / BM + i; });
     auto clamp = [](int x, int lo, int hi) { return x < lo ? lo : x > hi ? hi : x; };
-    const int q0 = clamp(p.cu_q[seq], 0, p.total_q), n = clamp(p.cu_q[seq + 1], q0, p.total_q) - q0;
-    const int32_t* cu_kv = p.cu_kv ? p.cu_kv : p.cu_q;
+    // (scalar loads: what they give decides branches)
+    typedef __attribute__((address_space(4))) const int32_t const_int;
+    const_int *cu_q = (const_int*)(uintptr_t)p.cu_q, *cu_kv = p.cu_kv ? (const_int*)(uintptr_t)p.cu_kv : cu_q;
+    // A sequence's last tile, which sees most keys, comes first: it is under way when the workgroups run out.  (The last tiles of all sequences before
+    // their others were slower: 256 for 248 us with 4 sequences of 2048, more keys at once in an L2.)
+    const int seq = last_at_most(p.seqs, unit, [&](int i) { return p.cu_q[i] / BM + i; }), at = unit - (cu_q[seq] / BM + seq);
+    const int q0 = clamp(cu_q[seq], 0, p.total_q), n = clamp(cu_q[seq + 1], q0, p.total_q) - q0;
     const int k0 = clamp(cu_kv[seq], 0, p.total_kv), n_kv = clamp(cu_kv[seq + 1], k0, p.total_kv) - k0;
-    const int tiles = (n + BM - 1) / BM, at = unit - (p.cu_q[seq] / BM + seq);
+    const int tiles = (n + BM - 1) / BM;
     if (at < 0 || at >= tiles) return;
     const int row0 = (tiles - 1 - at) * BM;                              // first query of the workgroup
     const int back = n_kv - n;                                           // position of query 0
@@ -111,38 +134,49 @@ __global__ void __launch_bounds__(NW * kWave, DP == 256 ? 1 : 2) attn_prompt_ker
     if (t_b > t_hi) t_b = t_hi;
     if (t_b < t_a) t_b = t_a;
     if (t_a > t_hi) t_a = t_b = t_hi;
-    const int masked = (t_a - t_lo) + (t_hi - t_b), all = t_hi - t_lo;
+    const int masked = (t_a - t_lo) + (t_hi - t_b), walk = t_hi - t_lo;
     // i-th tile of the walk: above the whole ones from the last down, below them, the whole ones
-    auto tile_of = [&](int i) {
+    auto tile_of = [&](int i) __attribute__((always_inline)) {
         if (i < t_hi - t_b) return t_hi - 1 - i;
         if (i < masked) return t_lo + (i - (t_hi - t_b));
         return t_b - 1 - (i - masked);
     };
+
+    // the workgroup's part of the walk
+    const int worth = (walk + kLeastTiles - 1) / kLeastTiles, parts = worth < 1 ? 1 : worth < p.splits ? worth : p.splits;
+    if (split >= parts) return;
+    const int begin = walk * split / parts, all = walk * (split + 1) / parts;
 
     const int kv_head = head / (p.Hq / p.Hk);
     const unsigned char* kbase = reinterpret_cast<const unsigned char*>(p.k + (size_t)k0 * p.k_stride + (size_t)kv_head * D);
     const unsigned char* vbase = reinterpret_cast<const unsigned char*>(p.v + (size_t)k0 * p.v_stride + (size_t)kv_head * D);
 
     // a wavefront's part of a tile: rows of kUnits places, each request 1 KB of them
-    int koff[T::kLoads], voff[T::kLoads];
+    int koff[T::kTurnsK], voff[T::kTurnsV];
+    const int load_row = wave * T::kLoads * T::kRowsPerLoad + lane / T::kUnits, load_unit = lane % T::kUnits;
 #pragma unroll
-    for (int i = 0; i < T::kLoads; ++i) {
-        const int place = (wave * T::kLoads + i) * kWave + lane, row = place / T::kUnits, u = place % T::kUnits;
-        const int uk = u ^ T::turn_k(row), uv = u ^ T::turn_v(row);
-        koff[i] = EXACT || 8 * uk < D ? row * p.k_stride * 2 + uk * 16 : 0x7ffffff0;
-        voff[i] = EXACT || 8 * uv < D ? row * p.v_stride * 2 + uv * 16 : 0x7ffffff0;
+    for (int i = 0; i < T::kTurnsK; ++i) {
+        const int row = load_row + i * T::kRowsPerLoad, u = load_unit ^ T::turn_k(row);
+        koff[i] = EXACT || 8 * u < D ? row * p.k_stride * 2 + u * 16 : 0x7f000000;
     }
-    auto request = [&](int tile, int buf) {
-        const int t0 = tile * BN, left = n_kv - t0 < BN ? n_kv - t0 : BN;
-        const u32x4_t kw = tile_words(kbase + (size_t)t0 * p.k_stride * 2, (uint32_t)((left - 1) * p.k_stride * 2 + D * 2));
-        const u32x4_t vw = tile_words(vbase + (size_t)t0 * p.v_stride * 2, (uint32_t)((left - 1) * p.v_stride * 2 + D * 2));
-        const uint32_t at_k = lds0 + (uint32_t)(buf * 2 * T::kBytes + wave * T::kLoads * 1024);
 #pragma unroll
-        for (int i = 0; i < T::kLoads; ++i) tile_to_lds(at_k + i * 1024, koff[i], kw);
+    for (int i = 0; i < T::kTurnsV; ++i) {
+        const int row = load_row + i * T::kRowsPerLoad, u = load_unit ^ T::turn_v(row);
+        voff[i] = EXACT || 8 * u < D ? row * p.v_stride * 2 + u * 16 : 0x7f000000;
+    }
+    // keys in buffers 0 and 1, values in 2 and 3
+    // left: keys from the tile's first on
+    auto request = [&](const unsigned char* tile, int stride, const int* off, int turns, int left, int buf) __attribute__((always_inline)) {
+        const u32x4_t words = tile_words(tile, (uint32_t)(((left < BN ? left : BN) - 1) * stride * 2 + D * 2));
+        const uint32_t to = lds0 + (uint32_t)(buf * T::kBytes + wave * T::kLoads * 1024);
 #pragma unroll
-        for (int i = 0; i < T::kLoads; ++i) tile_to_lds(at_k + T::kBytes + i * 1024, voff[i], vw);
+        for (int i = 0; i < T::kLoads; ++i) tile_to_lds(to + i * 1024, off[i % turns] + i / turns * turns * T::kRowsPerLoad * 2 * stride, words);
     };
+    const int64_t k_step = (int64_t)BN * p.k_stride * 2, v_step = (int64_t)BN * p.v_stride * 2;
+    auto request_k = [&](int tile, int buf) __attribute__((always_inline)) { request(kbase + tile * k_step, p.k_stride, koff, T::kTurnsK, n_kv - tile * BN, buf); };
+    auto request_v = [&](int tile, int buf) __attribute__((always_inline)) { request(vbase + tile * v_step, p.v_stride, voff, T::kTurnsV, n_kv - tile * BN, 2 + buf); };
 
+    if (begin < all) request_k(tile_of(begin), begin & 1);
     // Q^T: column qc, dimensions 16 s + 8 h .. + 7
     half8_t qf[DP / 16];
     const int row = row0 + 32 * wave + qc;
@@ -157,153 +191,224 @@ __global__ void __launch_bounds__(NW * kWave, DP == 256 ? 1 : 2) attn_prompt_ker
         }
     }
     const int pos = back + row;                                          // the lane's query
-    const int wave_first = back + row0 + 32 * wave, wave_last = wave_first + 31;
 
+    // The running maximum m of the scores, as shift = -m scale; l: the sum of the weights as they are rounded.
     float16_t o[DB];
-    float m, l;
-    auto clear = [&]() {
+    float m, l, shift, limit;       // limit: the score from which on the maximum follows
+    auto clear = [&]() __attribute__((always_inline)) {
 #pragma unroll
         for (int b = 0; b < DB; ++b)
 #pragma unroll
             for (int e = 0; e < 16; ++e) o[b][e] = 0.0f;
-        m = -INFINITY;
-        l = 0.0f;
+        m = limit = -INFINITY;
+        l = shift = 0.0f;
     };
     clear();
 
-    // where the lane's operands lie in a tile
-    const uint32_t k_at = lds0 + (uint32_t)(qc * DP * 2);                // + (2 s + h) ^ turn, 32 rows a block
+    // where the lane's operands lie in a tile; the unit's number is exclusive-ored in (rows of 16 bytes times a power of two start at a
+    // multiple of that, in LDS too: a kernel without static LDS has its own from address 0 on)
+    const uint32_t k_at = lds0 + (uint32_t)(qc * DP * 2 + (h ^ T::turn_k(qc)) * 16);                // ^ unit 2 i, + 32 rows a block
     const int vrow = 4 * h + ((lane & 15) >> 2);                         // + 16 ks, + 8
-    const uint32_t v_at = lds0 + (uint32_t)(T::kBytes + vrow * DP * 2 + 8 * (lane & 1));
-    const int vunit = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);         // + 4 b
-    auto v_operand = [&](int buf, int ks, int b) {
-        const uint32_t a = v_at + (uint32_t)(buf * 2 * T::kBytes + ks * 16 * DP * 2) + (uint32_t)(((4 * b + vunit) ^ T::turn_v(vrow)) * 16);
-        const uint32_t c = v_at + (uint32_t)(buf * 2 * T::kBytes + (ks * 16 + 8) * DP * 2) + (uint32_t)(((4 * b + vunit) ^ T::turn_v(vrow + 8)) * 16);
-        const short4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(uintptr_t)a);
-        const short4_t y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(uintptr_t)c);
+    uint32_t v_at[DB];
+#pragma unroll
+    for (int b = 0; b < DB; ++b)
+        v_at[b] = lds0 + (uint32_t)(2 * T::kBytes + vrow * DP * 2 + ((4 * b + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ T::turn_v(vrow)) * 16 + 8 * (lane & 1));
+    // products 16 ks .. of the tile at `tile` bytes from the first buffer of values
+    auto v_operand = [&](uint32_t tile, int ks, int b) __attribute__((always_inline)) {
+        const uint32_t at = v_at[b] + tile + (uint32_t)(ks * 16 * DP * 2);
+        const short4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(uintptr_t)at);
+        const short4_t y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(uintptr_t)(at + 8 * DP * 2));
         return __builtin_bit_cast(half8_t, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
     };
-    auto sees = [&](int key) { return key < n_kv && (!p.causal || key <= pos) && (p.window == 0 || key > pos - p.window); };
+    // the keys that the lane's query sees: from .. to
+    const int see_from = p.window > 0 ? pos - p.window + 1 : 0, see_to = p.causal && pos < n_kv ? pos : n_kv - 1;
+    auto sees = [&](int key) __attribute__((always_inline)) { return (key >= see_from) & (key <= see_to); };
 
-    auto compute = [&](int tile, int buf, bool is_masked, bool by_key) {
-        const int t0 = tile * BN;
-        if (is_masked && ((p.causal && t0 > wave_last) || (p.window > 0 && t0 + BN - 1 <= wave_first - p.window))) return;   // none of the wavefront's
-        float16_t s[KB];
+    // Scores of 32 keys of the tile at `tile` bytes from the first buffer of keys.
+    auto scores = [&](float16_t& to, uint32_t tile, int block) __attribute__((always_inline)) {
+        const uint32_t at = k_at + tile;
 #pragma unroll
-        for (int b = 0; b < KB; ++b) {
+        for (int e = 0; e < 16; ++e) to[e] = 0.0f;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) s[b][e] = 0.0f;
+        for (int i = 0; i < DP / 16; ++i)
+            to = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const lds_h8*)(uintptr_t)((at ^ (uint32_t)(32 * i)) + (uint32_t)(block * 32 * DP * 2)), qf[i], to, 0, 0, 0);
+    };
+    auto hide = [&](float16_t& of, int key0) __attribute__((always_inline)) {
 #pragma unroll
-            for (int i = 0; i < DP / 16; ++i) {
-                const half8_t kf = *(const lds_h8*)(uintptr_t)(k_at + (uint32_t)(buf * 2 * T::kBytes + b * 32 * DP * 2) + (uint32_t)(((2 * i + h) ^ T::turn_k(32 * b + qc)) * 16));
-                s[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qf[i], s[b], 0, 0, 0);
-            }
-        }
-        if (is_masked) {
-#pragma unroll
-            for (int b = 0; b < KB; ++b)
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    if (!sees(t0 + 32 * b + 8 * (e / 4) + 4 * h + e % 4)) s[b][e] = -INFINITY;
-        }
+        for (int e = 0; e < 16; ++e)
+            if (!sees(key0 + 8 * (e / 4) + 4 * h + e % 4)) of[e] = -INFINITY;
+    };
+    // The largest score of the lane's query.
+    auto largest = [&](const float16_t& of) __attribute__((always_inline)) {
         float most = -INFINITY;
 #pragma unroll
-        for (int b = 0; b < KB; ++b)
+        for (int e = 0; e < 16; ++e) most = fmaxf(most, of[e]);
+        const uint32_t w = __builtin_bit_cast(uint32_t, most);
+        const auto x = __builtin_amdgcn_permlane32_swap(w, w, false, false);
+        return fmaxf(__builtin_bit_cast(float, (uint32_t)x[0]), __builtin_bit_cast(float, (uint32_t)x[1]));
+    };
+    // The maximum follows the scores where it has to, and with it the sums and the weights that are still to go into them (their largest are then
+    // under 2^-8 of the new ones').  Without a maximum yet, shift is 0.
+    const float reach = 8.0f / p.scale;
+    auto follow = [&](float most, half8_t (&pending)[2]) __attribute__((always_inline)) {
+        const bool far = most > limit;
+        if (!__any(far)) return;
+        const float keep = far ? __builtin_amdgcn_exp2f((m - most) * p.scale) : 1.0f;
+        m = far ? most : m;
+        limit = far ? most + reach : limit;
+        shift = far ? -most * p.scale : shift;
+        l *= keep;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) most = fmaxf(most, s[b][e]);
-        {
-            const uint32_t w = __builtin_bit_cast(uint32_t, most);
-            const auto x = __builtin_amdgcn_permlane32_swap(w, w, false, false);
-            most = fmaxf(__builtin_bit_cast(float, (uint32_t)x[0]), __builtin_bit_cast(float, (uint32_t)x[1]));
-        }
-        const float m_new = fmaxf(m, most), base = m_new == -INFINITY ? 0.0f : m_new;
-        const float keep = __builtin_amdgcn_exp2f((m - base) * p.scale);
-        m = m_new;
-        const float shift = -base * p.scale;
-        float sum = 0.0f;
-        half8_t pf[BN / 16];
-#pragma unroll
-        for (int b = 0; b < KB; ++b)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][e], p.scale, shift));
-                sum += w;
-                pf[2 * b + e / 8][e % 8] = (_Float16)w;
-            }
-        l = l * keep + sum;
+        for (int i = 0; i < 2; ++i) pending[i] *= (_Float16)keep;
 #pragma unroll
         for (int b = 0; b < DB; ++b)
 #pragma unroll
             for (int e = 0; e < 16; ++e) o[b][e] *= keep;
-        if (!by_key) {
+    };
+    // Weights, and their sum as they are rounded.
+    auto weights = [&](half8_t (&pf)[2], const float16_t& of) __attribute__((always_inline)) {
+        const half2_t ones = {(_Float16)1.0f, (_Float16)1.0f};
+        float sum = 0.0f;
 #pragma unroll
-            for (int ks = 0; ks < BN / 16; ++ks)
-#pragma unroll
-                for (int b = 0; b < DB; ++b) o[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v_operand(buf, ks, b), pf[ks], o[b], 0, 0, 0);
-        } else {
-#pragma unroll
-            for (int ks = 0; ks < BN / 16; ++ks)
-                for (int j = 0; j < 16; ++j) {                           // one key of the 16, in both operands
-                    const bool seen = sees(t0 + 16 * ks + j);
-                    half8_t one = pf[ks];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) one[e] = 8 * (e / 4) + 4 * h + e % 4 == j && seen ? one[e] : (_Float16)0.0f;
-#pragma unroll
-                    for (int b = 0; b < DB; ++b) {
-                        half8_t v = v_operand(buf, ks, b);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) v[e] = 8 * (e / 4) + 4 * h + e % 4 == j ? v[e] : (_Float16)0.0f;
-                        float16_t x;
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) x[e] = 0.0f;
-                        x = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, one, x, 0, 0, 0);
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) o[b][e] += seen ? x[e] : 0.0f;
-                    }
-                }
+        for (int e = 0; e < 16; e += 2) {
+            const half2_t w = {(_Float16)__builtin_amdgcn_exp2f(__builtin_fmaf(of[e], p.scale, shift)), (_Float16)__builtin_amdgcn_exp2f(__builtin_fmaf(of[e + 1], p.scale, shift))};
+            pf[e / 8][e % 8] = w[0];
+            pf[e / 8][e % 8 + 1] = w[1];
+            sum = __builtin_amdgcn_fdot2(w, ones, sum, false);
         }
+        return sum;
     };
 
-    // The tile of step i is in LDS when all wavefronts have waited for their own requests and met; then the next one's requests
-    // go to the buffer that all have finished reading.
-    auto arrive = [&]() {
+    // A tile is in LDS when all wavefronts have waited for their own requests and met; then the next ones' requests go to buffers that all
+    // have finished reading.
+    auto arrive = [&]() __attribute__((always_inline)) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
     };
-    bool by_key = false;
-    if (all > 0) {
-        for (;;) {
-            request(tile_of(0), 0);
-            int i = 0;
-            for (; i < masked; ++i) {
-                arrive();
-                if (i + 1 < all) request(tile_of(i + 1), (i + 1) & 1);
-                compute(tile_of(i), i & 1, true, by_key);
-            }
-            if (!by_key && masked > 0) {
-                float probe = 0.0f;
+    float16_t s0, s1;
+    half8_t p0[2], p1[2];
+    // Before step i: the scores of its 64 keys and the weights of the first 32 of them are there, the maximum has followed the scores; its values
+    // and the next keys are on their way.  (Its keys have been asked for.)
+    auto prime = [&](int i) __attribute__((always_inline)) {
+        arrive();
+        request_v(tile_of(i), i & 1);
+        if (i + 1 < all) request_k(tile_of(i + 1), (i + 1) & 1);
+        const uint32_t k_tile = (uint32_t)((i & 1) * T::kBytes);
+        scores(s0, k_tile, 0);
+        scores(s1, k_tile, 1);
+        if (i < masked) {
+            hide(s0, tile_of(i) * BN);
+            hide(s1, tile_of(i) * BN + 32);
+        }
 #pragma unroll
-                for (int b = 0; b < DB; ++b)
+        for (int e = 0; e < 2; ++e) p0[e] = half8_t{0, 0, 0, 0, 0, 0, 0, 0};
+        follow(fmaxf(largest(s0), largest(s1)), p0);
+        l += weights(p0, s0);
+    };
+    // Three blocks of 32 keys: scores of the next (kind 0: there is none, what is computed is not looked at; 1: all are seen; 2: masked), weights
+    // of the present one, the last one's product with its values.
+    auto half_step = [&](float16_t& next, uint32_t k_tile, int kind, int next_key0, const float16_t& of, half8_t (&pf)[2], bool counts, const half8_t (&last)[2], uint32_t v_tile,
+                         int block) __attribute__((always_inline)) {
+        scores(next, k_tile, block);
+        const float sum = weights(pf, of);
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) probe = __builtin_fmaf(o[b][e], 0.0f, probe);
-                if (tid == 0) *flag = 0;
-                __syncthreads();
-                if (__any(probe != 0.0f) && lane == 0) *flag = 1;        // a NaN: 0 times a NaN or an infinity
-                arrive();
-                if (*flag != 0) {
-                    __syncthreads();
-                    clear();
-                    by_key = true;
-                    continue;
+        for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+            for (int b = 0; b < DB; ++b) o[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v_operand(v_tile, 2 * block + ks, b), last[ks], o[b], 0, 0, 0);
+        l = counts ? l + sum : l;
+        float most = largest(next);
+        // 3 DP / 16 LDS reads for 2 DP / 16 products: the first four before all of them, two more with each of the next, so that none waits for
+        // its own.  (1141 -> 1117 us for 8192 queries of 64 heads.)
+        __builtin_amdgcn_sched_group_barrier(kLdsReads, 4, 0);
+#pragma unroll
+        for (int e = 0; e < (3 * DP / 16 - 4) / 2; ++e) {
+            __builtin_amdgcn_sched_group_barrier(kProducts, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(kLdsReads, 2, 0);
+        }
+        if (kind != 1) {
+            if (kind == 0) return;
+            hide(next, next_key0);
+            most = largest(next);
+        }
+        follow(most, pf);
+    };
+    // The tile of step i, but for its scores and first weights; those of the next.
+    auto step = [&](int i) __attribute__((always_inline)) {
+        arrive();                                                        // keys of i + 1, values of i
+        const int after = tile_of(i + 1);
+        if (i + 2 < all) request_k(tile_of(i + 2), i & 1);
+        if (i + 1 < all) request_v(after, (i + 1) & 1);
+        const uint32_t k_next = (uint32_t)(((i + 1) & 1) * T::kBytes), v_now = (uint32_t)((i & 1) * T::kBytes);
+        const int kind = i + 1 >= all ? 0 : i + 1 < masked ? 2 : 1;
+        half_step(s0, k_next, kind, after * BN, s1, p1, true, p0, v_now, 0);
+        half_step(s1, k_next, kind, after * BN + 32, s0, p0, kind != 0, p1, v_now, 1);
+    };
+    // The masked tiles once more, key by key.
+    auto by_key = [&]() __attribute__((always_inline)) {
+        clear();
+        for (int i = begin; i < masked && i < all; ++i)
+            for (int block = 0; block < 2; ++block) {
+                const int tile = tile_of(i), key0 = tile * BN + 32 * block;
+                if (block == 0) {
+                    arrive();
+                    request_k(tile, 0);
+                    request_v(tile, 0);
+                    arrive();
                 }
-                __syncthreads();
+                scores(s0, 0, block);
+                hide(s0, key0);
+                half8_t pf[2] = {};
+                follow(largest(s0), pf);
+                l += weights(pf, s0);
+#pragma unroll
+                for (int ks = 0; ks < 2; ++ks)
+                    for (int j = 0; j < 16; ++j) {                       // one key of the 16, in both operands
+                        const bool seen = sees(key0 + 16 * ks + j);
+                        half8_t one = pf[ks];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) one[e] = ((8 * (e / 4) + 4 * h + e % 4 == j) & seen) ? one[e] : (_Float16)0.0f;
+#pragma unroll
+                        for (int b = 0; b < DB; ++b) {
+                            half8_t v = v_operand((uint32_t)(block * 32 * DP * 2), ks, b);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) v[e] = 8 * (e / 4) + 4 * h + e % 4 == j ? v[e] : (_Float16)0.0f;
+                            float16_t x;
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) x[e] = 0.0f;
+                            x = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, one, x, 0, 0, 0);
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) o[b][e] += seen ? x[e] : 0.0f;
+                        }
+                    }
             }
-            for (; i < all; ++i) {
-                arrive();
-                if (i + 1 < all) request(tile_of(i + 1), (i + 1) & 1);
-                compute(tile_of(i), i & 1, false, false);
+        arrive();
+    };
+    // Whether a wavefront's sums are not all finite (0 times a NaN or an infinity is a NaN), after step i, which was the last to read keys i + 1.
+    auto spoilt = [&](int i) __attribute__((always_inline)) {
+        float probe = 0.0f;
+#pragma unroll
+        for (int b = 0; b < DB; ++b)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) probe = __builtin_fmaf(o[b][e], 0.0f, probe);
+        volatile uint32_t* flag = reinterpret_cast<volatile uint32_t*>(smem + ((i + 1) & 1) * T::kBytes);
+        arrive();
+        if (tid == 0) *flag = 0;
+        __syncthreads();
+        if (__any(probe != 0.0f) && lane == 0) *flag = 1;
+        __syncthreads();
+        return __builtin_amdgcn_readfirstlane((int)*flag) != 0;
+    };
+    if (begin < all) {
+        prime(begin);
+        for (int i = begin; i < all; ++i) {
+            step(i);
+            if (i < masked && (i + 1 == masked || i + 1 == all) && spoilt(i)) {
+                by_key();
+                if (i + 1 < all) {
+                    request_k(tile_of(i + 1), (i + 1) & 1);
+                    prime(i + 1);
+                }
             }
-            break;
         }
     }
 
@@ -311,6 +416,66 @@ __global__ void __launch_bounds__(NW * kWave, DP == 256 ? 1 : 2) attn_prompt_ker
         const uint32_t w = __builtin_bit_cast(uint32_t, l);
         const auto x = __builtin_amdgcn_permlane32_swap(w, w, false, false);
         l = __builtin_bit_cast(float, (uint32_t)x[0]) + __builtin_bit_cast(float, (uint32_t)x[1]);
+    }
+    if (parts > 1) {
+        // All data that crosses workgroups is moved by device-scope accesses, acknowledged before the ticket is taken; the last workgroup of the
+        // item adds the parts in order and leaves the counter at zero.
+        constexpr size_t kPart = (size_t)BM * DP + NW * kWave * 2;
+        float* first = p.part + ((size_t)unit * p.Hq + head) * p.splits * kPart;
+        float* to = first + split * kPart;
+        auto put = [&](float* where, float a, float b) __attribute__((always_inline)) {
+            const unsigned long long w = (unsigned long long)__builtin_bit_cast(uint32_t, b) << 32 | __builtin_bit_cast(uint32_t, a);
+            __hip_atomic_store(reinterpret_cast<unsigned long long*>(where), w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        };
+        auto get = [&](const float* where) __attribute__((always_inline)) {
+            return __hip_atomic_load(reinterpret_cast<const unsigned long long*>(where), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        };
+        auto low = [](unsigned long long w) { return __builtin_bit_cast(float, (uint32_t)w); };
+        auto high = [](unsigned long long w) { return __builtin_bit_cast(float, (uint32_t)(w >> 32)); };
+        auto place = [&](int b, int e) __attribute__((always_inline)) { return ((size_t)(wave * (DP / 8) + b * 4 + e / 4) * kWave + lane) * 4; };
+        const size_t ml = (size_t)BM * DP + (wave * kWave + lane) * 2;
+        if (row < n) {
+#pragma unroll
+            for (int b = 0; b < DB; ++b)
+#pragma unroll
+                for (int e = 0; e < 16; e += 4) {
+                    put(to + place(b, e), o[b][e], o[b][e + 1]);
+                    put(to + place(b, e) + 2, o[b][e + 2], o[b][e + 3]);
+                }
+            put(to + ml, m, l);
+        }
+        arrive();
+        volatile uint32_t* flag = reinterpret_cast<volatile uint32_t*>(smem);
+        if (tid == 0) {
+            uint32_t* ctr = p.counters + ((size_t)unit * p.Hq + head) * (kCounterAreaWords / kPromptItems);
+            const bool done = __hip_atomic_fetch_add(ctr, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(parts - 1);
+            if (done) __hip_atomic_store(ctr, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            *flag = done ? 1u : 0u;
+        }
+        __syncthreads();
+        if (*flag == 0u) return;
+        clear();
+        if (row < n)
+            for (int k = 0; k < parts; ++k) {
+                const float* from = first + k * kPart;
+                unsigned long long w[DB * 8];
+                const unsigned long long both = get(from + ml);
+#pragma unroll
+                for (int b = 0; b < DB; ++b)
+#pragma unroll
+                    for (int e = 0; e < 16; e += 2) w[b * 8 + e / 2] = get(from + place(b, e) + e % 4);
+                const float m_new = fmaxf(m, low(both)), base = m_new == -INFINITY ? 0.0f : m_new;
+                const float keep = __builtin_amdgcn_exp2f((m - base) * p.scale), by = __builtin_amdgcn_exp2f((low(both) - base) * p.scale);
+                m = m_new;
+                l = l * keep + by * high(both);
+#pragma unroll
+                for (int b = 0; b < DB; ++b)
+#pragma unroll
+                    for (int e = 0; e < 16; e += 2) {
+                        o[b][e] = o[b][e] * keep + by * low(w[b * 8 + e / 2]);
+                        o[b][e + 1] = o[b][e + 1] * keep + by * high(w[b * 8 + e / 2]);
+                    }
+            }
     }
     if (row >= n) return;
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
@@ -329,25 +494,51 @@ int set_max_lds(const void* fn, size_t bytes);
 
 namespace {
 
-template <int DP, int NW, bool EXACT>
-int launch_prompt_one(PromptParams p, const codegemm_attn_desc& d, hipStream_t s)
+struct PromptPlan {
+    int dp, units, splits;
+    size_t bytes;           // of workspace
+};
+
+constexpr int kPromptWaves = 4;
+
+int prompt_plan(const codegemm_attn_desc* desc, PromptPlan* p)
 {
-    typedef PromptTile<DP, NW> T;
-    auto fn = attn_prompt_kernel<DP, NW, EXACT>;
+    const int st = check_attn(desc);
+    if (st) return st;
+    const codegemm_attn_desc& d = *desc;
+    constexpr int rows = 32 * kPromptWaves;
+    p->dp = d.head_dim <= 64 ? 64 : d.head_dim <= 128 ? 128 : 256;
+    // n queries are at most n / rows + 1 tiles
+    p->units = d.total_q / rows + d.num_seqs;
+    const long long items = (long long)p->units * d.q_heads;
+    if (items > 0x7fffffffll) return CODEGEMM_UNSUPPORTED;
+    // Few tiles of queries: their keys over several workgroups, as long as each has some tiles of them (as far as the host knows).
+    p->splits = 1;
+    if (items < kPromptItems) {
+        const int keys = d.window > 0 && d.window < d.max_kv - rows ? d.window + rows : d.max_kv;
+        const int worth = ceil_div(ceil_div(keys, 64), kLeastTiles), room = prompt_groups(p->dp) / (int)items;
+        p->splits = worth < room ? worth : room;
+    }
+    p->bytes = (size_t)kCounterAreaWords * sizeof(uint32_t) + kPairAreaBytes;
+    if (p->splits > 1) p->bytes += (size_t)items * p->splits * (rows * p->dp + kPromptWaves * kWave * 2) * sizeof(float);
+    return CODEGEMM_OK;
+}
+
+template <int DP, bool EXACT>
+int launch_prompt_one(const PromptParams& p, int units, hipStream_t s)
+{
+    typedef PromptTile<DP, kPromptWaves> T;
+    auto fn = attn_prompt_kernel<DP, kPromptWaves, EXACT>;
     const int st = set_max_lds(reinterpret_cast<const void*>(fn), T::kLds);
     if (st) return st;
-    // n queries are at most n / kRows + 1 tiles, the first of a sequence being number cu_q / kRows + i
-    p.units = d.total_q / T::kRows + d.num_seqs;
-    const long long blocks = (long long)p.units * d.q_heads;
-    if (blocks > 0x7fffffffll) return CODEGEMM_UNSUPPORTED;
-    hipLaunchKernelGGL(fn, dim3((unsigned)blocks), dim3(NW * kWave), T::kLds, s, p);
+    hipLaunchKernelGGL(fn, dim3((unsigned)(units * p.Hq * p.splits)), dim3(kPromptWaves * kWave), T::kLds, s, p);
     return hipGetLastError() == hipSuccess ? CODEGEMM_OK : CODEGEMM_LAUNCH_FAILED;
 }
 
-template <int DP, int NW>
-int launch_prompt(const PromptParams& p, const codegemm_attn_desc& d, hipStream_t s)
+template <int DP>
+int launch_prompt(const PromptParams& p, int units, hipStream_t s)
 {
-    return d.head_dim == DP ? launch_prompt_one<DP, NW, true>(p, d, s) : launch_prompt_one<DP, NW, false>(p, d, s);
+    return p.D == DP ? launch_prompt_one<DP, true>(p, units, s) : launch_prompt_one<DP, false>(p, units, s);
 }
 
 }  // namespace
@@ -357,20 +548,21 @@ using namespace cg;
 
 extern "C" size_t codegemm_attn_prompt_workspace_bytes(const codegemm_attn_desc* desc)
 {
-    if (check_attn(desc)) return 0;
-    return (size_t)kCounterAreaWords * sizeof(uint32_t) + kPairAreaBytes;
+    PromptPlan plan;
+    return prompt_plan(desc, &plan) ? 0 : plan.bytes;
 }
 
 extern "C" int codegemm_attn_prompt(const codegemm_attn_desc* desc, const void* q, const void* k, const void* v, const int32_t* cu_q,
                                     const int32_t* cu_kv, void* out, void* workspace, size_t workspace_bytes, void* stream)
 {
-    const int st = check_attn(desc);
+    PromptPlan plan;
+    const int st = prompt_plan(desc, &plan);
     if (st) return st;
     const codegemm_attn_desc& d = *desc;
     if (!q || !out || !cu_q || !workspace || misaligned(q) || misaligned(out) || misaligned(workspace) || misaligned_ints(cu_q)) return CODEGEMM_INVALID_ARG;
     if (d.total_kv > 0 && (!k || !v || misaligned(k) || misaligned(v))) return CODEGEMM_INVALID_ARG;
     if (cu_kv ? misaligned_ints(cu_kv) : d.total_kv != d.total_q) return CODEGEMM_INVALID_ARG;
-    if (workspace_bytes < codegemm_attn_prompt_workspace_bytes(desc)) return CODEGEMM_WORKSPACE_TOO_SMALL;
+    if (workspace_bytes < plan.bytes) return CODEGEMM_WORKSPACE_TOO_SMALL;
     PromptParams p;
     p.q = static_cast<const _Float16*>(q);
     p.k = static_cast<const _Float16*>(k);
@@ -389,8 +581,11 @@ extern "C" int codegemm_attn_prompt(const codegemm_attn_desc* desc, const void* 
     p.negate = d.scale < 0.0f;
     const float size = d.scale < 0.0f ? -d.scale : d.scale;
     p.scale = (float)((size > 1e-30f ? size : 1e-30f) * 1.4426950408889634);      // not 0: 0 times an infinite maximum is no number
+    p.splits = plan.splits;
+    p.counters = static_cast<uint32_t*>(workspace);
+    p.part = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + (size_t)kCounterAreaWords * sizeof(uint32_t) + kPairAreaBytes);
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (d.head_dim <= 64) return launch_prompt<64, 4>(p, d, s);
-    if (d.head_dim <= 128) return launch_prompt<128, 4>(p, d, s);
-    return launch_prompt<256, 4>(p, d, s);
+    if (plan.dp == 64) return launch_prompt<64>(p, plan.units, s);
+    if (plan.dp == 128) return launch_prompt<128>(p, plan.units, s);
+    return launch_prompt<256>(p, plan.units, s);
 }

@@ -281,6 +281,46 @@ def test_prompt_long(new, total):
     assert torch.equal(got, prompt(q, k, v, new, total))
 
 
+@pytest.mark.parametrize("dim", [64, 112, 128, 256])
+@pytest.mark.parametrize("new,total", [([1], [700]), ([3, 0, 140], [900, 5, 1000]), ([17], [4000]), ([130, 20], [130, 2000])])
+def test_prompt_few_queries_behind_long_prefixes(dim, new, total):
+    """The keys of one tile of queries over several workgroups."""
+    q, k, v = packed(sum(new), sum(total), 4, 2, dim)
+    rows = set(range(0, sum(new), 13)) | {0, 2, sum(new) - 1}
+    rows = {r for r in rows if r < sum(new)}
+    for window, causal in ((0, True), (0, False), (500, True)):
+        got = prompt(q, k, v, new, total, window=window, causal=causal)
+        check(got[sorted(rows)], *prompt_exact(q, k, v, new, total, window=window, causal=causal, rows=rows), f"D {dim}, {new} of {total}, window {window}")
+        assert torch.equal(got, prompt(q, k, v, new, total, window=window, causal=causal))
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_prompt_what_a_query_does_not_see_in_any_part_of_the_keys(bad):
+    """As above, where several workgroups share the keys: a bad value near the diagonal, and one at the lower end of the windows."""
+    new, total, dim = [40], [1500], 128
+    q, k, v = packed(40, 1500, 2, 1, dim)
+    for window, at in ((0, 1480), (700, 1480), (700, 780)):
+        vv = v.clone()
+        vv[at, 0, 7] = bad
+        got, (want, bound) = prompt(q, k, vv, new, total, window=window), prompt_exact(q, k, vv, new, total, window=window)
+        seen = [i for i in range(40) if at <= 1460 + i and (not window or at > 1460 + i - window)]
+        assert 0 < len(seen) < 40
+        fine = want.isfinite()
+        assert bool(fine[:, :, :7].all()) and int((~fine).sum()) == 2 * len(seen)
+        check(got[fine], want[fine], bound[fine], f"window {window}, {at}")
+        assert bool((~got[~fine].isfinite()).all())
+
+
+@pytest.mark.parametrize("new", [[300, 1, 0, 129], [128] * 64, [5, 700, 256] + [0] * 61, [1] * 65, [400] + [3] * 70])
+def test_prompt_order_of_sequences(new):
+    """Up to as many sequences as a wavefront has lanes, and more: every tile is taken once."""
+    q, k, v = packed(sum(new), sum(new), 16, 8, 64)
+    rows = set(range(0, sum(new), 61)) | {0, sum(new) - 1}
+    got = prompt(q, k, v, new, new)
+    assert bool(got.isfinite().all())
+    check(got[sorted(rows)], *prompt_exact(q, k, v, new, new, rows=rows), f"{len(new)} sequences")
+
+
 def test_prompt_many_sequences():
     """More sequences than a wavefront has lanes, some of them empty."""
     new = [(7 * i) % 5 for i in range(300)]
