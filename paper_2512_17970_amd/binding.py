@@ -13,8 +13,10 @@ import os
 from typing import Optional
 
 try:
-    from . import _calls                      # csrc/python_calls.cpp: the two calls of a decoding loop without ctypes
+    from . import _calls                      # csrc/python_calls.cpp: the calls of a decoding loop without ctypes
 except ImportError:                           # not built (yet), or for another Python: the ctypes forms below serve
+    _calls = None
+if not hasattr(_calls, "use_attention"):      # of an older source
     _calls = None
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -204,6 +206,7 @@ def load() -> ctypes.CDLL:
     lib.codegemm_status_string.restype = ctypes.c_char_p
     if _calls:
         _calls.use(ctypes.cast(lib.codegemm_gemm, vp).value, ctypes.cast(lib.codegemm_gemm_grouped, vp).value)
+        _calls.use_attention(*(ctypes.cast(f, vp).value for f in (lib.codegemm_kv_append, lib.codegemm_kv_gather, lib.codegemm_attn_decode, lib.codegemm_attn_prompt)))
     _lib = lib
     return lib
 
@@ -349,12 +352,12 @@ def codegemm_kv_scales_bytes(cache: KvCache) -> int:
     return int(load().codegemm_kv_scales_bytes(ctypes.byref(cache)))
 
 
-def codegemm_kv_append(cache: KvCache, desc: AppendDesc, cu_seqlens, q, k, v, q_norm, k_norm, rope, q_out, k_out, stream: int = 0) -> None:
+def _kv_append(cache: KvCache, desc: AppendDesc, cu_seqlens, q, k, v, q_norm, k_norm, rope, q_out, k_out, stream: int = 0) -> None:
     _check(load().codegemm_kv_append(ctypes.byref(cache), ctypes.byref(desc), _ptr(cu_seqlens), _ptr(q), _ptr(k), _ptr(v), _ptr(q_norm),
                                      _ptr(k_norm), _ptr(rope), _ptr(q_out), _ptr(k_out), stream), "codegemm_kv_append")
 
 
-def codegemm_kv_gather(cache: KvCache, rows: int, cu_rows, first, k_out, v_out, stream: int = 0) -> None:
+def _kv_gather(cache: KvCache, rows: int, cu_rows, first, k_out, v_out, stream: int = 0) -> None:
     _check(load().codegemm_kv_gather(ctypes.byref(cache), rows, _ptr(cu_rows), _ptr(first), _ptr(k_out), _ptr(v_out), stream),
            "codegemm_kv_gather")
 
@@ -363,7 +366,7 @@ def codegemm_attn_decode_workspace_bytes(cache: KvCache, desc: AttnDesc) -> int:
     return int(load().codegemm_attn_decode_workspace_bytes(ctypes.byref(cache), ctypes.byref(desc)))
 
 
-def codegemm_attn_decode(cache: KvCache, desc: AttnDesc, q, out, workspace, workspace_bytes: int, stream: int = 0) -> None:
+def _attn_decode(cache: KvCache, desc: AttnDesc, q, out, workspace, workspace_bytes: int, stream: int = 0) -> None:
     _check(load().codegemm_attn_decode(ctypes.byref(cache), ctypes.byref(desc), _ptr(q), _ptr(out), _ptr(workspace), workspace_bytes, stream),
            "codegemm_attn_decode")
 
@@ -372,9 +375,17 @@ def codegemm_attn_prompt_workspace_bytes(desc: AttnDesc) -> int:
     return int(load().codegemm_attn_prompt_workspace_bytes(ctypes.byref(desc)))
 
 
-def codegemm_attn_prompt(desc: AttnDesc, q, k, v, cu_q, cu_kv, out, workspace, workspace_bytes: int, stream: int = 0) -> None:
+def _attn_prompt(desc: AttnDesc, q, k, v, cu_q, cu_kv, out, workspace, workspace_bytes: int, stream: int = 0) -> None:
     _check(load().codegemm_attn_prompt(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(cu_q), _ptr(cu_kv), _ptr(out), _ptr(workspace),
                                        workspace_bytes, stream), "codegemm_attn_prompt")
+
+
+codegemm_kv_append = _calls.codegemm_kv_append if _calls else _kv_append
+codegemm_kv_gather = _calls.codegemm_kv_gather if _calls else _kv_gather
+codegemm_attn_decode = _calls.codegemm_attn_decode if _calls else _attn_decode
+codegemm_attn_prompt = _calls.codegemm_attn_prompt if _calls else _attn_prompt
+if _calls:
+    _calls.prepare_attention(KvCache, AppendDesc, AttnDesc, _kv_append, _kv_gather, _attn_decode, _attn_prompt)
 
 
 def compressed_bytes(B: int, K: int, N: int, v: int, m: int, g: int = -1) -> int:

@@ -1,13 +1,15 @@
-// The two calls that a decoding loop makes, codegemm_gemm and codegemm_gemm_grouped, as functions of a Python extension module.  Through ctypes
-// such a call spends 2.8 us in the interpreter and in argument conversion before it reaches the library, of the 8 us that
-// an eager call of a small layer takes in all (its kernels take 3); here 0.6.  Only the plain form of a call is handled: positional
+// The calls that a decoding loop makes, codegemm_gemm, codegemm_gemm_grouped and those of the cache and of attention, as functions of a Python
+// extension module.  Through ctypes such a call spends 2.8 us in the interpreter and in argument conversion before it reaches the library, of the
+// 8 us that an eager call of a small layer takes in all (its kernels take 3); here 0.6.  Only the plain form of a call is handled: positional
 // arguments, Desc and Plan themselves, tensors (anything with data_ptr()), integer addresses or None.  Every other form, and every
 // argument that the plain form refuses, goes to the ctypes functions, which then do and raise what they always did.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <climits>
 #include <cstddef>
 #include <cstdint>
+#include <cstring>
 #include <initializer_list>
 
 #include "codegemm.h"
@@ -144,6 +146,93 @@ PyObject* gemm_grouped(PyObject*, PyObject* const* a, Py_ssize_t n, PyObject* na
     return result(status, "codegemm_gemm_grouped");
 }
 
+// The calls around the cache.  What each takes in front of its stream: C a cache, A an append's description, T attention's, p an address, i 32 bits,
+// z a size.
+enum { kAppend, kGather, kDecode, kPrompt, kCalls };
+const char* const kTakes[kCalls] = {"CAppppppppp", "Cipppp", "CTpppz", "Tpppppppz"};
+const char* const kNames[kCalls] = {"codegemm_kv_append", "codegemm_kv_gather", "codegemm_attn_decode", "codegemm_attn_prompt"};
+PyTypeObject *cache_type = nullptr, *append_type = nullptr, *attn_type = nullptr;
+PyObject* slow_call[kCalls] = {};
+void* call_at[kCalls] = {};
+
+PyObject* attention_call(int which, PyObject* const* a, Py_ssize_t n, PyObject* names)
+{
+    const char* takes = kTakes[which];
+    const Py_ssize_t count = (Py_ssize_t)strlen(takes);
+    View view[2];
+    void *at[10] = {}, *stream = nullptr;
+    size_t bytes = 0;
+    long rows = 0;
+    Form form = call_at[which] && !names && (n == count || n == count + 1) ? kPlain : kOther;
+    int views = 0, addresses = 0;
+    for (Py_ssize_t k = 0; form == kPlain && k < count; ++k) {
+        PyTypeObject* type = takes[k] == 'C' ? cache_type : takes[k] == 'A' ? append_type : attn_type;
+        const size_t size_of = takes[k] == 'C' ? sizeof(codegemm_kv_cache) : takes[k] == 'A' ? sizeof(codegemm_append_desc) : sizeof(codegemm_attn_desc);
+        if (takes[k] == 'p') form = address(a[k], &at[addresses++]);
+        else if (takes[k] == 'z') form = size(a[k], &bytes) ? kPlain : kOther;
+        else if (takes[k] == 'i') {
+            rows = PyLong_CheckExact(a[k]) ? PyLong_AsLong(a[k]) : LONG_MIN;
+            form = rows >= INT32_MIN && rows <= INT32_MAX && !(rows == -1 && PyErr_Occurred()) ? kPlain : kOther;
+        } else if (Py_TYPE(a[k]) != type || !view[views++].of(a[k], size_of)) form = kOther;
+    }
+    if (form == kRaised) return nullptr;
+    if (form == kOther || (n == count + 1 && !(PyLong_CheckExact(a[count]) && address(a[count], &stream) == kPlain))) return slowly(slow_call[which], a, n, names);
+    void* const call = call_at[which];
+    const void* const first = view[0].b.buf;
+    const void* const second = views > 1 ? view[1].b.buf : nullptr;
+    int status;
+    Py_BEGIN_ALLOW_THREADS
+    switch (which) {
+    case kAppend:
+        status = reinterpret_cast<decltype(&codegemm_kv_append)>(call)(
+            static_cast<const codegemm_kv_cache*>(first), static_cast<const codegemm_append_desc*>(second), static_cast<const int32_t*>(at[0]), at[1], at[2], at[3],
+            at[4], at[5], static_cast<const float*>(at[6]), at[7], at[8], stream);
+        break;
+    case kGather:
+        status = reinterpret_cast<decltype(&codegemm_kv_gather)>(call)(static_cast<const codegemm_kv_cache*>(first), (int32_t)rows, static_cast<const int32_t*>(at[0]),
+                                                                       static_cast<const int32_t*>(at[1]), at[2], at[3], stream);
+        break;
+    case kDecode:
+        status = reinterpret_cast<decltype(&codegemm_attn_decode)>(call)(static_cast<const codegemm_kv_cache*>(first), static_cast<const codegemm_attn_desc*>(second),
+                                                                         at[0], at[1], at[2], bytes, stream);
+        break;
+    default:
+        status = reinterpret_cast<decltype(&codegemm_attn_prompt)>(call)(static_cast<const codegemm_attn_desc*>(first), at[0], at[1], at[2],
+                                                                         static_cast<const int32_t*>(at[3]), static_cast<const int32_t*>(at[4]), at[5], at[6], bytes, stream);
+    }
+    Py_END_ALLOW_THREADS
+    return result(status, kNames[which]);
+}
+PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t n, PyObject* names) { return attention_call(kAppend, a, n, names); }
+PyObject* kv_gather(PyObject*, PyObject* const* a, Py_ssize_t n, PyObject* names) { return attention_call(kGather, a, n, names); }
+PyObject* attn_decode(PyObject*, PyObject* const* a, Py_ssize_t n, PyObject* names) { return attention_call(kDecode, a, n, names); }
+PyObject* attn_prompt(PyObject*, PyObject* const* a, Py_ssize_t n, PyObject* names) { return attention_call(kPrompt, a, n, names); }
+
+// (KvCache, AppendDesc, AttnDesc, the ctypes forms of the four calls)
+PyObject* prepare_attention(PyObject*, PyObject* args)
+{
+    PyObject *c, *d, *t, *slow[kCalls];
+    if (!PyArg_ParseTuple(args, "O!O!O!OOOO", &PyType_Type, &c, &PyType_Type, &d, &PyType_Type, &t, &slow[0], &slow[1], &slow[2], &slow[3])) return nullptr;
+    for (PyObject* o : {c, d, t}) Py_INCREF(o);                         // for the life of the process
+    cache_type = reinterpret_cast<PyTypeObject*>(c);
+    append_type = reinterpret_cast<PyTypeObject*>(d);
+    attn_type = reinterpret_cast<PyTypeObject*>(t);
+    for (int k = 0; k < kCalls; ++k) {
+        Py_INCREF(slow[k]);
+        slow_call[k] = slow[k];
+    }
+    Py_RETURN_NONE;
+}
+
+// (addresses of codegemm_kv_append, codegemm_kv_gather, codegemm_attn_decode, codegemm_attn_prompt)
+PyObject* use_attention(PyObject*, PyObject* args)
+{
+    unsigned long long at[kCalls];
+    if (!PyArg_ParseTuple(args, "KKKK", &at[0], &at[1], &at[2], &at[3])) return nullptr;
+    for (int k = 0; k < kCalls; ++k) call_at[k] = reinterpret_cast<void*>(static_cast<uintptr_t>(at[k]));
+    Py_RETURN_NONE;
+}
+
 // (Desc, Plan, the ctypes forms of the two calls, what raises for a status)
 PyObject* prepare(PyObject*, PyObject* args)
 {
@@ -174,6 +263,16 @@ PyMethodDef methods[] = {
     {"codegemm_gemm_grouped", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(gemm_grouped)), METH_FASTCALL | METH_KEYWORDS,
      "codegemm_gemm_grouped(desc, plan, x, members, workspace, workspace_bytes, stream=0)\n--\n\n"
      "members: sequence of (out_features, packed_codes, codebooks, scales, y), tensors or raw device addresses."},
+    {"codegemm_kv_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(kv_append)), METH_FASTCALL | METH_KEYWORDS,
+     "codegemm_kv_append(cache, desc, cu_seqlens, q, k, v, q_norm, k_norm, rope, q_out, k_out, stream=0)\n--\n\n"},
+    {"codegemm_kv_gather", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(kv_gather)), METH_FASTCALL | METH_KEYWORDS,
+     "codegemm_kv_gather(cache, rows, cu_rows, first, k_out, v_out, stream=0)\n--\n\n"},
+    {"codegemm_attn_decode", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(attn_decode)), METH_FASTCALL | METH_KEYWORDS,
+     "codegemm_attn_decode(cache, desc, q, out, workspace, workspace_bytes, stream=0)\n--\n\n"},
+    {"codegemm_attn_prompt", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(attn_prompt)), METH_FASTCALL | METH_KEYWORDS,
+     "codegemm_attn_prompt(desc, q, k, v, cu_q, cu_kv, out, workspace, workspace_bytes, stream=0)\n--\n\n"},
+    {"prepare_attention", prepare_attention, METH_VARARGS, nullptr},
+    {"use_attention", use_attention, METH_VARARGS, nullptr},
     {"prepare", prepare, METH_VARARGS, nullptr},
     {"use", use, METH_VARARGS, nullptr},
     {nullptr, nullptr, 0, nullptr}};
