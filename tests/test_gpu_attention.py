@@ -321,6 +321,34 @@ def test_prompt_order_of_sequences(new):
     check(got[sorted(rows)], *prompt_exact(q, k, v, new, new, rows=rows), f"{len(new)} sequences")
 
 
+# Thousands of tiles of queries and heads, whose keys no workgroups share; empty sequences stand for them here.
+EMPTY = [0] * 4100
+
+
+@pytest.mark.parametrize("dim", [16, 64, 80, 128, 256])
+@pytest.mark.parametrize("new,total", [([1, 140], [1, 140]), ([129, 2], [300, 70]), ([40], [10]), ([200], [200])])
+def test_prompt_with_thousands_of_tiles(dim, new, total):
+    q, k, v = packed(sum(new), sum(total), 2, 1, dim)
+    for window, causal in ((0, True), (0, False), (50, True)):
+        got = prompt(q, k, v, new + EMPTY, total + EMPTY, window=window, causal=causal)
+        check(got, *prompt_exact(q, k, v, new, total, window=window, causal=causal), f"D {dim}, {new} of {total}, window {window}")
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_prompt_what_a_query_does_not_see_with_thousands_of_tiles(dim, bad):
+    q, k, v = packed(150, 400, 2, 1, dim)
+    for window, at in ((0, 300), (0, 383), (100, 200)):
+        vv = v.clone()
+        vv[at, 0, 5] = bad
+        got, (want, bound) = prompt(q, k, vv, [150] + EMPTY, [400] + EMPTY, window=window), prompt_exact(q, k, vv, [150], [400], window=window)
+        seen = [i for i in range(150) if at <= 250 + i and (not window or at > 250 + i - window)]
+        fine = want.isfinite()
+        assert 0 < len(seen) < 150 and int((~fine).sum()) == 2 * len(seen)
+        check(got[fine], want[fine], bound[fine], f"window {window}, {at}")
+        assert bool((~got[~fine].isfinite()).all())
+
+
 def test_prompt_many_sequences():
     """More sequences than a wavefront has lanes, some of them empty."""
     new = [(7 * i) % 5 for i in range(300)]
