@@ -136,12 +136,16 @@ __device__ void append_queries(const AppendParams& p, int blk)
 {
     const int token = blk / p.token_split, part = blk % p.token_split;
     const int lanes = p.row_lanes, c = threadIdx.x & (lanes - 1), rows = kAppendThreads / lanes;
+    const bool live = c < p.c.D / 16;
+    const Runs r = runs_of(c, p.R, p.interleaved != 0);
+    // the first rows are on their way while the token's position is looked up
+    float x[16];
+    auto load = [&](int h) { load_row(x, p.q + (size_t)token * p.q_stride + (h < p.Hq ? h : 0) * p.c.D, r, live && h < p.Hq); };
+    if (p.Hq > 0) load(part * rows + threadIdx.x / lanes);
     const int seq = p.cu ? last_at_most(p.c.seqs, token, [&](int i) { return p.cu[i]; }) : token;
     int row0;
     const int n = new_tokens(p, seq, &row0);
     const int len = p.c.lens[seq], position = (len < 0 ? 0 : len) - n + token - row0;
-    const bool live = c < p.c.D / 16;
-    const Runs r = runs_of(c, p.R, p.interleaved != 0);
     const float zeros[16] = {0};
     if (position < 0) {                              // no place in the sequence
         for (int h = part * rows + threadIdx.x / lanes; h < p.Hq; h += rows * p.token_split)
@@ -156,8 +160,7 @@ __device__ void append_queries(const AppendParams& p, int blk)
     for (int h0 = part * rows; h0 < p.Hq; h0 += rows * p.token_split) {          // uniform: the norm's exchanges need whole rows
         const int h = h0 + threadIdx.x / lanes;
         const bool mine = live && h < p.Hq;
-        float x[16];
-        load_row(x, p.q + (size_t)token * p.q_stride + (h < p.Hq ? h : 0) * p.c.D, r, mine);
+        if (h0 > part * rows) load(h);
         if (p.q_norm) norm_row(x, p.q_norm, r, mine, lanes, p.c.D, p.eps);
         if (!mine) continue;
         if (r.turns) rotate_row(x, t, p.interleaved != 0);
@@ -200,17 +203,24 @@ __device__ void append_unit(const AppendParams& p, int unit, int head, bool valu
         if (mine && r.turns) rotate_row(x, load_turn(p, pos, c), p.interleaved != 0);
     };
 
+    // Where all tokens of the unit lie in one group of 16 and a pass of the workgroup takes them, they stay in registers from the search for the
+    // largest to their conversion.
+    const bool kept = hi - lo <= rows && lo / kTokenGroup == (hi - 1) / kTokenGroup;
+    float x[16];
     uint32_t* of_block = reinterpret_cast<uint32_t*>(lds);                                 // [G / block <= 16]: the bits of the largest |x|, then of the scale
     auto scale_of_block = [&](int b) { return __builtin_bit_cast(float, of_block[b]); };
     if constexpr (TYPE != CODEGEMM_KV_FP16) {
         // The largest |x| of every block.  As bits: they order as the values do, with infinities and NaN above all numbers.
         const int blocks = G >> cv.block_shift;
         for (int b = tid; b < blocks; b += kAppendThreads) of_block[b] = 0;
+        float* scales = (values ? cv.v_scales : cv.k_scales) + (page < 0 ? 0 : scales_at(cv, page, head) + (slot0 >> cv.block_shift));
+        const int b_lo = (lo - pos0) >> cv.block_shift, first_lo = pos0 + (b_lo << cv.block_shift);
+        const bool earlier = page >= 0 && first_lo < lo;                                   // the block of the first new token holds tokens already
+        const float old = earlier ? scales[b_lo] : 0.0f;
         __syncthreads();
         for (int t0 = lo; t0 < hi; t0 += rows) {
             const int pos = t0 + tid / lanes;
             const bool mine = live && pos < hi;
-            float x[16];
             load(x, pos, mine);
             uint32_t m = 0;
 #pragma unroll
@@ -225,39 +235,40 @@ __device__ void append_unit(const AppendParams& p, int unit, int head, bool valu
             if (mine && c == 0) atomicMax(&of_block[(pos - pos0) >> cv.block_shift], m);
         }
         __syncthreads();
-        float* scales = (values ? cv.v_scales : cv.k_scales) + (page < 0 ? 0 : scales_at(cv, page, head) + (slot0 >> cv.block_shift));
         for (int b = tid; b < blocks; b += kAppendThreads) {
             const int first = pos0 + (b << cv.block_shift), past = first + (1 << cv.block_shift);
             if (page < 0 || past <= lo || first >= hi) continue;
             const uint32_t m = of_block[b];
             float s = __builtin_bit_cast(float, m) / KvType<TYPE>::kMax;
-            if (first < lo) {                                                              // earlier tokens: only in the first block
-                const float old = scales[b];
-                s = old <= s ? s : old;                                                    // a NaN stays
-            }
+            if (earlier && b == b_lo) s = old <= s ? s : old;                              // a NaN stays
             if (m >= 0x7f800000u || !(s <= 3.402823466e38f)) s = __builtin_nanf("");
             of_block[b] = __builtin_bit_cast(uint32_t, s);
+            scales[b] = s;
         }
         __syncthreads();
-        if (page >= 0) {
-            const int b = (lo - pos0) >> cv.block_shift, first = pos0 + (b << cv.block_shift);
-            if (first < lo) {
-                const float old = scales[b], s = scale_of_block(b);
-                if (old < s) {                                                             // the earlier tokens in the larger scale
-                    const float ratio = old > 0.0f ? old / s : 0.0f;
-                    const int count = (lo - first) * D;
-                    for (int i = tid; i < count; i += kAppendThreads) {
-                        const int slot = (first - pos0) + slot0 + i / D, d = i % D;
-                        unsigned char* e = pool + at + (values ? (size_t)(slot / kTokenGroup * D + d) * kTokenGroup + slot % kTokenGroup : (size_t)slot * D + d);
-                        *e = code_of<TYPE>(value_of<TYPE>(*e) * ratio);
-                    }
+        const float now = earlier ? scale_of_block(b_lo) : 0.0f;
+        if (earlier && old < now) {                                                        // the earlier tokens in the larger scale, 16 bytes at a time
+            const float ratio = old > 0.0f ? old / now : 0.0f;
+            const int slot_lo = slot0 + first_lo - pos0, slot_hi = slot0 + lo - pos0;
+            // of keys, 16 dimensions of a token; of values, a dimension's group of 16 tokens, of which the block may have a part
+            const int piece0 = values ? slot_lo / kTokenGroup * D : slot_lo * D / 16, pieces = (values ? ceil_div(slot_hi, kTokenGroup) * D : slot_hi * D / 16) - piece0;
+            for (int i = tid; i < pieces; i += kAppendThreads) {
+                u32x4_t* at16 = reinterpret_cast<u32x4_t*>(pool + at) + piece0 + i;
+                const int t0 = values ? (piece0 + i) / D * kTokenGroup : slot_lo;
+                const u32x4_t in = *at16;
+                alignas(16) uint8_t w[16];
+                __builtin_memcpy(w, &in, 16);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int slot = values ? t0 + e : t0;
+                    const uint8_t c2 = code_of<TYPE>(value_of<TYPE>(w[e]) * ratio);
+                    w[e] = slot >= slot_lo && slot < slot_hi ? c2 : w[e];
                 }
+                u32x4_t out;
+                __builtin_memcpy(&out, w, 16);
+                *at16 = out;
             }
-            __syncthreads();                                                               // the old scale has been read
-            for (int b2 = tid; b2 < blocks; b2 += kAppendThreads) {
-                const int first2 = pos0 + (b2 << cv.block_shift);
-                if (first2 + (1 << cv.block_shift) > lo && first2 < hi) scales[b2] = scale_of_block(b2);
-            }
+            __syncthreads();                                                               // before the new tokens go beside them
         }
     }
 
@@ -268,8 +279,7 @@ __device__ void append_unit(const AppendParams& p, int unit, int head, bool valu
         for (int t0 = glo; t0 < ghi; t0 += rows) {
             const int pos = t0 + tid / lanes;
             const bool mine = live && pos < ghi;
-            float x[16];
-            load(x, pos, mine);
+            if (TYPE == CODEGEMM_KV_FP16 || !kept) load(x, pos, mine);
             if (!mine) continue;
             if (!values && p.k_out) store_row(p.k_out + (size_t)(row0 + pos - start) * p.k_out_stride + head * D, x, r);
             if (page < 0) continue;
