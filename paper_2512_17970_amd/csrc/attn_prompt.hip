@@ -176,20 +176,21 @@ __global__ void __launch_bounds__(NW * kWave, DP == 256 ? 1 : 2) attn_prompt_ker
     auto request_k = [&](int tile, int buf) __attribute__((always_inline)) { request(kbase + tile * k_step, p.k_stride, koff, T::kTurnsK, n_kv - tile * BN, buf); };
     auto request_v = [&](int tile, int buf) __attribute__((always_inline)) { request(vbase + tile * v_step, p.v_stride, voff, T::kTurnsV, n_kv - tile * BN, 2 + buf); };
 
-    if (begin < all) request_k(tile_of(begin), begin & 1);
-    // Q^T: column qc, dimensions 16 s + 8 h .. + 7
-    half8_t qf[DP / 16];
-    const int row = row0 + 32 * wave + qc;
-    {
-        const _Float16* src = p.q + (size_t)(q0 + (row < n ? row : 0)) * p.q_stride + (size_t)head * D;
+    // The first tile, and Q: a wavefront's own rows to the places of its parts of the second one, 16 to a buffer, in the order of keys.  (Loaded row by
+    // row into registers, an instruction would touch 32 lines for 1 KB.)
+    const int row = row0 + 32 * wave + qc, own_rows = n - row0 - 32 * wave < 32 ? n - row0 - 32 * wave : 32;
+    const uint32_t own = lds0 + (uint32_t)(wave * T::kLoads * 1024);
+    if (begin < all) {
+        request_k(tile_of(begin), begin & 1);
+        request_v(tile_of(begin), begin & 1);
+        const u32x4_t words = tile_words(p.q + (size_t)(q0 + row0 + 32 * wave) * p.q_stride + (size_t)head * D, own_rows > 0 ? (uint32_t)((own_rows - 1) * p.q_stride * 2 + D * 2) : 0u);
 #pragma unroll
-        for (int s = 0; s < DP / 16; ++s) {
-            half8_t w = {0, 0, 0, 0, 0, 0, 0, 0};
-            const int d = 16 * s + 8 * h;
-            if (row < n && (EXACT || d < D)) w = *reinterpret_cast<const half8_t*>(src + d);
-            qf[s] = p.negate ? -w : w;
+        for (int i = 0; i < 2 * T::kLoads; ++i) {
+            const int r = i * T::kRowsPerLoad + lane / T::kUnits, u = lane % T::kUnits ^ T::turn_k(r);
+            tile_to_lds(own + (uint32_t)((i < T::kLoads ? 1 - (begin & 1) : 3 - (begin & 1)) * T::kBytes + i % T::kLoads * 1024), EXACT || 8 * u < D ? r * p.q_stride * 2 + u * 16 : 0x7f000000, words);
         }
     }
+    half8_t qf[DP / 16];                                                 // Q^T: column qc, dimensions 16 s + 8 h .. + 7
     const int pos = back + row;                                          // the lane's query
 
     // The running maximum m of the scores, as shift = -m scale; l: the sum of the weights as they are rounded.
@@ -288,10 +289,8 @@ __global__ void __launch_bounds__(NW * kWave, DP == 256 ? 1 : 2) attn_prompt_ker
     float16_t s0, s1;
     half8_t p0[2], p1[2];
     // Before step i: the scores of its 64 keys and the weights of the first 32 of them are there, the maximum has followed the scores; its values
-    // and the next keys are on their way.  (Its keys have been asked for.)
+    // are there or on their way, and so are the next keys.  (prime() finds its keys.)
     auto prime = [&](int i) __attribute__((always_inline)) {
-        arrive();
-        request_v(tile_of(i), i & 1);
         if (i + 1 < all) request_k(tile_of(i + 1), (i + 1) & 1);
         const uint32_t k_tile = (uint32_t)((i & 1) * T::kBytes);
         scores(s0, k_tile, 0);
@@ -399,6 +398,14 @@ __global__ void __launch_bounds__(NW * kWave, DP == 256 ? 1 : 2) attn_prompt_ker
         return __builtin_amdgcn_readfirstlane((int)*flag) != 0;
     };
     if (begin < all) {
+        arrive();
+#pragma unroll
+        for (int i = 0; i < DP / 16; ++i) {
+            qf[i] = *(const lds_h8*)(uintptr_t)(own + (uint32_t)((qc < 16 ? 1 - (begin & 1) : 3 - (begin & 1)) * T::kBytes + qc % 16 * DP * 2 + ((2 * i + h) ^ T::turn_k(qc)) * 16));
+            if (p.negate) qf[i] = -qf[i];
+        }
+#pragma unroll
+        for (int i = 0; i < DP / 16; ++i) asm volatile("" : "+v"(qf[i]));           // read before its places are asked to take keys
         prime(begin);
         for (int i = begin; i < all; ++i) {
             step(i);
@@ -406,6 +413,8 @@ __global__ void __launch_bounds__(NW * kWave, DP == 256 ? 1 : 2) attn_prompt_ker
                 by_key();
                 if (i + 1 < all) {
                     request_k(tile_of(i + 1), (i + 1) & 1);
+                    request_v(tile_of(i + 1), (i + 1) & 1);
+                    arrive();
                     prime(i + 1);
                 }
             }
@@ -477,17 +486,24 @@ __global__ void __launch_bounds__(NW * kWave, DP == 256 ? 1 : 2) attn_prompt_ker
                     }
             }
     }
-    if (row >= n) return;
+    // Out through LDS, row after row: a wavefront stores whole rows, not 16 bytes of each of 32.  With Q's way in: 256 prompts of 128 tokens, 32 heads,
+    // 246 -> 199 us; 8 of 1024, 126 -> 119.
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    _Float16* out = p.out + (size_t)(q0 + row) * p.out_stride + (size_t)head * D;
+    arrive();
+    unsigned char* rows = smem + wave * 32 * DP * 2;
 #pragma unroll
     for (int b = 0; b < DB; ++b)
 #pragma unroll
-        for (int e = 0; e < 16; e += 4) {
-            const int d = 32 * b + 2 * e + 4 * h;
-            if (EXACT || d < D)
-                *reinterpret_cast<half4_t*>(out + d) = half4_t{(_Float16)(o[b][e] * inv), (_Float16)(o[b][e + 1] * inv), (_Float16)(o[b][e + 2] * inv), (_Float16)(o[b][e + 3] * inv)};
-        }
+        for (int e = 0; e < 16; e += 4)
+            *reinterpret_cast<half4_t*>(rows + qc * DP * 2 + ((4 * b + e / 4) ^ T::turn_k(qc)) * 16 + 8 * h) =
+                half4_t{(_Float16)(o[b][e] * inv), (_Float16)(o[b][e + 1] * inv), (_Float16)(o[b][e + 2] * inv), (_Float16)(o[b][e + 3] * inv)};
+    _Float16* out = p.out + (size_t)(q0 + row0 + 32 * wave) * p.out_stride + (size_t)head * D;
+#pragma unroll
+    for (int i = 0; i < 32 / T::kRowsPerLoad; ++i) {
+        const int r = i * T::kRowsPerLoad + lane / T::kUnits, u = lane % T::kUnits;
+        if (r < own_rows && (EXACT || 8 * u < D))
+            __builtin_nontemporal_store(*reinterpret_cast<const half8_t*>(rows + r * DP * 2 + (u ^ T::turn_k(r)) * 16), reinterpret_cast<half8_t*>(out + (size_t)r * p.out_stride + 8 * u));
+    }
 }
 
 int set_max_lds(const void* fn, size_t bytes);
