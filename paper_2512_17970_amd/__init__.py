@@ -14,6 +14,6 @@ from .binding import (  # noqa: F401
     codegemm_pack_codes_host, codegemm_unpack_codes_host,
     codegemm_gemm_static, codegemm_static_workspace_limit,
     GroupMember, codegemm_gemm_grouped, codegemm_grouped_workspace_bytes,
-    KvCache, codegemm_kv_pool_bytes, codegemm_kv_scales_bytes, AppendDesc, codegemm_kv_append, codegemm_kv_gather,
+    KV_FP16, KV_INT8, KV_FP8, KvCache, codegemm_kv_pool_bytes, codegemm_kv_scales_bytes, AppendDesc, codegemm_kv_append, codegemm_kv_gather,
     AttnDesc, codegemm_attn_decode, codegemm_attn_decode_workspace_bytes, codegemm_attn_prompt, codegemm_attn_prompt_workspace_bytes,
 )

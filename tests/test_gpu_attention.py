@@ -88,6 +88,18 @@ def test_decode_split_ranges(dtype, block, dim):
         assert torch.equal(got, decode(c, q, max_kv=hint)), "bits differ from call to call"
 
 
+@pytest.mark.parametrize("dim", [64, 80, 128, 256])
+@pytest.mark.parametrize("dtype,block", [(FP16, 1), (INT8, 4), (FP8, 16)])
+def test_decode_more_items_than_compute_units(dtype, block, dim):
+    """Two workgroups a unit; sequences of many lengths, more of them than a wavefront has lanes, some empty, one long enough to be cut."""
+    lens = [(13 * i) % 40 for i in range(69)] + [1500]
+    c = Cache(lens, heads=4, dim=dim, dtype=dtype, block=block, seed=dim)
+    q = queries(70, 8, dim)
+    got = decode(c, q)
+    check(got, *decode_exact(c, q), f"type {dtype} D {dim}")
+    assert torch.equal(got, decode(c, q))
+
+
 def test_decode_strides_and_scale():
     c = Cache([100, 333], heads=2, dim=64, dtype=FP8, block=16, seed=11)
     wide = queries(2, 8, 64).reshape(2, 512).repeat(1, 2)[:, :640].contiguous()
