@@ -60,6 +60,8 @@ int check_attn(const codegemm_attn_desc* d);                     // status
 CacheView cache_view(const codegemm_kv_cache& c);
 
 inline bool misaligned_ints(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) != 0; }
+// A launch has fewer than 2^32 threads.
+inline bool too_many(long long blocks, int threads) { return blocks * threads > 0xffffffffll; }
 // A row stride of 0 stands for dense rows of `dense` elements.
 inline int row_stride(int stride, int dense) { return stride ? stride : dense; }
 inline bool bad_stride(int stride, int dense) { return stride != 0 && (stride < dense || stride > kMaxStride || (stride & 7) != 0); }

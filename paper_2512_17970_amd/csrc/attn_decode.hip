@@ -22,6 +22,7 @@ constexpr int kDecodeRows = 16;             // query heads of a workgroup
 constexpr int kDecodeUnits = 256;           // compute units
 constexpr int kJoinSteps = 1;               // what joining pieces takes, in steps of a wavefront: an item that is longer by less stays whole
 constexpr int kRoundSteps = 10;             // .. and a second piece for the same workgroup
+constexpr int kMostGroups = 1 << 20;        // workgroups of a launch, which has fewer than 2^32 threads
 constexpr float kLeastLog = -40.0f;         // of a scale's logarithm in the running maximum
 
 struct DecodeParams {
@@ -130,6 +131,7 @@ __device__ __forceinline__ Span span_of(const DecodeParams& p, int n)
     Span s;
     s.len = n < 0 ? 0 : n < held ? n : held;
     s.lo = p.window > 0 && n > p.window ? n - p.window : 0;
+    if (s.lo >= s.len) s.lo = s.len = 0;                             // none at all, or a window behind the table's end
     s.first = s.lo & ~31;
     s.steps = s.len > s.lo ? (s.len - s.first + 31) / 32 : 1;
     return s;
@@ -619,11 +621,12 @@ int decode_plan(const codegemm_kv_cache* cache, const codegemm_attn_desc* d, Dec
     // Up to as many items as there are compute units, a unit works on one: a workgroup each, or for all the pieces of 4 steps that there may be as
     // far as the host knows (any number is right).  More items: two at a time.
     const long long items = (long long)d->num_seqs * d->kv_heads * p->tiles;
-    const int keys = d->window > 0 && d->window < d->max_kv ? d->window : d->max_kv;
+    const int held = cache->max_pages * cache->page_size, longest = d->max_kv < held ? d->max_kv : held;
+    const int keys = d->window > 0 && d->window < longest ? d->window : longest;
     const long long pieces = (ceil_div(keys, 32) + 1ll) / 4 * items + items;
     p->narrow = items > kDecodeUnits;
     const int slots = p->narrow ? 2 * kDecodeUnits : kDecodeUnits;
-    p->groups = (int)(items > slots ? items : pieces < slots ? pieces : slots);
+    p->groups = (int)(items > kMostGroups ? kMostGroups : items > slots ? items : pieces < slots ? pieces : slots);
     // A cut item of x shares has at most 2 x pieces, and there are as many shares as workgroups that run at once.
     p->bytes = (size_t)kCounterAreaWords * sizeof(uint32_t) + kPairAreaBytes + 2 * (size_t)(p->groups < slots ? p->groups : slots) * kDecodeRows * (d->head_dim + 2) * sizeof(float);
     return CODEGEMM_OK;

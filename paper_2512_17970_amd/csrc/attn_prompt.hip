@@ -527,11 +527,12 @@ int prompt_plan(const codegemm_attn_desc* desc, PromptPlan* p)
     // n queries are at most n / rows + 1 tiles
     p->units = d.total_q / rows + d.num_seqs;
     const long long items = (long long)p->units * d.q_heads;
-    if (items > 0x7fffffffll) return CODEGEMM_UNSUPPORTED;
+    if (too_many(items, kPromptWaves * kWave)) return CODEGEMM_UNSUPPORTED;
     // Few tiles of queries: their keys over several workgroups, as long as each has some tiles of them (as far as the host knows).
     p->splits = 1;
     if (items < kPromptItems) {
-        const int keys = d.window > 0 && d.window < d.max_kv - rows ? d.window + rows : d.max_kv;
+        const int held = d.max_kv < d.total_kv ? d.max_kv : d.total_kv > 0 ? d.total_kv : 1;
+        const int keys = d.window > 0 && d.window < held - rows ? d.window + rows : held;
         const int worth = ceil_div(ceil_div(keys, 64), kLeastTiles), room = prompt_groups(p->dp) / (int)items;
         p->splits = worth < room ? worth : room;
     }

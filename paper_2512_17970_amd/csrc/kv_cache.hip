@@ -4,6 +4,7 @@
 namespace cg {
 
 constexpr int kAppendThreads = 128;
+constexpr int kLastEnd = 0x7ffffe00;        // a length past every table, from which counting on by a unit stays within 32 bits
 
 struct AppendParams {
     CacheView c;
@@ -179,7 +180,7 @@ __device__ void append_unit(const AppendParams& p, int unit, int head, bool valu
     if (p.cu) seq = last_at_most(cv.seqs, unit, [&](int i) { return p.cu[i] / G + 2 * i; });
     int row0;
     const int n = new_tokens(p, seq, &row0);
-    const int len = cv.lens[seq], end = len < 0 ? 0 : len, start = end - n;                 // positions of the new tokens: start .. end - 1
+    const int len = cv.lens[seq], end = len < 0 ? 0 : len < kLastEnd ? len : kLastEnd, start = end - n;         // positions of the new tokens: start .. end - 1
     const int from = start < 0 ? 0 : start;
     const int skip = p.cu ? unit - (p.cu[seq] / G + 2 * seq) : 0;
     if (skip < 0 || from >= end || from / G + skip > (end - 1) / G) return;
@@ -519,7 +520,7 @@ extern "C" int codegemm_kv_append(const codegemm_kv_cache* cache, const codegemm
     p.token_split = p.T >= 1024 || p.Hq == 0 ? 1 : ceil_div(p.Hq, rows);
     p.token_blocks = p.Hq > 0 || k_out ? p.T * p.token_split : 0;
     const long long blocks = p.token_blocks + 2ll * p.units * Hk;
-    if (blocks > 0x7fffffffll) return CODEGEMM_UNSUPPORTED;
+    if (too_many(blocks, kAppendThreads)) return CODEGEMM_UNSUPPORTED;
     const dim3 grid((unsigned)blocks), threads(kAppendThreads);
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (cache->dtype == CODEGEMM_KV_FP16) hipLaunchKernelGGL(kv_append_kernel<CODEGEMM_KV_FP16>, grid, threads, 0, s, p);
@@ -545,7 +546,7 @@ extern "C" int codegemm_kv_gather(const codegemm_kv_cache* cache, int32_t rows, 
     p.rows = rows;
     p.row_lanes = row_lanes(cache->head_dim);
     const long long blocks = (long long)(rows / kTokenGroup + 2 * cache->num_seqs) * cache->kv_heads;
-    if (blocks > 0x7fffffffll) return CODEGEMM_UNSUPPORTED;
+    if (too_many(blocks, kAppendThreads)) return CODEGEMM_UNSUPPORTED;
     const dim3 grid((unsigned)blocks, 2), threads(kAppendThreads);
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (cache->dtype == CODEGEMM_KV_FP16) hipLaunchKernelGGL(kv_gather_kernel<CODEGEMM_KV_FP16>, grid, threads, 0, s, p);

@@ -163,3 +163,23 @@ def test_decode_workspace():
     assert fixed + 2 * each <= need(1, 100) < need(1, 3000) < fixed + 256 * each
     assert need(1, 100000, window=100) == need(1, 100)
     assert need(1, 100000, window=1 << 30) == fixed + 256 * each
+
+
+def test_lengths_that_the_host_does_not_know():
+    """Any max_kv: what is split is bounded by the keys that there can be."""
+    most = (1 << 31) - 1
+    for total in (0, 1, 100, 5000, 1 << 24):
+        need = [cg.codegemm_attn_prompt_workspace_bytes(attn(q_heads=8, kv_heads=8, num_seqs=1, total_q=16, total_kv=total, max_kv=n, window=w)) for n in (1 << 24, most) for w in (0, most)]
+        assert len(set(need)) == 1 and 0 < need[0] < 64 << 20
+    single = dict(num_seqs=3, total_q=3)
+    need = [cg.codegemm_attn_decode_workspace_bytes(cache(max_pages=m), attn(max_kv=n, window=w, **single)) for m in (1000, 1 << 25) for n in (32000, most) for w in (0, most)]
+    assert all(x > 0 for x in need) and need[0] == need[1] == need[2] == need[3]
+
+
+def test_launches_that_are_too_large():
+    """2^32 threads and more are refused, not sent."""
+    c = cache(kv_heads=1024, head_dim=16, num_pages=1 << 30)
+    d = attn(q_heads=1024, kv_heads=1024, head_dim=16, total_q=1 << 24, total_kv=1 << 24)
+    assert cg.codegemm_attn_prompt_workspace_bytes(d) == 0 and status(cg.codegemm_attn_prompt, d, *[AT] * 7, 1 << 40) == UNSUPPORTED
+    assert status(cg.codegemm_kv_append, c, cg.AppendDesc.make(1 << 24, 0), AT, None, AT, AT, None, None, None, None, None) == UNSUPPORTED
+    assert status(cg.codegemm_kv_gather, c, 1 << 24, AT, None, AT, AT) == UNSUPPORTED

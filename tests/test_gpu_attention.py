@@ -74,6 +74,25 @@ def test_decode_lengths_beyond_the_table_end_there():
     assert not bool(decode(c, q).any())
 
 
+def test_decode_windows_beyond_the_table():
+    """The last tokens of a length that the page table does not reach have no page: nothing is attended to."""
+    c = Cache([64, 64, 64], heads=1, dim=64, dtype=INT8, block=16, seed=6)
+    q = queries(3, 4, 64)
+    c.lens_dev.copy_(torch.tensor([2 ** 31 - 1, 64 + 31, 64 + 40], dtype=torch.int32))
+    assert not bool(decode(c, q, window=31).any())
+    got, (want, bound) = decode(c, q, window=40), decode_exact(c, q, window=9)       # of the second, positions 55 to 63
+    check(got[1], want[1], bound[1], "a window over the end")
+    assert not bool(got[0].any()) and not bool(got[2].any())
+
+
+@pytest.mark.parametrize("new,total", [([20], [700]), ([5, 70], [300, 70])])
+def test_prompt_hints(new, total):
+    """Any hint of the longest sequence."""
+    q, k, v = packed(sum(new), sum(total), 4, 2, 64)
+    for hint in (1, 2 ** 31 - 1):
+        check(prompt(q, k, v, new, total, max_kv=hint), *prompt_exact(q, k, v, new, total), f"hint {hint}")
+
+
 @pytest.mark.parametrize("dtype,block", [(FP16, 1), (INT8, 4), (INT8, 16), (FP8, 64)])
 @pytest.mark.parametrize("dim", [64, 128, 256])
 def test_decode_split_ranges(dtype, block, dim):
@@ -82,7 +101,7 @@ def test_decode_split_ranges(dtype, block, dim):
     c = Cache(lens, heads=1, dim=dim, page=64, dtype=dtype, block=block, seed=9)
     q = queries(4, 8, dim)
     want = decode_exact(c, q)
-    for hint in (1, 700, 2900, 1 << 20):
+    for hint in (1, 700, 2900, 1 << 20, 2 ** 31 - 1):
         got = decode(c, q, max_kv=hint)
         check(got, *want, f"hint {hint}")
         assert torch.equal(got, decode(c, q, max_kv=hint)), "bits differ from call to call"

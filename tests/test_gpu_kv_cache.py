@@ -171,6 +171,26 @@ def test_append_positions_past_the_table_take_its_last_row():
     append(Cache(grown(past, new), heads=1, dim=64, dtype=FP16, seed=4, filled=past), new, positions=63)
 
 
+@pytest.mark.parametrize("dtype,block", [(FP16, 1), (INT8, 1), (INT8, 16)])
+def test_append_lengths_beyond_the_page_table(dtype, block):
+    """Up to the largest there are: no place in the cache, q_out and k_out turned by the rope table's last row."""
+    c = Cache([64, 64, 64], heads=1, dim=64, dtype=dtype, block=block, seed=4)
+    c.lens_dev.copy_(torch.tensor([2 ** 31 - 1, 2 ** 31 - 20, 64 + 40], dtype=torch.int32))
+    before = [x.clone() for x in (c.k, c.v)]
+    g = torch.Generator().manual_seed(1)
+    q, k, v = (torch.randn(120, 64, generator=g).half().cuda() for _ in range(3))
+    rope = rope_table(64, 64)
+    q_out, k_out = torch.full_like(q, float("nan")), torch.full_like(k, float("nan"))
+    d = cg.AppendDesc.make(120, 1, rotary_dim=64, rope_positions=64)
+    cg.codegemm_kv_append(c.struct(), d, starts([40, 40, 40]), q, k, v, None, None, rope, q_out, k_out, stream())
+    torch.cuda.synchronize()
+    assert c.intact() and all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(before, (c.k, c.v)))
+    at = torch.full((120,), 63, device="cuda")
+    for got, x in ((q_out, q), (k_out, k)):
+        want = rotated(x[:, None], None, at, rope, 64, False, EPS)[:, 0]
+        assert bool(((got.double() - want).abs() <= 2.0 ** -11 * want.abs() + F32 * 2 * want.abs().amax() + 2.0 ** -25).all())
+
+
 def test_append_nan_and_infinity():
     """A block that gets one reads as NaN, alone; it starts afresh with its first token."""
     for dtype in (INT8, FP8):
