@@ -206,17 +206,33 @@ __global__ void __launch_bounds__(NW * kWave, DP == 256 ? 1 : 2) attn_prompt_ker
     };
     clear();
 
-    // where the lane's operands lie in a tile; the unit's number is exclusive-ored in (rows of 16 bytes times a power of two start at a
-    // multiple of that, in LDS too: a kernel without static LDS has its own from address 0 on)
-    const uint32_t k_at = lds0 + (uint32_t)(qc * DP * 2 + (h ^ T::turn_k(qc)) * 16);                // ^ unit 2 i, + 32 rows a block
+    // Where the lane's operands lie in the tile of keys that is read next, and in that of values: kept, and turned to the other buffer once a tile
+    // (1170 -> 1150 us; an address each would be a vector instruction).  The unit's number, and the buffer's, are exclusive-ored in: rows of 16 bytes
+    // times a power of two start at a multiple of that, in LDS too, as a kernel without static LDS has its own from address 0 on.
+    uint32_t k_at[DP / 16], v_at[DB];
+#pragma unroll
+    for (int i = 0; i < DP / 16; ++i) k_at[i] = lds0 + (uint32_t)(qc * DP * 2 + ((2 * i + h) ^ T::turn_k(qc)) * 16);       // + 32 rows a block
     const int vrow = 4 * h + ((lane & 15) >> 2);                         // + 16 ks, + 8
-    uint32_t v_at[DB];
 #pragma unroll
     for (int b = 0; b < DB; ++b)
         v_at[b] = lds0 + (uint32_t)(2 * T::kBytes + vrow * DP * 2 + ((4 * b + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ T::turn_v(vrow)) * 16 + 8 * (lane & 1));
-    // products 16 ks .. of the tile at `tile` bytes from the first buffer of values
-    auto v_operand = [&](uint32_t tile, int ks, int b) __attribute__((always_inline)) {
-        const uint32_t at = v_at[b] + tile + (uint32_t)(ks * 16 * DP * 2);
+    auto other_keys = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < DP / 16; ++i) {
+            k_at[i] ^= (uint32_t)T::kBytes;
+            asm volatile("" : "+v"(k_at[i]));                            // no address of the first buffer and a difference
+        }
+    };
+    auto other_values = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int b = 0; b < DB; ++b) {
+            v_at[b] ^= (uint32_t)T::kBytes;
+            asm volatile("" : "+v"(v_at[b]));
+        }
+    };
+    // of products 16 ks ..
+    auto v_operand = [&](int ks, int b) __attribute__((always_inline)) {
+        const uint32_t at = v_at[b] + (uint32_t)(ks * 16 * DP * 2);
         const short4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(uintptr_t)at);
         const short4_t y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(uintptr_t)(at + 8 * DP * 2));
         return __builtin_bit_cast(half8_t, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
@@ -225,14 +241,13 @@ __global__ void __launch_bounds__(NW * kWave, DP == 256 ? 1 : 2) attn_prompt_ker
     const int see_from = p.window > 0 ? pos - p.window + 1 : 0, see_to = p.causal && pos < n_kv ? pos : n_kv - 1;
     auto sees = [&](int key) __attribute__((always_inline)) { return (key >= see_from) & (key <= see_to); };
 
-    // Scores of 32 keys of the tile at `tile` bytes from the first buffer of keys.
-    auto scores = [&](float16_t& to, uint32_t tile, int block) __attribute__((always_inline)) {
-        const uint32_t at = k_at + tile;
+    // Scores of 32 keys.
+    auto scores = [&](float16_t& to, int block) __attribute__((always_inline)) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) to[e] = 0.0f;
 #pragma unroll
         for (int i = 0; i < DP / 16; ++i)
-            to = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const lds_h8*)(uintptr_t)((at ^ (uint32_t)(32 * i)) + (uint32_t)(block * 32 * DP * 2)), qf[i], to, 0, 0, 0);
+            to = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const lds_h8*)(uintptr_t)(k_at[i] + (uint32_t)(block * 32 * DP * 2)), qf[i], to, 0, 0, 0);
     };
     auto hide = [&](float16_t& of, int key0) __attribute__((always_inline)) {
 #pragma unroll
@@ -292,9 +307,8 @@ __global__ void __launch_bounds__(NW * kWave, DP == 256 ? 1 : 2) attn_prompt_ker
     // are there or on their way, and so are the next keys.  (prime() finds its keys.)
     auto prime = [&](int i) __attribute__((always_inline)) {
         if (i + 1 < all) request_k(tile_of(i + 1), (i + 1) & 1);
-        const uint32_t k_tile = (uint32_t)((i & 1) * T::kBytes);
-        scores(s0, k_tile, 0);
-        scores(s1, k_tile, 1);
+        scores(s0, 0);
+        scores(s1, 1);
         if (i < masked) {
             hide(s0, tile_of(i) * BN);
             hide(s1, tile_of(i) * BN + 32);
@@ -306,14 +320,13 @@ __global__ void __launch_bounds__(NW * kWave, DP == 256 ? 1 : 2) attn_prompt_ker
     };
     // Three blocks of 32 keys: scores of the next (kind 0: there is none, what is computed is not looked at; 1: all are seen; 2: masked), weights
     // of the present one, the last one's product with its values.
-    auto half_step = [&](float16_t& next, uint32_t k_tile, int kind, int next_key0, const float16_t& of, half8_t (&pf)[2], bool counts, const half8_t (&last)[2], uint32_t v_tile,
-                         int block) __attribute__((always_inline)) {
-        scores(next, k_tile, block);
+    auto half_step = [&](float16_t& next, int kind, int next_key0, const float16_t& of, half8_t (&pf)[2], bool counts, const half8_t (&last)[2], int block) __attribute__((always_inline)) {
+        scores(next, block);
         const float sum = weights(pf, of);
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-            for (int b = 0; b < DB; ++b) o[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v_operand(v_tile, 2 * block + ks, b), last[ks], o[b], 0, 0, 0);
+            for (int b = 0; b < DB; ++b) o[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v_operand(2 * block + ks, b), last[ks], o[b], 0, 0, 0);
         l = counts ? l + sum : l;
         float most = largest(next);
         // 3 DP / 16 LDS reads for 2 DP / 16 products: the first four before all of them, two more with each of the next, so that none waits for
@@ -336,15 +349,18 @@ __global__ void __launch_bounds__(NW * kWave, DP == 256 ? 1 : 2) attn_prompt_ker
         arrive();                                                        // keys of i + 1, values of i
         const int after = tile_of(i + 1);
         if (i + 2 < all) request_k(tile_of(i + 2), i & 1);
-        if (i + 1 < all) request_v(after, (i + 1) & 1);
-        const uint32_t k_next = (uint32_t)(((i + 1) & 1) * T::kBytes), v_now = (uint32_t)((i & 1) * T::kBytes);
         const int kind = i + 1 >= all ? 0 : i + 1 < masked ? 2 : 1;
-        half_step(s0, k_next, kind, after * BN, s1, p1, true, p0, v_now, 0);
-        half_step(s1, k_next, kind, after * BN + 32, s0, p0, kind != 0, p1, v_now, 1);
+        half_step(s0, kind, after * BN, s1, p1, true, p0, 0);
+        if (i + 1 < all) request_v(after, (i + 1) & 1);
+        half_step(s1, kind, after * BN + 32, s0, p0, kind != 0, p1, 1);
+        other_keys();                                                    // of i + 2
+        other_values();
     };
-    // The masked tiles once more, key by key.
-    auto by_key = [&]() __attribute__((always_inline)) {
+    // The masked tiles once more, key by key, after step `at`.
+    auto by_key = [&](int at) __attribute__((always_inline)) {
         clear();
+        if (at & 1) other_keys();                                        // both to the first buffer
+        else other_values();
         for (int i = begin; i < masked && i < all; ++i)
             for (int block = 0; block < 2; ++block) {
                 const int tile = tile_of(i), key0 = tile * BN + 32 * block;
@@ -354,7 +370,7 @@ __global__ void __launch_bounds__(NW * kWave, DP == 256 ? 1 : 2) attn_prompt_ker
                     request_v(tile, 0);
                     arrive();
                 }
-                scores(s0, 0, block);
+                scores(s0, block);
                 hide(s0, key0);
                 half8_t pf[2] = {};
                 follow(largest(s0), pf);
@@ -368,7 +384,7 @@ __global__ void __launch_bounds__(NW * kWave, DP == 256 ? 1 : 2) attn_prompt_ker
                         for (int e = 0; e < 8; ++e) one[e] = ((8 * (e / 4) + 4 * h + e % 4 == j) & seen) ? one[e] : (_Float16)0.0f;
 #pragma unroll
                         for (int b = 0; b < DB; ++b) {
-                            half8_t v = v_operand((uint32_t)(block * 32 * DP * 2), ks, b);
+                            half8_t v = v_operand(2 * block + ks, b);
 #pragma unroll
                             for (int e = 0; e < 8; ++e) v[e] = 8 * (e / 4) + 4 * h + e % 4 == j ? v[e] : (_Float16)0.0f;
                             float16_t x;
@@ -381,6 +397,10 @@ __global__ void __launch_bounds__(NW * kWave, DP == 256 ? 1 : 2) attn_prompt_ker
                     }
             }
         arrive();
+        if (!(at & 1)) {                                                 // to those of step at + 1
+            other_keys();
+            other_values();
+        }
     };
     // Whether a wavefront's sums are not all finite (0 times a NaN or an infinity is a NaN), after step i, which was the last to read keys i + 1.
     auto spoilt = [&](int i) __attribute__((always_inline)) {
@@ -406,16 +426,22 @@ __global__ void __launch_bounds__(NW * kWave, DP == 256 ? 1 : 2) attn_prompt_ker
         }
 #pragma unroll
         for (int i = 0; i < DP / 16; ++i) asm volatile("" : "+v"(qf[i]));           // read before its places are asked to take keys
+        if (begin & 1) {
+            other_keys();
+            other_values();
+        }
         prime(begin);
+        other_keys();
         for (int i = begin; i < all; ++i) {
             step(i);
             if (i < masked && (i + 1 == masked || i + 1 == all) && spoilt(i)) {
-                by_key();
+                by_key(i);
                 if (i + 1 < all) {
                     request_k(tile_of(i + 1), (i + 1) & 1);
                     request_v(tile_of(i + 1), (i + 1) & 1);
                     arrive();
                     prime(i + 1);
+                    other_keys();
                 }
             }
         }
