@@ -22,7 +22,7 @@ struct PromptParams {
     _Float16* out;
     const int32_t *cu_q, *cu_kv;
     int seqs, total_q, total_kv;
-    int Hq, Hk, D;
+    int Hq, r, D;           // r: query heads of a key head
     int q_stride, k_stride, v_stride, out_stride;
     int window, causal;
     int negate;             // a negative scale: of -q
@@ -67,7 +67,7 @@ struct PromptTile {
     static constexpr int kUnits = DP / 8;                 // 16-byte units of a row
     static constexpr int kBytes = kKeys * DP * 2;         // of a tile of keys, or of values
     static constexpr int kLoads = kBytes / 1024 / NW;     // a wavefront's requests for one of them
-    static constexpr int kLds = 4 * kBytes;               // two tiles of each
+    static constexpr int kLds = 4 * kBytes + 16;          // two tiles of each, a flag
     // Unit u of row `row` lies in place u ^ turn(row): the 16 lanes that the LDS serves together take the same unit of 16 rows of keys, the 32 take
     // 4 units of 4 rows of values, and find them in different banks (256 bytes of them).
     __host__ __device__ static constexpr int turn_k(int row) { return kUnits == 8 ? (row >> 1) & 7 : row & 15; }
@@ -103,8 +103,11 @@ __global__ void __launch_bounds__(NW * kWave, DP == 256 ? 1 : 2) attn_prompt_ker
             head = id % p.Hq;
             unit = id / p.Hq;
         }
-        split = unit % p.splits;
-        unit /= p.splits;
+        split = 0;
+        if (p.splits > 1) {
+            split = unit % p.splits;
+            unit /= p.splits;
+        }
     }
     auto clamp = [](int x, int lo, int hi) { return x < lo ? lo : x > hi ? hi : x; };
     // (scalar loads: what they give decides branches)
@@ -143,11 +146,16 @@ __global__ void __launch_bounds__(NW * kWave, DP == 256 ? 1 : 2) attn_prompt_ker
     };
 
     // the workgroup's part of the walk
-    const int worth = (walk + kLeastTiles - 1) / kLeastTiles, parts = worth < 1 ? 1 : worth < p.splits ? worth : p.splits;
-    if (split >= parts) return;
-    const int begin = walk * split / parts, all = walk * (split + 1) / parts;
+    int parts = 1, begin = 0, all = walk;
+    if (p.splits > 1) {
+        const int worth = (walk + kLeastTiles - 1) / kLeastTiles;
+        parts = worth < 1 ? 1 : worth < p.splits ? worth : p.splits;
+        if (split >= parts) return;
+        begin = walk * split / parts;
+        all = walk * (split + 1) / parts;
+    }
 
-    const int kv_head = head / (p.Hq / p.Hk);
+    const int kv_head = head / p.r;
     const unsigned char* kbase = reinterpret_cast<const unsigned char*>(p.k + (size_t)k0 * p.k_stride + (size_t)kv_head * D);
     const unsigned char* vbase = reinterpret_cast<const unsigned char*>(p.v + (size_t)k0 * p.v_stride + (size_t)kv_head * D);
 
@@ -250,9 +258,12 @@ __global__ void __launch_bounds__(NW * kWave, DP == 256 ? 1 : 2) attn_prompt_ker
             to = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const lds_h8*)(uintptr_t)(k_at[i] + (uint32_t)(block * 32 * DP * 2)), qf[i], to, 0, 0, 0);
     };
     auto hide = [&](float16_t& of, int key0) __attribute__((always_inline)) {
+        const int from = see_from - key0 - 4 * h, to = see_to - key0 - 4 * h;         // compared with constants
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
-            if (!sees(key0 + 8 * (e / 4) + 4 * h + e % 4)) of[e] = -INFINITY;
+        for (int e = 0; e < 16; ++e) {
+            const int at = 8 * (e / 4) + e % 4;
+            of[e] = ((at < from) | (at > to)) ? -INFINITY : of[e];
+        }
     };
     // The largest score of the lane's query.
     auto largest = [&](const float16_t& of) __attribute__((always_inline)) {
@@ -402,22 +413,20 @@ __global__ void __launch_bounds__(NW * kWave, DP == 256 ? 1 : 2) attn_prompt_ker
             other_values();
         }
     };
-    // Whether a wavefront's sums are not all finite (0 times a NaN or an infinity is a NaN), after step i, which was the last to read keys i + 1.
-    auto spoilt = [&](int i) __attribute__((always_inline)) {
+    // Whether a wavefront's sums are not all finite (0 times a NaN or an infinity is a NaN); once for a workgroup.
+    volatile uint32_t* spoilt_flag = reinterpret_cast<volatile uint32_t*>(smem + 4 * T::kBytes);
+    auto spoilt = [&]() __attribute__((always_inline)) {
         float probe = 0.0f;
 #pragma unroll
         for (int b = 0; b < DB; ++b)
 #pragma unroll
             for (int e = 0; e < 16; ++e) probe = __builtin_fmaf(o[b][e], 0.0f, probe);
-        volatile uint32_t* flag = reinterpret_cast<volatile uint32_t*>(smem + ((i + 1) & 1) * T::kBytes);
-        arrive();
-        if (tid == 0) *flag = 0;
+        if (__any(probe != 0.0f) && lane == 0) *spoilt_flag = 1;
         __syncthreads();
-        if (__any(probe != 0.0f) && lane == 0) *flag = 1;
-        __syncthreads();
-        return __builtin_amdgcn_readfirstlane((int)*flag) != 0;
+        return __builtin_amdgcn_readfirstlane((int)*spoilt_flag) != 0;
     };
     if (begin < all) {
+        if (tid == 0) *spoilt_flag = 0;
         arrive();
 #pragma unroll
         for (int i = 0; i < DP / 16; ++i) {
@@ -434,7 +443,7 @@ __global__ void __launch_bounds__(NW * kWave, DP == 256 ? 1 : 2) attn_prompt_ker
         other_keys();
         for (int i = begin; i < all; ++i) {
             step(i);
-            if (i < masked && (i + 1 == masked || i + 1 == all) && spoilt(i)) {
+            if (i < masked && (i + 1 == masked || i + 1 == all) && spoilt()) {
                 by_key(i);
                 if (i + 1 < all) {
                     request_k(tile_of(i + 1), (i + 1) & 1);
@@ -614,7 +623,7 @@ extern "C" int codegemm_attn_prompt(const codegemm_attn_desc* desc, const void* 
     p.cu_q = cu_q;
     p.cu_kv = cu_kv;
     p.seqs = d.num_seqs; p.total_q = d.total_q; p.total_kv = d.total_kv;
-    p.Hq = d.q_heads; p.Hk = d.kv_heads; p.D = d.head_dim;
+    p.Hq = d.q_heads; p.r = d.q_heads / d.kv_heads; p.D = d.head_dim;
     p.q_stride = row_stride(d.q_stride, d.q_heads * d.head_dim);
     p.k_stride = row_stride(d.k_stride, d.kv_heads * d.head_dim);
     p.v_stride = row_stride(d.v_stride, d.kv_heads * d.head_dim);
