@@ -322,6 +322,8 @@ int codegemm_dequant_gemm(const codegemm_desc *desc, const void *x, const uint8_
  * CODEGEMM_KV_INT8 (-127..127) and CODEGEMM_KV_FP8 (e4m3: 3 bits of mantissa,
  * largest value 448), scale_block consecutive tokens of a page sharing a scale.
  * Places that hold no token of a sequence may hold anything, NaN too.
+ * Arrays of int32 (page_table, kv_lens, cu_*, first) need 4-byte alignment, all else
+ * 16.  Calls with 2^32 threads and more are refused (CODEGEMM_UNSUPPORTED).
  * A page number outside 0..num_pages-1 stands for no page: nothing is written
  * there, and its tokens are not attended to and read as zeros.  The same holds for
  * positions from max_pages * page_size on.
@@ -456,7 +458,8 @@ int codegemm_attn_decode(const codegemm_kv_cache *cache, const codegemm_attn_des
  * p = n_kv - n + j and sees the keys t with t <= p (CODEGEMM_ATTN_CAUSAL; all of
  * them otherwise) and t > p - window (window > 0); out [total_q][q_heads][D] is
  * zero where it sees none.  Keys and values that a query does not see do not reach
- * its result, whatever they hold.  Sums as for codegemm_attn_decode.
+ * its result, whatever they hold.  Sums as for codegemm_attn_decode; where queries
+ * are few, their keys are split over workgroups and joined in a fixed order.
  */
 size_t codegemm_attn_prompt_workspace_bytes(const codegemm_attn_desc *desc);
 int codegemm_attn_prompt(const codegemm_attn_desc *desc, const void *q, const void *k, const void *v,

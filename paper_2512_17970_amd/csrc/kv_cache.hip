@@ -1,4 +1,11 @@
 // The paged cache: new keys and values go in, rotated and normalised on the way, and come out again as contiguous fp16.
+//
+// Append: a workgroup takes the queries of a token, or the keys (or values) of one head for the tokens that share a scale, so that their largest
+// |x| stays within it; a lane has 16 elements of a row, those that turn with each other, so that rotation needs no exchange and the norm a few.
+// Bound by the bytes: 8446 tokens, 64 and 8 heads of 128, 8 bits: 73 us for 346 MB, 4.7 TB/s; by launch and dependent loads where there are few: one
+// token of 32 heads 3.6 us, 32 sequences' 5.7 (lengths, page, old scale, tokens).
+// Gather: a workgroup takes 16 tokens of one head, values by way of LDS, which turns them.  30087 tokens of 8 heads, 8 bits: 30 to 33 us for
+// 185 MB, 5.6 to 6.2 TB/s.
 #include "attn_common.h"
 
 namespace cg {
