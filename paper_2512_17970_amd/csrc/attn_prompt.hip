@@ -34,6 +34,7 @@ struct PromptParams {
     int window, causal;
     int negate;             // a negative scale: of -q
     float scale;            // its size, times log2(e)
+    float reach;            // 8 over that: so far scores may pass the maximum
     int splits;             // workgroups of a tile of queries and head, at most
     float* part;            // [item][split][NW][DP / 8][64 lanes][4] sums, [NW][64] maximum and weight
     uint32_t* counters;     // of an item
@@ -117,14 +118,39 @@ __global__ void __launch_bounds__(NW * kWave, DP == 256 ? 1 : 2) attn_prompt_ker
         }
     }
     auto clamp = [](int x, int lo, int hi) { return x < lo ? lo : x > hi ? hi : x; };
-    // (scalar loads: what they give decides branches)
-    typedef __attribute__((address_space(4))) const int32_t const_int;
-    const_int *cu_q = (const_int*)(uintptr_t)p.cu_q, *cu_kv = p.cu_kv ? (const_int*)(uintptr_t)p.cu_kv : cu_q;
     // A sequence's last tile, which sees most keys, comes first: it is under way when the workgroups run out.  (The last tiles of all sequences before
     // their others were slower: 256 for 248 us with 4 sequences of 2048, more keys at once in an L2.)
-    const int seq = last_at_most(p.seqs, unit, [&](int i) { return p.cu_q[i] / BM + i; }), at = unit - (cu_q[seq] / BM + seq);
-    const int q0 = clamp(cu_q[seq], 0, p.total_q), n = clamp(cu_q[seq + 1], q0, p.total_q) - q0;
-    const int k0 = clamp(cu_kv[seq], 0, p.total_kv), n_kv = clamp(cu_kv[seq + 1], k0, p.total_kv) - k0;
+    // (Up to 64 sequences: one load of all their ends; more: a search, and scalar loads of the one that is found.)
+    int q0, q1, k0, k1, at;
+    if (p.seqs <= kWave) {
+        const int32_t* ends = p.cu_kv ? p.cu_kv : p.cu_q;
+        int from = 0, to = 0, kv_from = 0, kv_to = 0;
+        if (lane < p.seqs) {
+            from = p.cu_q[lane];
+            to = p.cu_q[lane + 1];
+            kv_from = ends[lane];
+            kv_to = ends[lane + 1];
+        }
+        const int first = from / BM + lane;
+        const int below = __popcll(__ballot(lane < p.seqs && first <= unit)), seq = below > 0 ? below - 1 : 0;
+        at = unit - __builtin_amdgcn_readlane(first, seq);
+        q0 = __builtin_amdgcn_readlane(from, seq);
+        q1 = __builtin_amdgcn_readlane(to, seq);
+        k0 = __builtin_amdgcn_readlane(kv_from, seq);
+        k1 = __builtin_amdgcn_readlane(kv_to, seq);
+    } else {
+        typedef __attribute__((address_space(4))) const int32_t const_int;
+        const_int *cu_q = (const_int*)(uintptr_t)p.cu_q, *cu_kv = p.cu_kv ? (const_int*)(uintptr_t)p.cu_kv : cu_q;
+        const int seq = last_at_most(p.seqs, unit, [&](int i) { return p.cu_q[i] / BM + i; });
+        q0 = cu_q[seq];
+        q1 = cu_q[seq + 1];
+        k0 = cu_kv[seq];
+        k1 = cu_kv[seq + 1];
+        at = unit - (q0 / BM + seq);
+    }
+    q0 = clamp(q0, 0, p.total_q);
+    k0 = clamp(k0, 0, p.total_kv);
+    const int n = clamp(q1, q0, p.total_q) - q0, n_kv = clamp(k1, k0, p.total_kv) - k0;
     const int tiles = (n + BM - 1) / BM;
     if (at < 0 || at >= tiles) return;
     const int row0 = (tiles - 1 - at) * BM;                              // first query of the workgroup
@@ -265,11 +291,14 @@ __global__ void __launch_bounds__(NW * kWave, DP == 256 ? 1 : 2) attn_prompt_ker
             to = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const lds_h8*)(uintptr_t)(k_at[i] + (uint32_t)(block * 32 * DP * 2)), qf[i], to, 0, 0, 0);
     };
     auto hide = [&](float16_t& of, int key0) __attribute__((always_inline)) {
-        const int from = see_from - key0 - 4 * h, to = see_to - key0 - 4 * h;         // compared with constants
+        // a bit for each key that is seen, spread over the score by a field insert: no compare, whose result a scalar register would hold
+        const int from = see_from - key0 - 4 * h, to = see_to - key0 - 4 * h;
+        const uint32_t seen = (to < 0 ? 0u : to >= 31 ? ~0u : (2u << to) - 1u) & (from <= 0 ? ~0u : from > 31 ? 0u : ~0u << from);
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-            const int at = 8 * (e / 4) + e % 4;
-            of[e] = ((at < from) | (at > to)) ? -INFINITY : of[e];
+            const uint32_t keep = (uint32_t)__builtin_amdgcn_sbfe((int)seen, 8 * (e / 4) + e % 4, 1);
+            const float x = of[e];                                        // (bit-cast in place, a vector's element would be its first)
+            of[e] = __builtin_bit_cast(float, (keep & __builtin_bit_cast(uint32_t, x)) | (~keep & 0xff800000u));
         }
     };
     // The largest score of the lane's query.
@@ -283,13 +312,12 @@ __global__ void __launch_bounds__(NW * kWave, DP == 256 ? 1 : 2) attn_prompt_ker
     };
     // The maximum follows the scores where it has to, and with it the sums and the weights that are still to go into them (their largest are then
     // under 2^-8 of the new ones').  Without a maximum yet, shift is 0.
-    const float reach = 8.0f / p.scale;
     auto follow = [&](float most, half8_t (&pending)[2]) __attribute__((always_inline)) {
         const bool far = most > limit;
         if (!__any(far)) return;
         const float keep = far ? __builtin_amdgcn_exp2f((m - most) * p.scale) : 1.0f;
         m = far ? most : m;
-        limit = far ? most + reach : limit;
+        limit = far ? most + p.reach : limit;
         shift = far ? -most * p.scale : shift;
         l *= keep;
 #pragma unroll
@@ -640,6 +668,7 @@ extern "C" int codegemm_attn_prompt(const codegemm_attn_desc* desc, const void* 
     p.negate = d.scale < 0.0f;
     const float size = d.scale < 0.0f ? -d.scale : d.scale;
     p.scale = (float)((size > 1e-30f ? size : 1e-30f) * 1.4426950408889634);      // not 0: 0 times an infinite maximum is no number
+    p.reach = 8.0f / p.scale;
     p.splits = plan.splits;
     p.counters = static_cast<uint32_t*>(workspace);
     p.part = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + (size_t)kCounterAreaWords * sizeof(uint32_t) + kPairAreaBytes);
