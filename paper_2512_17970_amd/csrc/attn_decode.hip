@@ -28,6 +28,7 @@ constexpr int kDecodeRows = 16;             // query heads of a workgroup
 constexpr int kDecodeUnits = 256;           // compute units
 constexpr int kJoinSteps = 1;               // what joining pieces takes, in steps of a wavefront: an item that is longer by less stays whole
 constexpr int kRoundSteps = 10;             // .. and a second piece for the same workgroup
+constexpr int kJoined = 8;                  // pieces that are joined at a time
 constexpr int kMostGroups = 1 << 20;        // workgroups of a launch, which has fewer than 2^32 threads
 constexpr float kLeastLog = -40.0f;         // of a scale's logarithm in the running maximum
 
@@ -519,24 +520,17 @@ attn_decode_kernel(const DecodeParams p)
 #pragma unroll
             for (int i = 0; i < T::kBlocks; ++i) store(wave * T::kBlocks + i, mine_o[i], inv);
         } else {
-            // All data that crosses workgroups is moved by device-scope accesses, acknowledged before the ticket is taken; the last workgroup of
-            // the item adds the pieces in order and leaves the counter at zero.
-            const size_t each = (size_t)kDecodeRows * (D + 2);
-            const float* first = p.part + (size_t)kept * each;
-            float* to = p.part + (size_t)(kept + (unsigned)k_part) * each;
-            auto put = [&](float* at, float a, float b) {
-                const unsigned long long w = (unsigned long long)__builtin_bit_cast(uint32_t, b) << 32 | __builtin_bit_cast(uint32_t, a);
-                __hip_atomic_store(reinterpret_cast<unsigned long long*>(at), w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            };
+            // Stores acknowledged before the ticket is taken; the last workgroup of the item adds the pieces in order and leaves the counter at zero.
+            const int each = kDecodeRows * (D + 2) * 4, own = k_part * each, ml_of = kDecodeRows * D * 4 + col * 8;
+            const __amdgpu_buffer_rsrc_t sums = parts_of(p.part + (size_t)kept * kDecodeRows * (D + 2));        // the item's pieces
             if (col < rows) {
 #pragma unroll
                 for (int i = 0; i < T::kBlocks; ++i) {
                     const int b = wave * T::kBlocks + i;
                     if (16 * b >= D) continue;
-                    put(to + (b * kWave + lane) * 4, mine_o[i][0], mine_o[i][1]);
-                    put(to + (b * kWave + lane) * 4 + 2, mine_o[i][2], mine_o[i][3]);
+                    put16(sums, own + (b * kWave + lane) * 16, mine_o[i]);
                 }
-                if (wave == 0 && g == 0) put(to + kDecodeRows * D + 2 * col, top, weight);
+                if (wave == 0 && g == 0) put8(sums, own + ml_of, top, weight);
             }
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             __syncthreads();
@@ -548,39 +542,30 @@ attn_decode_kernel(const DecodeParams p)
             }
             __syncthreads();
             if (*flag != 0u && col < rows) {
-                auto get = [&](const float* from) {
-                    return __hip_atomic_load(reinterpret_cast<const unsigned long long*>(from), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                };
-                auto low = [](unsigned long long w) { return __builtin_bit_cast(float, (uint32_t)w); };
-                auto high = [](unsigned long long w) { return __builtin_bit_cast(float, (uint32_t)(w >> 32)); };
                 for (int b = wave; 16 * b < D; b += NW) {
                     float4_t x = {0, 0, 0, 0};
                     float upto = -INFINITY, all = 0.0f;
-                    for (int k0 = 0; k0 < parts; k0 += 8) {
-                        unsigned long long w[8], ml[8], v[8];
+                    for (int k0 = 0; k0 < parts; k0 += kJoined) {
+                        float4_t w[kJoined];
+                        Pair ml[kJoined];
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) {
-                            const float* from = first + (size_t)(k0 + k < parts ? k0 + k : k0) * each;
-                            ml[k] = get(from + kDecodeRows * D + 2 * col);
-                            w[k] = get(from + (b * kWave + lane) * 4);
-                            v[k] = get(from + (b * kWave + lane) * 4 + 2);
+                        for (int k = 0; k < kJoined; ++k) {
+                            const int from = (k0 + k < parts ? k0 + k : k0) * each;         // (one that is there, with weight 0)
+                            ml[k] = get8(sums, from + ml_of);
+                            w[k] = get16(sums, from + (b * kWave + lane) * 16);
                         }
                         float m_new = upto;
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) m_new = fmaxf(m_new, low(ml[k]));
+                        for (int k = 0; k < kJoined; ++k) m_new = fmaxf(m_new, ml[k].a);
                         const float base = m_new == -INFINITY ? 0.0f : m_new, keep = __builtin_amdgcn_exp2f(upto - base);
                         upto = m_new;
                         all *= keep;
                         x *= keep;
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) {
-                            if (k0 + k >= parts) continue;
-                            const float f = __builtin_amdgcn_exp2f(low(ml[k]) - base);
-                            all += f * high(ml[k]);
-                            x[0] += f * low(w[k]);
-                            x[1] += f * high(w[k]);
-                            x[2] += f * low(v[k]);
-                            x[3] += f * high(v[k]);
+                        for (int k = 0; k < kJoined; ++k) {
+                            const float f = k0 + k < parts ? __builtin_amdgcn_exp2f(ml[k].a - base) : 0.0f;
+                            all += f * ml[k].b;
+                            x += f * w[k];
                         }
                     }
                     store(b, x, all == 0.0f ? 0.0f : 1.0f / all);

@@ -42,8 +42,8 @@ struct PromptParams {
 
 // Where there are fewer than kPromptItems tiles of queries and heads, as many workgroups as run at once share the keys of each, and the last of them
 // to end adds the parts up, in order.  A part is worth it from kLeastTiles tiles of keys on: 16 queries behind 8000 keys, 64 heads: 90 -> 30 us;
-// 512 of them, 32 heads: 109 -> 69; a prompt of 500, 32 heads, in parts of 3 tiles: 18.4 -> 22.7.
-constexpr int kPromptItems = 256, kLeastTiles = 8;
+// 512 of them, 32 heads: 109 -> 60; prompts of 953, 7 heads: 19.3 in parts of 8 tiles, 17.5 of 3.
+constexpr int kPromptItems = 256, kLeastTiles = 3;
 constexpr int prompt_groups(int dp) { return dp == 256 ? 256 : 512; }
 
 constexpr int kLdsReads = 0x100, kProducts = 0x8;       // groups of instructions, for the scheduler
@@ -497,31 +497,17 @@ __global__ void __launch_bounds__(NW * kWave, DP == 256 ? 1 : 2) attn_prompt_ker
         l = __builtin_bit_cast(float, (uint32_t)x[0]) + __builtin_bit_cast(float, (uint32_t)x[1]);
     }
     if (parts > 1) {
-        // All data that crosses workgroups is moved by device-scope accesses, acknowledged before the ticket is taken; the last workgroup of the
-        // item adds the parts in order and leaves the counter at zero.
-        constexpr size_t kPart = (size_t)BM * DP + NW * kWave * 2;
-        float* first = p.part + ((size_t)unit * p.Hq + head) * p.splits * kPart;
-        float* to = first + split * kPart;
-        auto put = [&](float* where, float a, float b) __attribute__((always_inline)) {
-            const unsigned long long w = (unsigned long long)__builtin_bit_cast(uint32_t, b) << 32 | __builtin_bit_cast(uint32_t, a);
-            __hip_atomic_store(reinterpret_cast<unsigned long long*>(where), w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        };
-        auto get = [&](const float* where) __attribute__((always_inline)) {
-            return __hip_atomic_load(reinterpret_cast<const unsigned long long*>(where), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        };
-        auto low = [](unsigned long long w) { return __builtin_bit_cast(float, (uint32_t)w); };
-        auto high = [](unsigned long long w) { return __builtin_bit_cast(float, (uint32_t)(w >> 32)); };
-        auto place = [&](int b, int e) __attribute__((always_inline)) { return ((size_t)(wave * (DP / 8) + b * 4 + e / 4) * kWave + lane) * 4; };
-        const size_t ml = (size_t)BM * DP + (wave * kWave + lane) * 2;
+        // Stores acknowledged before the ticket is taken; the last workgroup of the item adds the parts in order and leaves the counter at zero.
+        constexpr int kPart = (BM * DP + NW * kWave * 2) * 4;
+        const __amdgpu_buffer_rsrc_t sums = parts_of(p.part + ((size_t)unit * p.Hq + head) * p.splits * (kPart / 4));
+        auto place = [&](int b, int e) __attribute__((always_inline)) { return ((wave * (DP / 8) + b * 4 + e / 4) * kWave + lane) * 16; };
+        const int own_part = split * kPart, ml = BM * DP * 4 + (wave * kWave + lane) * 8;
         if (row < n) {
 #pragma unroll
             for (int b = 0; b < DB; ++b)
 #pragma unroll
-                for (int e = 0; e < 16; e += 4) {
-                    put(to + place(b, e), o[b][e], o[b][e + 1]);
-                    put(to + place(b, e) + 2, o[b][e + 2], o[b][e + 3]);
-                }
-            put(to + ml, m, l);
+                for (int e = 0; e < 16; e += 4) put16(sums, own_part + place(b, e), float4_t{o[b][e], o[b][e + 1], o[b][e + 2], o[b][e + 3]});
+            put8(sums, own_part + ml, m, l);
         }
         arrive();
         volatile uint32_t* flag = reinterpret_cast<volatile uint32_t*>(smem);
@@ -536,24 +522,20 @@ __global__ void __launch_bounds__(NW * kWave, DP == 256 ? 1 : 2) attn_prompt_ker
         clear();
         if (row < n)
             for (int k = 0; k < parts; ++k) {
-                const float* from = first + k * kPart;
-                unsigned long long w[DB * 8];
-                const unsigned long long both = get(from + ml);
+                float4_t w[DB * 4];
+                const Pair other = get8(sums, k * kPart + ml);
 #pragma unroll
                 for (int b = 0; b < DB; ++b)
 #pragma unroll
-                    for (int e = 0; e < 16; e += 2) w[b * 8 + e / 2] = get(from + place(b, e) + e % 4);
-                const float m_new = fmaxf(m, low(both)), base = m_new == -INFINITY ? 0.0f : m_new;
-                const float keep = __builtin_amdgcn_exp2f((m - base) * p.scale), by = __builtin_amdgcn_exp2f((low(both) - base) * p.scale);
+                    for (int e = 0; e < 16; e += 4) w[b * 4 + e / 4] = get16(sums, k * kPart + place(b, e));
+                const float m_new = fmaxf(m, other.a), base = m_new == -INFINITY ? 0.0f : m_new;
+                const float keep = __builtin_amdgcn_exp2f((m - base) * p.scale), by = __builtin_amdgcn_exp2f((other.a - base) * p.scale);
                 m = m_new;
-                l = l * keep + by * high(both);
+                l = l * keep + by * other.b;
 #pragma unroll
                 for (int b = 0; b < DB; ++b)
 #pragma unroll
-                    for (int e = 0; e < 16; e += 2) {
-                        o[b][e] = o[b][e] * keep + by * low(w[b * 8 + e / 2]);
-                        o[b][e + 1] = o[b][e + 1] * keep + by * high(w[b * 8 + e / 2]);
-                    }
+                    for (int e = 0; e < 16; ++e) o[b][e] = o[b][e] * keep + by * w[b * 4 + e / 4][e % 4];
             }
     }
     // Out through LDS, row after row: a wavefront stores whole rows, not 16 bytes of each of 32.  With Q's way in: 256 prompts of 128 tokens, 32 heads,
