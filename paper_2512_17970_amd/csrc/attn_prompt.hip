@@ -1,6 +1,8 @@
 // Attention of packed prompts: causal, grouped heads, sequences of different lengths.
 //
-// A workgroup takes 32 NW consecutive queries of one sequence and head, each wavefront 32 of them, and walks over the keys in tiles of
+// A workgroup takes 32 NW rows, each wavefront 32 of them: the query heads of one key head for some consecutive queries of a sequence, head after
+// head for each query (with a tile of queries to each head, 256 prompts of 128 tokens, 32 and 8 heads, took 190 us, so 170: fewer tiles that are part
+// full, fewer keys that only some rows see).  It walks over the keys in tiles of
 // BN.  S^T = K Q^T (rows: keys, columns: queries) in 32x32x16 products, so a lane holds all its scores for one query, and what the
 // running maximum and sum of the softmax need from other lanes is one exchange with the other half of the wavefront.  P^T goes from the
 // score tiles into the right operand of O^T += V^T P^T as it lies; V^T comes out of LDS transposed (ds_read_tr16).  Keys and values
@@ -14,12 +16,12 @@
 // which leaves its sum alone unless the value is a NaN or an infinity; so the sums are looked at once after these tiles, and where they are
 // not all finite, the tiles are run again key by key, each product added only where the query sees the key.
 //
-// Why 32 queries a wavefront and four of those: S^T and O^T of 32 queries and 128 dimensions take 96 registers, Q^T and the weights 48, which
+// Why 32 rows a wavefront and four of those: S^T and O^T of 32 rows and 128 dimensions take 96 registers, Q^T and the weights 48, which
 // leaves room for two wavefronts on a SIMD; two workgroups on a compute unit fill each other's waits (one of 8 wavefronts: 1134 for 1117 us, of 2:
-// 1634), and 128 queries share a tile of keys and values in LDS.
-// Bound by: power, where sequences are long.  8192 causal queries, 64 and 8 heads of 128: 1150 to 1190 us from card to card, 0.92 to 0.96 PFLOP/s (a
+// 1634), and 128 rows share a tile of keys and values in LDS.
+// Bound by: power, where sequences are long.  8192 causal queries, 64 and 8 heads of 128: 1140 to 1190 us from card to card, 0.92 to 0.96 PFLOP/s (a
 // library product of 8192^3 reaches 1.12), the matrix cores busy in 53 % of the cycles at 1.7 GHz; all zeros take 943 us.  Of ragged
-// prompts of 500 to 1100 tokens, 32 and 8 heads: 78 us, 0.60 PFLOP/s; a tile of 128 queries costs some 8 us besides its keys.
+// prompts of 500 to 1100 tokens, 32 and 8 heads: 72 us, 0.65 PFLOP/s; a tile of rows costs some 7 us besides its keys.
 #include "attn_common.h"
 
 namespace cg {
@@ -29,7 +31,8 @@ struct PromptParams {
     _Float16* out;
     const int32_t *cu_q, *cu_kv;
     int seqs, total_q, total_kv;
-    int Hq, r, D;           // r: query heads of a key head
+    int Hk, r, D;           // r: query heads of a key head
+    float by_r;             // 1 / r
     int q_stride, k_stride, v_stride, out_stride;
     int window, causal;
     int negate;             // a negative scale: of -q
@@ -41,10 +44,16 @@ struct PromptParams {
 };
 
 // Where there are fewer than kPromptItems tiles of queries and heads, as many workgroups as run at once share the keys of each, and the last of them
-// to end adds the parts up, in order.  A part is worth it from kLeastTiles tiles of keys on: 16 queries behind 8000 keys, 64 heads: 90 -> 30 us;
-// 512 of them, 32 heads: 109 -> 60; prompts of 953, 7 heads: 19.3 in parts of 8 tiles, 17.5 of 3.
+// to end adds the parts up, in order.  A tile of keys takes about twice what adding a part does, so that sqrt(2 tiles) parts are best, of kLeastTiles
+// at least: 16 queries behind 8000 keys, 64 heads: 90 us in one, 30 in 32 parts, 26 in 16; a prompt of 953, 7 heads: 19.3 in parts
+// of 8 tiles, 17.5 of 3.
 constexpr int kPromptItems = 256, kLeastTiles = 3;
-constexpr int prompt_groups(int dp) { return dp == 256 ? 256 : 512; }
+constexpr int prompt_groups(int dp) { return dp == 256 ? 256 : 512; }        // that run at once
+__host__ __device__ inline int parts_worth(int tiles)
+{
+    const int most = (tiles + kLeastTiles - 1) / kLeastTiles, best = (int)__builtin_sqrtf(2.0f * (float)tiles) + 1;
+    return most < 1 ? 1 : most < best ? most : best;
+}
 
 constexpr int kLdsReads = 0x100, kProducts = 0x8;       // groups of instructions, for the scheduler
 
@@ -97,21 +106,20 @@ __global__ void __launch_bounds__(NW * kWave, DP == 256 ? 1 : 2) attn_prompt_ker
     const int qc = lane & 31, h = lane >> 5;
     const int D = EXACT ? DP : p.D;
 
-    // Workgroups that follow each other land on the 8 XCDs in turn: where the heads divide evenly, an XCD keeps to its own, so
-    // that a key head's tiles are read through one L2.
-    int head, unit, split;
+    // Workgroups that follow each other land on the 8 XCDs in turn: where the key heads divide evenly, an XCD keeps to its own, so that a key
+    // head's tiles are read through one L2.
+    int head, unit, split = 0;                                           // key head
     {
         const int id = blockIdx.x;
-        if (p.Hq % 8 == 0) {
-            const int per = p.Hq / 8;
+        if (p.Hk % 8 == 0) {
+            const int per = p.Hk / 8;
             unit = id / 8;
             head = id % 8 * per + unit % per;
             unit /= per;
         } else {
-            head = id % p.Hq;
-            unit = id / p.Hq;
+            head = id % p.Hk;
+            unit = id / p.Hk;
         }
-        split = 0;
         if (p.splits > 1) {
             split = unit % p.splits;
             unit /= p.splits;
@@ -121,6 +129,7 @@ __global__ void __launch_bounds__(NW * kWave, DP == 256 ? 1 : 2) attn_prompt_ker
     // A sequence's last tile, which sees most keys, comes first: it is under way when the workgroups run out.  (The last tiles of all sequences before
     // their others were slower: 256 for 248 us with 4 sequences of 2048, more keys at once in an L2.)
     // (Up to 64 sequences: one load of all their ends; more: a search, and scalar loads of the one that is found.)
+    auto first_of = [&](int q, int seq) { return (int)((long long)q * p.r / BM) + seq; };        // a sequence's first tile is at most this one
     int q0, q1, k0, k1, at;
     if (p.seqs <= kWave) {
         const int32_t* ends = p.cu_kv ? p.cu_kv : p.cu_q;
@@ -131,7 +140,7 @@ __global__ void __launch_bounds__(NW * kWave, DP == 256 ? 1 : 2) attn_prompt_ker
             kv_from = ends[lane];
             kv_to = ends[lane + 1];
         }
-        const int first = from / BM + lane;
+        const int first = first_of(from, lane);
         const int below = __popcll(__ballot(lane < p.seqs && first <= unit)), seq = below > 0 ? below - 1 : 0;
         at = unit - __builtin_amdgcn_readlane(first, seq);
         q0 = __builtin_amdgcn_readlane(from, seq);
@@ -141,30 +150,33 @@ __global__ void __launch_bounds__(NW * kWave, DP == 256 ? 1 : 2) attn_prompt_ker
     } else {
         typedef __attribute__((address_space(4))) const int32_t const_int;
         const_int *cu_q = (const_int*)(uintptr_t)p.cu_q, *cu_kv = p.cu_kv ? (const_int*)(uintptr_t)p.cu_kv : cu_q;
-        const int seq = last_at_most(p.seqs, unit, [&](int i) { return p.cu_q[i] / BM + i; });
+        const int seq = last_at_most(p.seqs, unit, [&](int i) { return first_of(p.cu_q[i], i); });
         q0 = cu_q[seq];
         q1 = cu_q[seq + 1];
         k0 = cu_kv[seq];
         k1 = cu_kv[seq + 1];
-        at = unit - (q0 / BM + seq);
+        at = unit - first_of(q0, seq);
     }
     q0 = clamp(q0, 0, p.total_q);
     k0 = clamp(k0, 0, p.total_kv);
     const int n = clamp(q1, q0, p.total_q) - q0, n_kv = clamp(k1, k0, p.total_kv) - k0;
-    const int tiles = (n + BM - 1) / BM;
+    const int rows = n * p.r, tiles = (rows + BM - 1) / BM;              // (the host sees to it that this is less than 2^31)
     if (at < 0 || at >= tiles) return;
-    const int row0 = (tiles - 1 - at) * BM;                              // first query of the workgroup
+    const int row0 = (tiles - 1 - at) * BM, rows_here = rows - row0 < BM ? rows - row0 : BM;
+    const int first = row0 / p.r, ahead = row0 - first * p.r;            // its first query, and the rows of that one that are not the workgroup's
+    // The query of a row of the workgroup, counted from the first: a quotient of numbers under 2^11, which the product with the reciprocal is exact for.
+    auto query_of = [&](int r) __attribute__((always_inline)) { return (int)(((float)(ahead + r) + 0.5f) * p.by_r); };
     const int back = n_kv - n;                                           // position of query 0
-    const int last = (row0 + BM < n ? row0 + BM : n) - 1;
+    const int last = first + __builtin_amdgcn_readfirstlane(query_of(rows_here - 1));
 
     // keys that any query of the workgroup sees
     int k_lo = 0, k_hi = n_kv;
     if (p.causal && back + last + 1 < k_hi) k_hi = back + last + 1;
-    if (p.window > 0 && back + row0 - p.window + 1 > 0) k_lo = back + row0 - p.window + 1;
+    if (p.window > 0 && back + first - p.window + 1 > 0) k_lo = back + first - p.window + 1;
     const int t_lo = k_lo / BN, t_hi = k_hi > k_lo ? (k_hi + BN - 1) / BN : t_lo;
     // tiles that all its queries see whole: t_a .. t_b - 1
     int t_a = t_lo, t_b = n_kv / BN;
-    if (p.causal && (back + row0 + 1 < 0 ? 0 : (back + row0 + 1) / BN) < t_b) t_b = back + row0 + 1 < 0 ? 0 : (back + row0 + 1) / BN;
+    if (p.causal && (back + first + 1 < 0 ? 0 : (back + first + 1) / BN) < t_b) t_b = back + first + 1 < 0 ? 0 : (back + first + 1) / BN;
     if (p.window > 0 && back + last - p.window >= 0) t_a = (back + last - p.window) / BN + 1;
     if (t_a < t_lo) t_a = t_lo;
     if (t_b > t_hi) t_b = t_hi;
@@ -181,16 +193,15 @@ __global__ void __launch_bounds__(NW * kWave, DP == 256 ? 1 : 2) attn_prompt_ker
     // the workgroup's part of the walk
     int parts = 1, begin = 0, all = walk;
     if (p.splits > 1) {
-        const int worth = (walk + kLeastTiles - 1) / kLeastTiles;
-        parts = worth < 1 ? 1 : worth < p.splits ? worth : p.splits;
+        const int worth = parts_worth(walk);
+        parts = worth < p.splits ? worth : p.splits;
         if (split >= parts) return;
         begin = walk * split / parts;
         all = walk * (split + 1) / parts;
     }
 
-    const int kv_head = head / p.r;
-    const unsigned char* kbase = reinterpret_cast<const unsigned char*>(p.k + (size_t)k0 * p.k_stride + (size_t)kv_head * D);
-    const unsigned char* vbase = reinterpret_cast<const unsigned char*>(p.v + (size_t)k0 * p.v_stride + (size_t)kv_head * D);
+    const unsigned char* kbase = reinterpret_cast<const unsigned char*>(p.k + (size_t)k0 * p.k_stride + (size_t)head * D);
+    const unsigned char* vbase = reinterpret_cast<const unsigned char*>(p.v + (size_t)k0 * p.v_stride + (size_t)head * D);
 
     // a wavefront's part of a tile: rows of kUnits places, each request 1 KB of them
     int koff[T::kTurnsK], voff[T::kTurnsV];
@@ -219,20 +230,21 @@ __global__ void __launch_bounds__(NW * kWave, DP == 256 ? 1 : 2) attn_prompt_ker
 
     // The first tile, and Q: a wavefront's own rows to the places of its parts of the second one, 16 to a buffer, in the order of keys.  (Loaded row by
     // row into registers, an instruction would touch 32 lines for 1 KB.)
-    const int row = row0 + 32 * wave + qc, own_rows = n - row0 - 32 * wave < 32 ? n - row0 - 32 * wave : 32;
+    const int row = 32 * wave + qc;                                      // the lane's, of the workgroup's
     const uint32_t own = lds0 + (uint32_t)(wave * T::kLoads * 1024);
     if (begin < all) {
         request_k(tile_of(begin), begin & 1);
         request_v(tile_of(begin), begin & 1);
-        const u32x4_t words = tile_words(p.q + (size_t)(q0 + row0 + 32 * wave) * p.q_stride + (size_t)head * D, own_rows > 0 ? (uint32_t)((own_rows - 1) * p.q_stride * 2 + D * 2) : 0u);
+        const u32x4_t words = tile_words(p.q + (size_t)(q0 + first) * p.q_stride + (size_t)head * p.r * D, 0x70000000u);
 #pragma unroll
         for (int i = 0; i < 2 * T::kLoads; ++i) {
-            const int r = i * T::kRowsPerLoad + lane / T::kUnits, u = lane % T::kUnits ^ T::turn_k(r);
-            tile_to_lds(own + (uint32_t)((i < T::kLoads ? 1 - (begin & 1) : 3 - (begin & 1)) * T::kBytes + i % T::kLoads * 1024), EXACT || 8 * u < D ? r * p.q_stride * 2 + u * 16 : 0x7f000000, words);
+            const int in = i * T::kRowsPerLoad + lane / T::kUnits, r = 32 * wave + in, u = lane % T::kUnits ^ T::turn_k(in), q = query_of(r);
+            tile_to_lds(own + (uint32_t)((i < T::kLoads ? 1 - (begin & 1) : 3 - (begin & 1)) * T::kBytes + i % T::kLoads * 1024),
+                        r < rows_here && (EXACT || 8 * u < D) ? (q * p.q_stride + (ahead + r - q * p.r) * D + 8 * u) * 2 : 0x7f000000, words);
         }
     }
     half8_t qf[DP / 16];                                                 // Q^T: column qc, dimensions 16 s + 8 h .. + 7
-    const int pos = back + row;                                          // the lane's query
+    const int pos = back + first + query_of(row);                                          // the lane's query
 
     // The running maximum m of the scores, as shift = -m scale; l: the sum of the weights as they are rounded.
     float16_t o[DB];
@@ -499,10 +511,10 @@ __global__ void __launch_bounds__(NW * kWave, DP == 256 ? 1 : 2) attn_prompt_ker
     if (parts > 1) {
         // Stores acknowledged before the ticket is taken; the last workgroup of the item adds the parts in order and leaves the counter at zero.
         constexpr int kPart = (BM * DP + NW * kWave * 2) * 4;
-        const __amdgpu_buffer_rsrc_t sums = parts_of(p.part + ((size_t)unit * p.Hq + head) * p.splits * (kPart / 4));
+        const __amdgpu_buffer_rsrc_t sums = parts_of(p.part + ((size_t)unit * p.Hk + head) * p.splits * (kPart / 4));
         auto place = [&](int b, int e) __attribute__((always_inline)) { return ((wave * (DP / 8) + b * 4 + e / 4) * kWave + lane) * 16; };
         const int own_part = split * kPart, ml = BM * DP * 4 + (wave * kWave + lane) * 8;
-        if (row < n) {
+        if (row < rows_here) {
 #pragma unroll
             for (int b = 0; b < DB; ++b)
 #pragma unroll
@@ -512,7 +524,7 @@ __global__ void __launch_bounds__(NW * kWave, DP == 256 ? 1 : 2) attn_prompt_ker
         arrive();
         volatile uint32_t* flag = reinterpret_cast<volatile uint32_t*>(smem);
         if (tid == 0) {
-            uint32_t* ctr = p.counters + ((size_t)unit * p.Hq + head) * (kCounterAreaWords / kPromptItems);
+            uint32_t* ctr = p.counters + ((size_t)unit * p.Hk + head) * (kCounterAreaWords / kPromptItems);
             const bool done = __hip_atomic_fetch_add(ctr, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(parts - 1);
             if (done) __hip_atomic_store(ctr, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             *flag = done ? 1u : 0u;
@@ -520,7 +532,7 @@ __global__ void __launch_bounds__(NW * kWave, DP == 256 ? 1 : 2) attn_prompt_ker
         __syncthreads();
         if (*flag == 0u) return;
         clear();
-        if (row < n)
+        if (row < rows_here)
             for (int k = 0; k < parts; ++k) {
                 float4_t w[DB * 4];
                 const Pair other = get8(sums, k * kPart + ml);
@@ -539,22 +551,23 @@ __global__ void __launch_bounds__(NW * kWave, DP == 256 ? 1 : 2) attn_prompt_ker
             }
     }
     // Out through LDS, row after row: a wavefront stores whole rows, not 16 bytes of each of 32.  With Q's way in: 256 prompts of 128 tokens, 32 heads,
-    // 246 -> 199 us; 8 of 1024, 126 -> 119.
+    // from 246 to 199 us; 8 of 1024, from 126 to 119.
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
     arrive();
-    unsigned char* rows = smem + wave * 32 * DP * 2;
+    unsigned char* mine = smem + wave * 32 * DP * 2;
 #pragma unroll
     for (int b = 0; b < DB; ++b)
 #pragma unroll
         for (int e = 0; e < 16; e += 4)
-            *reinterpret_cast<half4_t*>(rows + qc * DP * 2 + ((4 * b + e / 4) ^ T::turn_k(qc)) * 16 + 8 * h) =
+            *reinterpret_cast<half4_t*>(mine + qc * DP * 2 + ((4 * b + e / 4) ^ T::turn_k(qc)) * 16 + 8 * h) =
                 half4_t{(_Float16)(o[b][e] * inv), (_Float16)(o[b][e + 1] * inv), (_Float16)(o[b][e + 2] * inv), (_Float16)(o[b][e + 3] * inv)};
-    _Float16* out = p.out + (size_t)(q0 + row0 + 32 * wave) * p.out_stride + (size_t)head * D;
+    _Float16* out = p.out + (size_t)(q0 + first) * p.out_stride + (size_t)head * p.r * D;
 #pragma unroll
     for (int i = 0; i < 32 / T::kRowsPerLoad; ++i) {
-        const int r = i * T::kRowsPerLoad + lane / T::kUnits, u = lane % T::kUnits;
-        if (r < own_rows && (EXACT || 8 * u < D))
-            __builtin_nontemporal_store(*reinterpret_cast<const half8_t*>(rows + r * DP * 2 + (u ^ T::turn_k(r)) * 16), reinterpret_cast<half8_t*>(out + (size_t)r * p.out_stride + 8 * u));
+        const int in = i * T::kRowsPerLoad + lane / T::kUnits, r = 32 * wave + in, u = lane % T::kUnits, q = query_of(r);
+        if (r < rows_here && (EXACT || 8 * u < D))
+            __builtin_nontemporal_store(*reinterpret_cast<const half8_t*>(mine + in * DP * 2 + (u ^ T::turn_k(in)) * 16),
+                                        reinterpret_cast<half8_t*>(out + (size_t)q * p.out_stride + (ahead + r - q * p.r) * D + 8 * u));
     }
 }
 
@@ -576,16 +589,16 @@ int prompt_plan(const codegemm_attn_desc* desc, PromptPlan* p)
     const codegemm_attn_desc& d = *desc;
     constexpr int rows = 32 * kPromptWaves;
     p->dp = d.head_dim <= 64 ? 64 : d.head_dim <= 128 ? 128 : 256;
-    // n queries are at most n / rows + 1 tiles
-    p->units = d.total_q / rows + d.num_seqs;
-    const long long items = (long long)p->units * d.q_heads;
+    // n rows are at most n / rows + 1 tiles
+    const long long units = (long long)d.total_q * (d.q_heads / d.kv_heads) / rows + d.num_seqs, items = units * d.kv_heads;
     if (too_many(items, kPromptWaves * kWave)) return CODEGEMM_UNSUPPORTED;
+    p->units = (int)units;
     // Few tiles of queries: their keys over several workgroups, as long as each has some tiles of them (as far as the host knows).
     p->splits = 1;
     if (items < kPromptItems) {
         const int held = d.max_kv < d.total_kv ? d.max_kv : d.total_kv > 0 ? d.total_kv : 1;
         const int keys = d.window > 0 && d.window < held - rows ? d.window + rows : held;
-        const int worth = ceil_div(ceil_div(keys, 64), kLeastTiles), room = prompt_groups(p->dp) / (int)items;
+        const int worth = parts_worth(ceil_div(keys, 64)), room = prompt_groups(p->dp) / (int)items;
         p->splits = worth < room ? worth : room;
     }
     p->bytes = (size_t)kCounterAreaWords * sizeof(uint32_t) + kPairAreaBytes;
@@ -600,7 +613,7 @@ int launch_prompt_one(const PromptParams& p, int units, hipStream_t s)
     auto fn = attn_prompt_kernel<DP, kPromptWaves, EXACT>;
     const int st = set_max_lds(reinterpret_cast<const void*>(fn), T::kLds);
     if (st) return st;
-    hipLaunchKernelGGL(fn, dim3((unsigned)(units * p.Hq * p.splits)), dim3(kPromptWaves * kWave), T::kLds, s, p);
+    hipLaunchKernelGGL(fn, dim3((unsigned)(units * p.Hk * p.splits)), dim3(kPromptWaves * kWave), T::kLds, s, p);
     return hipGetLastError() == hipSuccess ? CODEGEMM_OK : CODEGEMM_LAUNCH_FAILED;
 }
 
@@ -640,7 +653,8 @@ extern "C" int codegemm_attn_prompt(const codegemm_attn_desc* desc, const void* 
     p.cu_q = cu_q;
     p.cu_kv = cu_kv;
     p.seqs = d.num_seqs; p.total_q = d.total_q; p.total_kv = d.total_kv;
-    p.Hq = d.q_heads; p.r = d.q_heads / d.kv_heads; p.D = d.head_dim;
+    p.Hk = d.kv_heads; p.r = d.q_heads / d.kv_heads; p.D = d.head_dim;
+    p.by_r = 1.0f / (float)p.r;
     p.q_stride = row_stride(d.q_stride, d.q_heads * d.head_dim);
     p.k_stride = row_stride(d.k_stride, d.kv_heads * d.head_dim);
     p.v_stride = row_stride(d.v_stride, d.kv_heads * d.head_dim);

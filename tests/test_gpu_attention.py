@@ -234,6 +234,20 @@ def test_prompt_head_layouts(heads, group):
     check(prompt(q, k, v, [50, 100], [50, 100]), *prompt_exact(q, k, v, [50, 100], [50, 100]), f"{heads} x {group}")
 
 
+@pytest.mark.parametrize("group", [3, 7, 127, 128, 129, 1024])
+def test_prompt_heads_that_share_a_tile(group):
+    """Rows of a tile are query heads of some queries; where they do not divide evenly, a query's heads lie in two tiles or more."""
+    new, total = [1, 3, 0, 9], [1, 80, 4, 70]
+    if group < 100:
+        new, total = [150, 3, 0, 61], [150, 80, 4, 300]
+    q, k, v = packed(sum(new), sum(total), group, 1, 64)
+    rows = set(range(0, sum(new), 9)) | {1, sum(new) - 1}
+    for window, causal in ((0, True), (20, True), (0, False)):
+        got = prompt(q, k, v, new, total, window=window, causal=causal)
+        assert bool(got.isfinite().all())
+        check(got[sorted(rows)], *prompt_exact(q, k, v, new, total, window=window, causal=causal, rows=rows), f"{group} heads, window {window}")
+
+
 @pytest.mark.parametrize("new,total", [([5, 70], [300, 70]), ([1, 1, 1], [1, 64, 200]), ([33], [97]), ([40, 100], [10, 60]), ([20], [0]), ([0, 3], [50, 3]), ([130], [131])])
 @pytest.mark.parametrize("causal", [True, False])
 def test_prompt_lengths_of_queries_and_keys(new, total, causal):
