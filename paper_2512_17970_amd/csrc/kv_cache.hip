@@ -1,7 +1,7 @@
 // The paged cache: new keys and values go in, rotated and normalised on the way, and come out again as contiguous fp16.
 //
-// Append: a workgroup takes the queries of a token, or the keys (or values) of one head for the tokens that share a scale, so that their largest
-// |x| stays within it; a lane has 16 elements of a row, those that turn with each other, so that rotation needs no exchange and the norm a few.
+// Append: a team of 128 threads takes the queries of a token, a workgroup the keys (or values) of one head for the tokens that share a scale, so
+// that their largest |x| stays within it; a lane has 16 elements of a row, those that turn with each other, so that rotation needs no exchange and the norm a few.
 // Bound by the bytes: 8446 tokens, 64 and 8 heads of 128, 8 bits: 73 us for 346 MB, 4.7 TB/s; by launch and dependent loads where there are few: one
 // token of 32 heads 3.6 us, 32 sequences' 5.7 (lengths, page, old scale, tokens).
 // Gather: a workgroup takes 16 tokens of one head, values by way of LDS, which turns them.  30087 tokens of 8 heads, 8 bits: 30 to 33 us for
@@ -10,7 +10,9 @@
 
 namespace cg {
 
-constexpr int kAppendThreads = 128;
+constexpr int kAppendThreads = 128;         // that take 16 tokens of a head, or the queries of a token
+constexpr int kMostTeams = 8;               // of them in a workgroup
+constexpr int kTeamsAtOnce = 2048;          // 16 wavefronts on each of 256 compute units
 constexpr int kLastEnd = 0x7ffffe00;        // a length past every table, from which counting on by a unit stays within 32 bits
 
 struct AppendParams {
@@ -26,8 +28,9 @@ struct AppendParams {
     int row_lanes;      // lanes of a row of D: the power of two from D / 16 on
     int group;          // tokens of a unit: those that share a scale, at least kTokenGroup
     int units;          // of keys, and of values
+    int teams;          // of a workgroup
     int token_blocks;   // workgroups that work on queries, ahead of those of keys and values
-    int token_split;    // .. of one token
+    int token_split;    // teams of one token
 };
 
 __device__ __forceinline__ int new_tokens(const AppendParams& p, int seq, int* row0)
@@ -139,34 +142,35 @@ __device__ __forceinline__ float value_of(uint8_t c)
     else return (float)__builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)c, 1.0f, false)[0];
 }
 
-// Queries of one token: a workgroup, or token_split of them.
-__device__ void append_queries(const AppendParams& p, int blk)
+// Queries of one token: a team, or token_split of them.
+__device__ void append_queries(const AppendParams& p, int team)
 {
-    const int token = blk / p.token_split, part = blk % p.token_split;
-    const int lanes = p.row_lanes, c = threadIdx.x & (lanes - 1), rows = kAppendThreads / lanes;
+    const int token = team / p.token_split, part = team % p.token_split;
+    if (token >= p.T) return;
+    const int tid = threadIdx.x % kAppendThreads, lanes = p.row_lanes, c = tid & (lanes - 1), rows = kAppendThreads / lanes;
     const bool live = c < p.c.D / 16;
     const Runs r = runs_of(c, p.R, p.interleaved != 0);
     // the first rows are on their way while the token's position is looked up
     float x[16];
     auto load = [&](int h) { load_row(x, p.q + (size_t)token * p.q_stride + (h < p.Hq ? h : 0) * p.c.D, r, live && h < p.Hq); };
-    if (p.Hq > 0) load(part * rows + threadIdx.x / lanes);
+    if (p.Hq > 0) load(part * rows + tid / lanes);
     const int seq = p.cu ? last_at_most(p.c.seqs, token, [&](int i) { return p.cu[i]; }) : token;
     int row0;
     const int n = new_tokens(p, seq, &row0);
     const int len = p.c.lens[seq], position = (len < 0 ? 0 : len) - n + token - row0;
     const float zeros[16] = {0};
     if (position < 0) {                              // no place in the sequence
-        for (int h = part * rows + threadIdx.x / lanes; h < p.Hq; h += rows * p.token_split)
+        for (int h = part * rows + tid / lanes; h < p.Hq; h += rows * p.token_split)
             if (live) store_row(p.q_out + (size_t)token * p.q_out_stride + h * p.c.D, zeros, r);
         if (part == 0 && p.k_out)
-            for (int h = threadIdx.x / lanes; h < p.c.Hk; h += rows)
+            for (int h = tid / lanes; h < p.c.Hk; h += rows)
                 if (live) store_row(p.k_out + (size_t)token * p.k_out_stride + h * p.c.D, zeros, r);
         return;
     }
     Turn t;
     if (live && r.turns) t = load_turn(p, position, c);
     for (int h0 = part * rows; h0 < p.Hq; h0 += rows * p.token_split) {          // uniform: the norm's exchanges need whole rows
-        const int h = h0 + threadIdx.x / lanes;
+        const int h = h0 + tid / lanes;
         const bool mine = live && h < p.Hq;
         if (h0 > part * rows) load(h);
         if (p.q_norm) norm_row(x, p.q_norm, r, mine, lanes, p.c.D, p.eps);
@@ -177,12 +181,13 @@ __device__ void append_queries(const AppendParams& p, int blk)
 }
 
 // Keys or values of one unit: up to `group` new tokens of one sequence and head that share a page, and their scales.
-template <int TYPE>
+template <int TYPE, bool TEAMS>
 __device__ void append_unit(const AppendParams& p, int unit, int head, bool values, unsigned char* lds)
 {
     typedef typename KvType<TYPE>::elem elem;
     const CacheView& cv = p.c;
-    const int D = cv.D, G = p.group, lanes = p.row_lanes, tid = threadIdx.x, c = tid & (lanes - 1), rows = kAppendThreads / lanes;
+    const int D = cv.D, G = p.group, lanes = p.row_lanes, teams = TEAMS ? p.teams : 1, threads = teams * kAppendThreads, tid = threadIdx.x;
+    const int team = TEAMS ? __builtin_amdgcn_readfirstlane(tid / kAppendThreads) : 0, member = TEAMS ? tid % kAppendThreads : tid, c = member & (lanes - 1), rows = kAppendThreads / lanes;
     int seq = unit;
     if (p.cu) seq = last_at_most(cv.seqs, unit, [&](int i) { return p.cu[i] / G + 2 * i; });
     int row0;
@@ -211,24 +216,27 @@ __device__ void append_unit(const AppendParams& p, int unit, int head, bool valu
         if (mine && r.turns) rotate_row(x, load_turn(p, pos, c), p.interleaved != 0);
     };
 
-    // Where all tokens of the unit lie in one group of 16 and a pass of the workgroup takes them, they stay in registers from the search for the
-    // largest to their conversion.
-    const bool kept = hi - lo <= rows && lo / kTokenGroup == (hi - 1) / kTokenGroup;
+    // The unit's groups of 16 tokens go round the teams; where each team has one at most and takes it at once, tokens stay in registers from the search
+    // for the largest to their conversion.
+    const int group0 = lo & ~(kTokenGroup - 1), groups = (hi - 1 - group0) / kTokenGroup + 1, rounds = (groups + teams - 1) / teams;
+    const bool kept = rounds == 1 && (rows >= kTokenGroup || (groups == 1 && hi - lo <= rows));
     float x[16];
     uint32_t* of_block = reinterpret_cast<uint32_t*>(lds);                                 // [G / block <= 16]: the bits of the largest |x|, then of the scale
     auto scale_of_block = [&](int b) { return __builtin_bit_cast(float, of_block[b]); };
     if constexpr (TYPE != CODEGEMM_KV_FP16) {
         // The largest |x| of every block.  As bits: they order as the values do, with infinities and NaN above all numbers.
         const int blocks = G >> cv.block_shift;
-        for (int b = tid; b < blocks; b += kAppendThreads) of_block[b] = 0;
+        for (int b = tid; b < blocks; b += threads) of_block[b] = 0;
         float* scales = (values ? cv.v_scales : cv.k_scales) + (page < 0 ? 0 : scales_at(cv, page, head) + (slot0 >> cv.block_shift));
         const int b_lo = (lo - pos0) >> cv.block_shift, first_lo = pos0 + (b_lo << cv.block_shift);
         const bool earlier = page >= 0 && first_lo < lo;                                   // the block of the first new token holds tokens already
         const float old = earlier ? scales[b_lo] : 0.0f;
         __syncthreads();
-        for (int t0 = lo; t0 < hi; t0 += rows) {
-            const int pos = t0 + tid / lanes;
-            const bool mine = live && pos < hi;
+        // tokens that stay: those of the team's group; else as they come
+        const int g0 = group0 + team * kTokenGroup, t_lo = !kept ? lo + team * rows : g0 > lo ? g0 : lo, t_hi = kept && g0 + kTokenGroup < hi ? g0 + kTokenGroup : hi;
+        for (int t0 = t_lo; t0 < t_hi; t0 += teams * rows) {
+            const int pos = t0 + member / lanes;
+            const bool mine = live && pos < t_hi;
             load(x, pos, mine);
             uint32_t m = 0;
 #pragma unroll
@@ -243,7 +251,7 @@ __device__ void append_unit(const AppendParams& p, int unit, int head, bool valu
             if (mine && c == 0) atomicMax(&of_block[(pos - pos0) >> cv.block_shift], m);
         }
         __syncthreads();
-        for (int b = tid; b < blocks; b += kAppendThreads) {
+        for (int b = tid; b < blocks; b += threads) {
             const int first = pos0 + (b << cv.block_shift), past = first + (1 << cv.block_shift);
             if (page < 0 || past <= lo || first >= hi) continue;
             const uint32_t m = of_block[b];
@@ -260,7 +268,7 @@ __device__ void append_unit(const AppendParams& p, int unit, int head, bool valu
             const int slot_lo = slot0 + first_lo - pos0, slot_hi = slot0 + lo - pos0;
             // of keys, 16 dimensions of a token; of values, a dimension's group of 16 tokens, of which the block may have a part
             const int piece0 = values ? slot_lo / kTokenGroup * D : slot_lo * D / 16, pieces = (values ? ceil_div(slot_hi, kTokenGroup) * D : slot_hi * D / 16) - piece0;
-            for (int i = tid; i < pieces; i += kAppendThreads) {
+            for (int i = tid; i < pieces; i += threads) {
                 u32x4_t* at16 = reinterpret_cast<u32x4_t*>(pool + at) + piece0 + i;
                 const int t0 = values ? (piece0 + i) / D * kTokenGroup : slot_lo;
                 const u32x4_t in = *at16;
@@ -280,12 +288,12 @@ __device__ void append_unit(const AppendParams& p, int unit, int head, bool valu
         }
     }
 
-    elem* stage = reinterpret_cast<elem*>(lds + 64);                                       // [D][16] of a group of 16 tokens, 16 bytes more every 16 rows
     constexpr int kPad = 16 / (int)sizeof(elem);
-    for (int g0 = lo & ~(kTokenGroup - 1); g0 < hi; g0 += kTokenGroup) {
-        const int glo = g0 > lo ? g0 : lo, ghi = g0 + kTokenGroup < hi ? g0 + kTokenGroup : hi;
+    elem* stage = reinterpret_cast<elem*>(lds + 64) + team * (D * kTokenGroup + D / 16 * kPad);      // [D][16] of a group of 16 tokens, 16 bytes more every 16 rows
+    for (int round = 0; round < rounds; ++round) {                                         // a team may have none in the last
+        const int g0 = group0 + (round * teams + team) * kTokenGroup, glo = g0 > lo ? g0 : lo, ghi = g0 + kTokenGroup < hi ? g0 + kTokenGroup : hi;
         for (int t0 = glo; t0 < ghi; t0 += rows) {
-            const int pos = t0 + tid / lanes;
+            const int pos = t0 + member / lanes;
             const bool mine = live && pos < ghi;
             if (TYPE == CODEGEMM_KV_FP16 || !kept) load(x, pos, mine);
             if (!mine) continue;
@@ -320,13 +328,13 @@ __device__ void append_unit(const AppendParams& p, int unit, int head, bool valu
             elem* dst = reinterpret_cast<elem*>(pool) + at + (size_t)((slot0 + g0 - pos0) / kTokenGroup) * D * kTokenGroup;
             if (ghi - glo == kTokenGroup) {
                 constexpr int kVec = 16 / (int)sizeof(elem);                               // elements of 16 bytes
-                for (int i = tid; i < D * kTokenGroup / kVec; i += kAppendThreads) {
+                for (int i = member; i < D * kTokenGroup / kVec; i += kAppendThreads) {
                     const int d = i * kVec / kTokenGroup;
                     *reinterpret_cast<u32x4_t*>(dst + i * kVec) = *reinterpret_cast<const u32x4_t*>(stage + i * kVec + d / 16 * kPad);
                 }
             } else {
                 const int tokens = ghi - glo;
-                for (int i = tid; i < D * tokens; i += kAppendThreads) {
+                for (int i = member; i < D * tokens; i += kAppendThreads) {
                     const int d = i / tokens, t = (glo & (kTokenGroup - 1)) + i % tokens;
                     dst[d * kTokenGroup + t] = stage[d * kTokenGroup + d / 16 * kPad + t];
                 }
@@ -336,19 +344,37 @@ __device__ void append_unit(const AppendParams& p, int unit, int head, bool valu
     }
 }
 
+// Bytes of LDS of a workgroup.
 template <int TYPE>
-__global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(const AppendParams p)
+constexpr size_t append_lds(int teams, int D) { return 64 + (size_t)teams * (D * kTokenGroup * sizeof(typename KvType<TYPE>::elem) + D); }
+
+template <int TYPE, bool TEAMS>
+__global__ void __launch_bounds__(TEAMS ? kMostTeams * kAppendThreads : kAppendThreads) kv_append_kernel(const AppendParams p)
 {
-    __shared__ __align__(16) unsigned char lds[64 + (kMaxHeadDim * kTokenGroup + 256) * sizeof(typename KvType<TYPE>::elem)];
+    extern __shared__ __align__(16) unsigned char lds[];
     const int blk = blockIdx.x;
     if (blk < p.token_blocks) {
-        append_queries(p, blk);
+        append_queries(p, TEAMS ? blk * p.teams + __builtin_amdgcn_readfirstlane(threadIdx.x / kAppendThreads) : blk);
         return;
     }
     const int i = blk - p.token_blocks, half = p.units * p.c.Hk;
     const bool values = i >= half;
     const int j = values ? i - half : i;
-    append_unit<TYPE>(p, j / p.c.Hk, j % p.c.Hk, values, lds);
+    append_unit<TYPE, TEAMS>(p, j / p.c.Hk, j % p.c.Hk, values, lds);
+}
+
+template <int TYPE>
+static void launch_append(const AppendParams& p, unsigned blocks, hipStream_t s)
+{
+    const dim3 grid(blocks), threads(p.teams * kAppendThreads);
+    const size_t lds = append_lds<TYPE>(p.teams, p.c.D);
+    if constexpr (TYPE != CODEGEMM_KV_FP16) {
+        if (p.teams > 1) {
+            hipLaunchKernelGGL((kv_append_kernel<TYPE, true>), grid, threads, lds, s, p);
+            return;
+        }
+    }
+    hipLaunchKernelGGL((kv_append_kernel<TYPE, false>), grid, threads, lds, s, p);
 }
 
 struct GatherParams {
@@ -522,17 +548,22 @@ extern "C" int codegemm_kv_append(const codegemm_kv_cache* cache, const codegemm
     p.group = cache->dtype == CODEGEMM_KV_FP16 || block < kTokenGroup ? kTokenGroup : block;
     // A sequence of n new tokens touches at most n / group + 2 units, its first unit being number cu / group + 2 i.
     p.units = cu_seqlens ? p.T / p.group + 2 * cache->num_seqs : cache->num_seqs;
-    // Few tokens: their heads over several workgroups.  Many: a workgroup keeps a token's cosines for all its heads.
+    // Few tokens: their heads over several teams.  Many: a team keeps a token's cosines for all its heads.
     const int rows = kAppendThreads / p.row_lanes;
     p.token_split = p.T >= 1024 || p.Hq == 0 ? 1 : ceil_div(p.Hq, rows);
-    p.token_blocks = p.Hq > 0 || k_out ? p.T * p.token_split : 0;
+    // Long blocks with many new tokens: a team for each 16 of them, as long as the card has room for all (12 sequences of 4 heads, 2500 tokens: blocks
+    // of 256 take 49.8 us with one team, 27.5 with 7; 4 of 8 heads, blocks of 64 30.7 with one, 28.7 with 2; of 32, 27.3 and 28.0).
+    const int fresh = ceil_div(p.T, cache->num_seqs), useful = (fresh < p.group ? fresh : p.group) / kTokenGroup;
+    const long long room = kTeamsAtOnce / (2ll * p.units * Hk);
+    const int teams = useful < 4 ? 1 : room < useful ? (int)room : useful;
+    p.teams = teams < 1 ? 1 : teams < kMostTeams ? teams : kMostTeams;
+    p.token_blocks = p.Hq > 0 || k_out ? (int)(((long long)p.T * p.token_split + p.teams - 1) / p.teams) : 0;
     const long long blocks = p.token_blocks + 2ll * p.units * Hk;
-    if (too_many(blocks, kAppendThreads)) return CODEGEMM_UNSUPPORTED;
-    const dim3 grid((unsigned)blocks), threads(kAppendThreads);
+    if (too_many(blocks, p.teams * kAppendThreads)) return CODEGEMM_UNSUPPORTED;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (cache->dtype == CODEGEMM_KV_FP16) hipLaunchKernelGGL(kv_append_kernel<CODEGEMM_KV_FP16>, grid, threads, 0, s, p);
-    else if (cache->dtype == CODEGEMM_KV_INT8) hipLaunchKernelGGL(kv_append_kernel<CODEGEMM_KV_INT8>, grid, threads, 0, s, p);
-    else hipLaunchKernelGGL(kv_append_kernel<CODEGEMM_KV_FP8>, grid, threads, 0, s, p);
+    if (cache->dtype == CODEGEMM_KV_FP16) launch_append<CODEGEMM_KV_FP16>(p, (unsigned)blocks, s);
+    else if (cache->dtype == CODEGEMM_KV_INT8) launch_append<CODEGEMM_KV_INT8>(p, (unsigned)blocks, s);
+    else launch_append<CODEGEMM_KV_FP8>(p, (unsigned)blocks, s);
     return hipGetLastError() == hipSuccess ? CODEGEMM_OK : CODEGEMM_LAUNCH_FAILED;
 }
 

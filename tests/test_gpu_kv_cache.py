@@ -123,6 +123,15 @@ def test_append_blocks_and_pages(page, block, dtype):
     append(Cache(grown(past, new), heads=1, dim=64, page=page, dtype=dtype, block=block, seed=page, filled=past), new)
 
 
+@pytest.mark.parametrize("page,block", [(32, 32), (64, 64), (128, 128), (256, 256)])
+@pytest.mark.parametrize("dtype,dim", [(INT8, 128), (FP8, 64), (INT8, 256), (FP8, 16)])
+def test_append_long_blocks_with_many_new_tokens(page, block, dtype, dim):
+    """The 16-token groups of a block go round several teams of a workgroup."""
+    past, new = [0, 37, 250], [301, 100, 17]
+    append(Cache(grown(past, new), heads=1, dim=dim, page=page, dtype=dtype, block=block, seed=page, filled=past), new, norm=dim == 64)
+    append(Cache(grown([5], [11]), heads=2, dim=dim, page=page, dtype=dtype, block=block, seed=page, filled=[5]), [11])
+
+
 @pytest.mark.parametrize("size", [1e-3, 1.0, 30.0])
 @pytest.mark.parametrize("dtype", [INT8, FP8])
 def test_append_scales_grow_and_stay(size, dtype):
