@@ -13,10 +13,10 @@
 // 8-bit codes become fp16 exactly on the way into the matrix cores; a key's scale multiplies its score, a value's scale its weight.
 //
 // Bound by: the cache's bytes, where there are many.  32 sequences of 206 376 tokens, 64 and 8 heads of 128, 8 bits: 82 us, 5.2 TB/s; 3 of 240 551,
-// fp8: 88 us, 5.6 TB/s (a large copy: 4.85, read and written); loads that nothing is computed with take 81 and 87.  13 of twenty heads of 64 in fp16
+// fp8: 86 us, 5.7 TB/s (a large copy: 4.85, read and written); loads that nothing is computed with take 81 and 87.  13 of twenty heads of 64 in fp16
 // with a window of 1500: 22.5 us, 4.0 TB/s.  Steps held in registers instead of LDS took 93 and 136 us at best.
-// Shortest: 700 tokens of one sequence, 10.5 us, of which 6.3 are one step of every wavefront (of 100 tokens) and 4 the exchange between workgroups;
-// three steps in one workgroup take 11.3.
+// Shortest: 700 tokens of one sequence, 10.2 us, of which 6.3 are one step of every wavefront (of 100 tokens) and 4 the exchange between workgroups;
+// three steps in one workgroup take 11.3.  8000 tokens: 15.0.
 #include <cmath>
 #include <type_traits>
 

@@ -21,7 +21,7 @@
 // 1634), and 128 rows share a tile of keys and values in LDS.
 // Bound by: power, where sequences are long.  8192 causal queries, 64 and 8 heads of 128: 1140 to 1190 us from card to card, 0.92 to 0.96 PFLOP/s (a
 // library product of 8192^3 reaches 1.12), the matrix cores busy in 53 % of the cycles at 1.7 GHz; all zeros take 943 us.  Of ragged
-// prompts of 500 to 1100 tokens, 32 and 8 heads: 72 us, 0.65 PFLOP/s; a tile of rows costs some 7 us besides its keys.
+// prompts of 500 to 1100 tokens, 32 and 8 heads: 69 to 72 us, 0.65 to 0.68 PFLOP/s; a tile of rows costs some 7 us besides its keys.
 #include "attn_common.h"
 
 namespace cg {
