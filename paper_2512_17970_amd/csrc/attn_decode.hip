@@ -31,6 +31,10 @@ constexpr int kRoundSteps = 10;             // .. and a second piece for the sam
 constexpr int kJoined = 8;                  // pieces that are joined at a time
 constexpr int kMostGroups = 1 << 20;        // workgroups of a launch, which has fewer than 2^32 threads
 constexpr float kLeastLog = -40.0f;         // of a scale's logarithm in the running maximum
+// The largest weight is 2^kLift, so that fp16 holds weights down to 2^-28 of it with all their places and down to 2^-38 at all: behind one key that has most of
+// the weight and values near zero, thousands of others with little weight each make the result.  (With 1 for the largest, the weights of the keys that share
+// a wavefront with such a key were off by 2.6 % at 15 nats below it, by 44 % at 17, and zero at 18.)  Not from scores of kFine on, which may have no place for it.
+constexpr float kLift = 14.0f, kFine = 1048576.0f;
 
 struct DecodeParams {
     CacheView c;
@@ -376,7 +380,7 @@ attn_decode_kernel(const DecodeParams p)
                         if constexpr (!T::kHalf) vs[n][r] = seen ? vs[n][r] : 0.0f;
                     }
             }
-            // The maximum is taken over score + log2 of the value's scale, so that weight times scale, rounded to fp16, is at most 1.
+            // The maximum is taken over score + log2 of the value's scale, so that weight times scale, rounded to fp16, is at most 2^kLift.
             float most = -INFINITY;
             if (T::kHalf || (whole && cv.block_shift >= 3)) {           // one scale for the run
 #pragma unroll
@@ -391,6 +395,7 @@ attn_decode_kernel(const DecodeParams p)
                     for (int r = 0; r < 4; ++r) most = fmaxf(most, s[n][r] + fmaxf(__builtin_amdgcn_logf(vs[n][r]), kLeastLog));
             }
             most = over_groups(most, [](float a, float b) { return fmaxf(a, b); });
+            most -= fabsf(most) < kFine ? kLift : 0.0f;
             const float m_new = fmaxf(m, most), base = m_new == -INFINITY ? 0.0f : m_new;
             const float keep = __builtin_amdgcn_exp2f(m - base);
             m = m_new;
@@ -401,9 +406,13 @@ attn_decode_kernel(const DecodeParams p)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const float w = __builtin_amdgcn_exp2f(s[n][r] - base);
-                    add += w;
                     pf[4 * n + r] = (_Float16)(T::kHalf ? w : w * vs[n][r]);
+                    if constexpr (!T::kHalf) add += w;                   // (unrounded, as products have scales: off by 2^-11 at most)
                 }
+            if constexpr (T::kHalf) {                                    // the sum of the weights as they are rounded
+#pragma unroll
+                for (int i = 0; i < 8; i += 2) add = __builtin_amdgcn_fdot2(half2_t{pf[i], pf[i + 1]}, half2_t{(_Float16)1.0f, (_Float16)1.0f}, add, false);
+            }
             l = l * keep + add;
             // values that do not count are zeros: what lies there may be a NaN
             u32x4_t mask = {~0u, ~0u, ~0u, ~0u};

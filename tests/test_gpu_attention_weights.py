@@ -1,0 +1,88 @@
+"""Softmax weights far below the largest: one key that takes most of the weight and has values of zero, and tens of thousands of equal keys whose small
+weights make the whole result.  Against the definition in 64 bits."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+cg = pytest.importorskip("paper_2512_17970_amd")
+from attention_util import Cache, decode  # noqa: E402
+
+FP16, INT8, FP8 = cg.binding.KV_FP16, cg.binding.KV_INT8, cg.binding.KV_FP8
+N = 50000
+
+
+def bound(n):
+    """Relative error of a result that n equal weights make: a weight's rounding to fp16 (2^-11, all of them the same way) and the result's (2^-11); a score of
+    up to 30 in base 2 is off by 30 2^-23 ln 2 at most, its exponential by two units of 2^-23; sums in 32 bits add n / 32 products of 32 keys to one another in
+    turn, and twice as many times a handful of weights to the sum of all, of which one may be far larger: 3 n / 32 2^-24 (with the former, 2^-11 at least)."""
+    return 2.0 ** -10 + max(2.0 ** -11, 3 * n / 32 * 2.0 ** -24)
+
+
+def column(dim):
+    """Values of the equal keys, one for each dimension; exact in fp16, and times 64 in int8; of 3 bits of mantissa."""
+    return (torch.arange(dim) % 8 + 8).double().cuda() / 8
+
+
+def close(got, gap, n, dim):
+    """got [..][dim]; n equal keys `gap` nats under the one whose values are zero."""
+    w = n * math.exp(-gap)
+    want = w / (1 + w) * column(dim)
+    error = float(((got.double() - want).abs() / want).max())
+    assert error <= bound(n), f"{gap} nats: {error:.1e}, {error / bound(n):.2f} times the bound"
+
+
+def sink_cache(n, at, dim, dtype, block, heads=1, seqs=1):
+    """n + 1 tokens, all keys zero but that of token `at`, which has 4 in dimension 0 and values of zero."""
+    c = Cache([n + 1] * seqs, heads=heads, dim=dim, page=64, dtype=dtype, block=block, filled=[0] * seqs)
+    one, v = {FP16: (1.0, column(dim).half()), INT8: (64.0, (column(dim) * 64).to(torch.int8).view(torch.uint8)),
+              FP8: (1.0, column(dim).to(torch.float8_e4m3fn).view(torch.uint8))}[dtype]
+    c.k.zero_()
+    c.v.copy_(v[:, None].expand_as(c.v))
+    key = torch.zeros(1, dim, device="cuda")
+    key[0, 0] = 4.0
+    if dtype == FP16:
+        key = key.half()
+    else:
+        c.k_scales.fill_(1 / 16 if dtype == INT8 else 1.0)
+        c.v_scales.fill_(1 / one)
+        key = (key * 16).to(torch.int8).view(torch.uint8) if dtype == INT8 else key.to(torch.float8_e4m3fn).view(torch.uint8)
+    for i in range(seqs):
+        c.place(c.k, i, at, False).copy_(key.expand(heads, dim))
+        c.place(c.v, i, at, True).zero_()
+        for t in range(n + 1, -(-(n + 1) // 64) * 64):                   # behind the last token
+            c.place(c.v, i, t, True).fill_(float("nan") if dtype == FP16 else 0x7F)
+    return c
+
+
+def sink_query(heads, dim, seqs=1):
+    q = torch.zeros(seqs, heads, dim, dtype=torch.float16, device="cuda")
+    q[:, :, 0] = 8.0
+    return q
+
+
+@pytest.mark.parametrize("dtype,block,dim", [(FP16, 1, 64), (FP16, 1, 256), (INT8, 16, 128), (INT8, 1, 64), (INT8, 4, 80), (FP8, 64, 128), (FP8, 1, 64)])
+@pytest.mark.parametrize("at", [0, 20011, N])
+def test_decode_small_weights_behind_a_sink(dtype, block, dim, at):
+    c, q = sink_cache(N, at, dim, dtype, block), sink_query(8, dim)
+    for gap in (5.0, 10.0, 12.5, 14.0, 15.0, 16.0, 17.0, 18.0):
+        close(decode(c, q, scale=gap / 32), gap, N, dim)
+
+
+@pytest.mark.parametrize("dtype,block,dim", [(FP16, 1, 64), (FP16, 1, 128), (INT8, 16, 128), (INT8, 16, 64), (INT8, 4, 80), (FP8, 64, 128), (FP8, 16, 256)])
+def test_decode_small_weights_behind_a_sink_in_one_workgroup(dtype, block, dim):
+    """More items than compute units: none is cut, and a wavefront has a quarter or half of a sequence's keys."""
+    n = 6000
+    c, q = sink_cache(n, 0, dim, dtype, block, heads=60, seqs=5), sink_query(60, dim, 5)
+    for gap in (5.0, 10.0, 12.5, 14.0, 15.0, 16.0, 17.0):
+        close(decode(c, q, scale=gap / 32), gap, n, dim)
+
+
+@pytest.mark.parametrize("below", [20, 24, 27, 28, 30])
+def test_decode_weights_that_are_powers_of_two(below):
+    """A million keys a power of two below the sink."""
+    n, dim, ln2 = 1 << 20, 64, math.log(2.0)
+    for at in (0, n):
+        close(decode(sink_cache(n, at, dim, FP16, 1), sink_query(2, dim), scale=below * ln2 / 32), below * ln2, n, dim)
