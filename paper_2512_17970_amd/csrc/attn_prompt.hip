@@ -4,13 +4,12 @@
 // head for each query (with a tile of queries to each head, 256 prompts of 128 tokens, 32 and 8 heads, took 190 us, so 170: fewer tiles that are part
 // full, fewer keys that only some rows see).  It walks over the keys in tiles of
 // BN.  S^T = K Q^T (rows: keys, columns: queries) in 32x32x16 products, so a lane holds all its scores for one query, and what the
-// running maximum and sum of the softmax need from other lanes is one exchange with the other half of the wavefront.  P^T goes from the
+// softmax's running maximum and sum need from other lanes is one exchange with the other half of the wavefront.  P^T goes from the
 // score tiles into the right operand of O^T += V^T P^T as it lies; V^T comes out of LDS transposed (ds_read_tr16).  Keys and values
 // come into LDS by the memory pipeline (buffer_load .. lds), one tile ahead.  A wavefront goes on in blocks of 32 keys, three at a time: the
 // scores of one and the product of another's weights with its values on the matrix cores, the weights of the one between by vector
 // instructions; none waits for the others.  (Matrix and vector instructions of one wavefront overlap; those of two disturb each other.)
-// The running maximum follows the scores only where one is over 2^8 times its weight above it (fp16 holds up to 2^16), so that the sums are
-// seldom rescaled.
+// What weights are scaled by follows the scores only where one would pass 2^kReach, so that the sums are seldom rescaled.
 //
 // Tiles in which some query of the workgroup does not see some key come first.  A value that a query does not see has weight 0 there,
 // which leaves its sum alone unless the value is a NaN or an infinity; so the sums are looked at once after these tiles, and where they are
@@ -37,7 +36,7 @@ struct PromptParams {
     int window, causal;
     int negate;             // a negative scale: of -q
     float scale;            // its size, times log2(e)
-    float reach;            // 8 over that: so far scores may pass the maximum
+    float unit;             // 1 / scale
     int splits;             // workgroups of a tile of queries and head, at most
     float* part;            // [item][split][NW][DP / 8][64 lanes][4] sums, [NW][64] maximum and weight
     uint32_t* counters;     // of an item
@@ -54,6 +53,12 @@ __host__ __device__ inline int parts_worth(int tiles)
     const int most = (tiles + kLeastTiles - 1) / kLeastTiles, best = (int)__builtin_sqrtf(2.0f * (float)tiles) + 1;
     return most < 1 ? 1 : most < best ? most : best;
 }
+
+// A query's largest weight so far is between 2^(kLift - 1) and 2^kReach (fp16 holds up to 2^16).
+constexpr float kLift = 0.0f, kReach = 8.0f;
+// From this size on, times scale, scores have too few places for that: weights are those of the differences from the largest score.
+constexpr float kFine = 65536.0f;
+constexpr float kNone = -3.402823466e38f;               // the logarithm of nothing
 
 constexpr int kLdsReads = 0x100, kProducts = 0x8;       // groups of instructions, for the scheduler
 
@@ -246,16 +251,18 @@ __global__ void __launch_bounds__(NW * kWave, DP == 256 ? 1 : 2) attn_prompt_ker
     half8_t qf[DP / 16];                                                 // Q^T: column qc, dimensions 16 s + 8 h .. + 7
     const int pos = back + first + query_of(row);                                          // the lane's query
 
-    // The running maximum m of the scores, as shift = -m scale; l: the sum of the weights as they are rounded.
+    // A weight is 2^((score - origin) scale + shift), the origin being 0 but for scores of kFine and more; l: the sum of the weights as they are rounded.
     float16_t o[DB];
-    float m, l, shift, limit;       // limit: the score from which on the maximum follows
+    float l, origin, shift, limit;  // limit: the score from which on these follow
+    uint64_t moved = 0;             // the lanes whose origin is not 0
     auto clear = [&]() __attribute__((always_inline)) {
 #pragma unroll
         for (int b = 0; b < DB; ++b)
 #pragma unroll
             for (int e = 0; e < 16; ++e) o[b][e] = 0.0f;
-        m = limit = -INFINITY;
-        l = shift = 0.0f;
+        limit = -INFINITY;
+        l = origin = shift = 0.0f;
+        moved = 0;
     };
     clear();
 
@@ -322,15 +329,19 @@ __global__ void __launch_bounds__(NW * kWave, DP == 256 ? 1 : 2) attn_prompt_ker
         const auto x = __builtin_amdgcn_permlane32_swap(w, w, false, false);
         return fmaxf(__builtin_bit_cast(float, (uint32_t)x[0]), __builtin_bit_cast(float, (uint32_t)x[1]));
     };
-    // The maximum follows the scores where it has to, and with it the sums and the weights that are still to go into them (their largest are then
-    // under 2^-8 of the new ones').  Without a maximum yet, shift is 0.
-    auto follow = [&](float most, half8_t (&pending)[2]) __attribute__((always_inline)) {
-        const bool far = most > limit;
-        if (!__any(far)) return;
-        const float keep = far ? __builtin_amdgcn_exp2f((m - most) * p.scale) : 1.0f;
-        m = far ? most : m;
-        limit = far ? most + p.reach : limit;
-        shift = far ? -most * p.scale : shift;
+    // The shift follows the scores where it has to, by whole numbers, and with it the sums and the weights that are still to go into them, which a power of two
+    // leaves all their places.  Where one query's does, those of others come along.
+    auto follow = [&](float most, half8_t (&pending)[2], auto&... scores) __attribute__((always_inline)) {
+        if ((__ballot(most > limit) | moved) == 0) return;
+        const float size = most * p.scale, weight = __builtin_fmaf(most - origin, p.scale, shift);      // its logarithm as it is
+        const bool fine = fabsf(size) < kFine, far = (most > limit) | (fine & (weight > kLift));
+        const float to = fine ? kLift - ceilf(size) : kLift, less = (fine ? __builtin_fmaf(most, p.scale, to) : kLift) - weight;
+        const float last = limit;
+        limit = far ? (fine ? (kReach - to) * p.unit : most) : limit;
+        shift = far ? to : shift;
+        origin = far ? (fine ? 0.0f : most) : origin;
+        const float keep = __builtin_amdgcn_exp2f(far ? (last == -INFINITY ? -INFINITY : less) : 0.0f);
+        moved = __ballot(origin != 0.0f);
         l *= keep;
 #pragma unroll
         for (int i = 0; i < 2; ++i) pending[i] *= (_Float16)keep;
@@ -338,6 +349,12 @@ __global__ void __launch_bounds__(NW * kWave, DP == 256 ? 1 : 2) attn_prompt_ker
         for (int b = 0; b < DB; ++b)
 #pragma unroll
             for (int e = 0; e < 16; ++e) o[b][e] *= keep;
+        if (moved == 0) return;
+        auto from_origin = [&](float16_t& of) __attribute__((always_inline)) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) of[e] -= origin;
+        };
+        (from_origin(scores), ...);
     };
     // Weights, and their sum as they are rounded.
     auto weights = [&](half8_t (&pf)[2], const float16_t& of) __attribute__((always_inline)) {
@@ -373,7 +390,7 @@ __global__ void __launch_bounds__(NW * kWave, DP == 256 ? 1 : 2) attn_prompt_ker
         }
 #pragma unroll
         for (int e = 0; e < 2; ++e) p0[e] = half8_t{0, 0, 0, 0, 0, 0, 0, 0};
-        follow(fmaxf(largest(s0), largest(s1)), p0);
+        follow(fmaxf(largest(s0), largest(s1)), p0, s0, s1);
         l += weights(p0, s0);
     };
     // Three blocks of 32 keys: scores of the next (kind 0: there is none, what is computed is not looked at; 1: all are seen; 2: masked), weights
@@ -400,7 +417,7 @@ __global__ void __launch_bounds__(NW * kWave, DP == 256 ? 1 : 2) attn_prompt_ker
             hide(next, next_key0);
             most = largest(next);
         }
-        follow(most, pf);
+        follow(most, pf, next);
     };
     // The tile of step i, but for its scores and first weights; those of the next.
     auto step = [&](int i) __attribute__((always_inline)) {
@@ -431,7 +448,7 @@ __global__ void __launch_bounds__(NW * kWave, DP == 256 ? 1 : 2) attn_prompt_ker
                 scores(s0, block);
                 hide(s0, key0);
                 half8_t pf[2] = {};
-                follow(largest(s0), pf);
+                follow(largest(s0), pf, s0);
                 l += weights(pf, s0);
 #pragma unroll
                 for (int ks = 0; ks < 2; ++ks)
@@ -519,7 +536,7 @@ __global__ void __launch_bounds__(NW * kWave, DP == 256 ? 1 : 2) attn_prompt_ker
             for (int b = 0; b < DB; ++b)
 #pragma unroll
                 for (int e = 0; e < 16; e += 4) put16(sums, own_part + place(b, e), float4_t{o[b][e], o[b][e + 1], o[b][e + 2], o[b][e + 3]});
-            put8(sums, own_part + ml, m, l);
+            put8(sums, own_part + ml, limit == -INFINITY ? kNone : origin * p.scale - shift, l);      // the logarithm of what l and the sums are multiples of
         }
         arrive();
         volatile uint32_t* flag = reinterpret_cast<volatile uint32_t*>(smem);
@@ -532,6 +549,7 @@ __global__ void __launch_bounds__(NW * kWave, DP == 256 ? 1 : 2) attn_prompt_ker
         __syncthreads();
         if (*flag == 0u) return;
         clear();
+        float m = kNone;
         if (row < rows_here)
             for (int k = 0; k < parts; ++k) {
                 float4_t w[DB * 4];
@@ -540,14 +558,13 @@ __global__ void __launch_bounds__(NW * kWave, DP == 256 ? 1 : 2) attn_prompt_ker
                 for (int b = 0; b < DB; ++b)
 #pragma unroll
                     for (int e = 0; e < 16; e += 4) w[b * 4 + e / 4] = get16(sums, k * kPart + place(b, e));
-                const float m_new = fmaxf(m, other.a), base = m_new == -INFINITY ? 0.0f : m_new;
-                const float keep = __builtin_amdgcn_exp2f((m - base) * p.scale), by = __builtin_amdgcn_exp2f((other.a - base) * p.scale);
+                const float m_new = fmaxf(m, other.a), keep = __builtin_amdgcn_exp2f(m - m_new), add = __builtin_amdgcn_exp2f(other.a - m_new);
                 m = m_new;
-                l = l * keep + by * other.b;
+                l = l * keep + add * other.b;
 #pragma unroll
                 for (int b = 0; b < DB; ++b)
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) o[b][e] = o[b][e] * keep + by * w[b * 4 + e / 4][e % 4];
+                    for (int e = 0; e < 16; ++e) o[b][e] = o[b][e] * keep + add * w[b * 4 + e / 4][e % 4];
             }
     }
     // Out through LDS, row after row: a wavefront stores whole rows, not 16 bytes of each of 32.  With Q's way in: 256 prompts of 128 tokens, 32 heads,
@@ -663,8 +680,8 @@ extern "C" int codegemm_attn_prompt(const codegemm_attn_desc* desc, const void* 
     p.causal = d.flags & CODEGEMM_ATTN_CAUSAL;
     p.negate = d.scale < 0.0f;
     const float size = d.scale < 0.0f ? -d.scale : d.scale;
-    p.scale = (float)((size > 1e-30f ? size : 1e-30f) * 1.4426950408889634);      // not 0: 0 times an infinite maximum is no number
-    p.reach = 8.0f / p.scale;
+    p.scale = (float)((size > 1e-30f ? size : 1e-30f) * 1.4426950408889634);      // not 0: 0 times an infinite score is no number
+    p.unit = 1.0f / p.scale;
     p.splits = plan.splits;
     p.counters = static_cast<uint32_t*>(workspace);
     p.part = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + (size_t)kCounterAreaWords * sizeof(uint32_t) + kPairAreaBytes);

@@ -1,5 +1,5 @@
 """Softmax weights far below the largest: one key that takes most of the weight and has values of zero, and tens of thousands of equal keys whose small
-weights make the whole result.  Against the definition in 64 bits."""
+weights make the whole result; scores beyond the range in which 32 bits hold their fractions.  Against the definition in 64 bits."""
 import math
 
 import pytest
@@ -8,10 +8,11 @@ import torch
 pytestmark = pytest.mark.gpu
 
 cg = pytest.importorskip("paper_2512_17970_amd")
-from attention_util import Cache, decode  # noqa: E402
+from attention_util import Cache, decode, prompt  # noqa: E402
 
 FP16, INT8, FP8 = cg.binding.KV_FP16, cg.binding.KV_INT8, cg.binding.KV_FP8
 N = 50000
+EMPTY = [0] * 4100          # sequences without tokens: as many tiles as keep the keys of one from being shared
 
 
 def bound(n):
@@ -86,3 +87,37 @@ def test_decode_weights_that_are_powers_of_two(below):
     n, dim, ln2 = 1 << 20, 64, math.log(2.0)
     for at in (0, n):
         close(decode(sink_cache(n, at, dim, FP16, 1), sink_query(2, dim), scale=below * ln2 / 32), below * ln2, n, dim)
+
+
+@pytest.mark.parametrize("size", [100.0, 1000.0, 8000.0, 60000.0])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_scores_beyond_all_fractions(size, sign, dim):
+    """Keys and queries up to the largest of fp16, scores up to 10^12, of which 32 bits hold no fraction: the one key whose score is the largest by far has all
+    the weight."""
+    n, heads, best = 700, 4, 333
+    g = torch.Generator().manual_seed(int(size) + dim)
+    signs = torch.where(torch.rand(dim, generator=g) < 0.5, -1.0, 1.0)
+    amount = torch.rand(n, generator=g) * 0.5                            # of positive scores; of negative ones 0.5 to 1, and the least for the largest
+    amount[best] = 1.0
+    if sign < 0:
+        amount = -(amount + 0.5)
+        amount[best] = -0.25
+    jitter = 1 + torch.rand(heads, generator=g) * 2.0 ** -4              # products with many places
+    q = (signs * jitter[None, :, None] * 0.9 * size).half().cuda()
+    k = (signs * amount[:, None, None] * size).half().cuda()
+    v = torch.randn(n, 1, dim, generator=g).half().cuda()
+    scale = dim ** -0.5
+    first, second = ((q[0].double() @ k[:, 0].double().t()) * scale).topk(2, dim=1).values.unbind(1)
+    assert bool((first - second > 0.2 * torch.maximum(first.abs(), second.abs())).all()) and float((first - second).min()) > 1000
+    want = v[best, 0]
+    for beside in ([], EMPTY):
+        for rows in (1, 60):
+            got = prompt(q.expand(rows, heads, dim).contiguous(), k, v, [rows] + beside, [n] + beside, scale=scale, causal=False)
+            assert torch.equal(got, want.expand_as(got)), f"prompt of {rows}"
+    c = Cache([n], heads=1, dim=dim, page=64, dtype=FP16, filled=[0])
+    for t in range(n):
+        c.place(c.k, 0, t, False).copy_(k[t])
+        c.place(c.v, 0, t, True).copy_(v[t])
+    got = decode(c, q, scale=scale)
+    assert torch.equal(got, want.expand_as(got)), "decode"
