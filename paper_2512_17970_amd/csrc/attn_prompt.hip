@@ -54,8 +54,11 @@ __host__ __device__ inline int parts_worth(int tiles)
     return most < 1 ? 1 : most < best ? most : best;
 }
 
-// A query's largest weight so far is between 2^(kLift - 1) and 2^kReach (fp16 holds up to 2^16).
-constexpr float kLift = 0.0f, kReach = 8.0f;
+// A query's largest weight so far is between 2^(kLift - 1) and 2^kReach: fp16 holds weights down to 2^-24 of it with all their places, and down to 2^-34 at
+// all.  Behind one key that has most of the weight and values near zero, thousands of others with little weight each make the result.  (With 1 to 2^8 for the
+// largest, 50000 keys 12.5 nats below such a key lost 0.7 % of their weight, at 17 it was off by 44 %, and zero at 18.  The further kReach is from kLift,
+// the seldomer weights are rescaled: 8192 queries of 64 heads take 1143 us, 1131 with 8 powers of two between them, 3 % more than that with 2.)
+constexpr float kLift = 11.0f, kReach = 15.9f;
 // From this size on, times scale, scores have too few places for that: weights are those of the differences from the largest score.
 constexpr float kFine = 65536.0f;
 constexpr float kNone = -3.402823466e38f;               // the logarithm of nothing

@@ -81,12 +81,52 @@ def test_decode_small_weights_behind_a_sink_in_one_workgroup(dtype, block, dim):
         close(decode(c, q, scale=gap / 32), gap, n, dim)
 
 
+def sink_prompt(n, at, dim):
+    k, v = torch.zeros(n + 1, 1, dim, dtype=torch.float16, device="cuda"), column(dim).half().expand(n + 1, 1, dim).contiguous()
+    k[at, 0, 0] = 4.0
+    v[at] = 0
+    return k, v
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("at", [0, 20011, N])
+@pytest.mark.parametrize("shared", [True, False])
+def test_prompt_small_weights_behind_a_sink(dim, at, shared):
+    """Keys of a tile of queries shared by several workgroups, and not."""
+    k, v = sink_prompt(N, at, dim)
+    q = sink_query(4, dim).expand(40, 4, dim).contiguous()
+    beside = [] if shared else EMPTY
+    for gap in (5.0, 10.0, 12.5, 14.0, 15.0, 16.0, 17.0, 18.0):
+        close(prompt(q, k, v, [40] + beside, [N + 1] + beside, scale=gap / 32, causal=False), gap, N, dim)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_prompt_small_weights_in_masked_tiles(dim):
+    """The sink is the last key that all queries see; the equal keys in front of it are seen in part by the window."""
+    n, gap = 3000, 14.0
+    k, v = sink_prompt(n, n, dim)
+    q = sink_query(2, dim).expand(64, 2, dim).contiguous()
+    k, v = torch.cat([k, torch.zeros_like(k[:63])]), torch.cat([v, v[:63]])
+    got = prompt(q, k, v, [64], [n + 64], scale=gap / 32, window=2000)
+    for i in range(64):                                                  # query i sees the 2000 keys up to n + i, the sink among them
+        close(got[i], gap, 1999, dim)
+
+
 @pytest.mark.parametrize("below", [20, 24, 27, 28, 30])
 def test_decode_weights_that_are_powers_of_two(below):
     """A million keys a power of two below the sink."""
     n, dim, ln2 = 1 << 20, 64, math.log(2.0)
     for at in (0, n):
         close(decode(sink_cache(n, at, dim, FP16, 1), sink_query(2, dim), scale=below * ln2 / 32), below * ln2, n, dim)
+
+
+@pytest.mark.parametrize("below", [20, 24, 27, 28, 30])
+def test_prompt_weights_that_are_powers_of_two(below):
+    n, dim, ln2 = 1 << 20, 64, math.log(2.0)
+    for at in (0, n):
+        k, v = sink_prompt(n, at, dim)
+        for beside in ([], EMPTY):
+            close(prompt(sink_query(2, dim), k, v, [1] + beside, [n + 1] + beside, scale=below * ln2 / 32, causal=False), below * ln2, n, dim)
 
 
 @pytest.mark.parametrize("size", [100.0, 1000.0, 8000.0, 60000.0])
