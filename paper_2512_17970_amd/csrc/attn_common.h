@@ -87,6 +87,13 @@ int check_attn(const codegemm_attn_desc* d);                     // status
 CacheView cache_view(const codegemm_kv_cache& c);
 
 inline bool misaligned_ints(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) != 0; }
+// The scale of scores times log2(e).  From 1e25 on all are the same, as any difference of scores of fp16 times that leaves the smaller no weight; and no score
+// times that is infinite.
+inline float log2_scale(float scale)
+{
+    const double s = scale > 1e25f ? 1e25 : scale < -1e25f ? -1e25 : (double)scale;
+    return (float)(s * 1.4426950408889634);
+}
 // A launch has fewer than 2^32 threads.
 inline bool too_many(long long blocks, int threads) { return blocks * threads > 0xffffffffll; }
 // A row stride of 0 stands for dense rows of `dense` elements.

@@ -693,7 +693,7 @@ extern "C" int codegemm_attn_decode(const codegemm_kv_cache* cache, const codege
     p.q_stride = row_stride(desc->q_stride, desc->q_heads * desc->head_dim);
     p.out_stride = row_stride(desc->out_stride, desc->q_heads * desc->head_dim);
     p.window = desc->window;
-    p.scale = (float)(desc->scale * 1.4426950408889634);
+    p.scale = log2_scale(desc->scale);
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (cache->dtype == CODEGEMM_KV_FP16) return launch_decode_of<CODEGEMM_KV_FP16>(p, plan.narrow, plan.groups, s);
     if (cache->dtype == CODEGEMM_KV_INT8) return launch_decode_of<CODEGEMM_KV_INT8>(p, plan.narrow, plan.groups, s);

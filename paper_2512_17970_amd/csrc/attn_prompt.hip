@@ -683,7 +683,7 @@ extern "C" int codegemm_attn_prompt(const codegemm_attn_desc* desc, const void* 
     p.causal = d.flags & CODEGEMM_ATTN_CAUSAL;
     p.negate = d.scale < 0.0f;
     const float size = d.scale < 0.0f ? -d.scale : d.scale;
-    p.scale = (float)((size > 1e-30f ? size : 1e-30f) * 1.4426950408889634);      // not 0: 0 times an infinite score is no number
+    p.scale = log2_scale(size > 1e-30f ? size : 1e-30f);           // not 0: 0 times an infinite score is no number
     p.unit = 1.0f / p.scale;
     p.splits = plan.splits;
     p.counters = static_cast<uint32_t*>(workspace);

@@ -161,3 +161,23 @@ def test_scores_beyond_all_fractions(size, sign, dim):
         c.place(c.v, 0, t, True).copy_(v[t])
     got = decode(c, q, scale=scale)
     assert torch.equal(got, want.expand_as(got)), "decode"
+
+
+@pytest.mark.parametrize("scale", [3.4e38, 1e30, 1e20, -1e30, -3.4e38])
+@pytest.mark.parametrize("dtype,block,dim", [(FP16, 1, 64), (INT8, 16, 128), (FP8, 1, 256)])
+def test_any_finite_scale(scale, dtype, block, dim):
+    """The largest score (of a negative scale, the smallest) has all the weight."""
+    n, heads = 300, 4
+    c = Cache([n], heads=1, dim=dim, page=64, dtype=dtype, block=block, seed=5)
+    k, v = (torch.stack([c.read(0, t, values) for t in range(n)]) for values in (False, True))
+    q = (torch.randn(1, heads, dim, generator=torch.Generator().manual_seed(3)) * 2).half().cuda()
+    scores = q[0].double() @ k[:, 0].t() * math.copysign(1, scale)
+    first, second = scores.topk(2, dim=1).values.unbind(1)
+    assert float((first - second).min()) > 1e-3 * float(scores.abs().max())
+    want = v[scores.argmax(dim=1), 0]
+    got = decode(c, q, scale=scale)[0].double()
+    assert bool(((got - want).abs() <= 2.0 ** -10 * want.abs() + 2.0 ** -25).all()), "decode"      # the rounding of a weight with its scale, and the result's
+    if dtype == FP16:
+        for beside in ([], EMPTY):
+            got = prompt(q, k.half(), v.half(), [1] + beside, [n] + beside, scale=scale, causal=False)
+            assert torch.equal(got[0].double(), want), "prompt"
