@@ -33,10 +33,14 @@ def ablate_lib(mask: int) -> str:
     return os.path.join(PKG, f"libcodegemm_ablate_{mask}.so")
 
 
+def can_build_calls() -> bool:
+    return shutil.which("g++") is not None and os.path.exists(os.path.join(sysconfig.get_paths()["include"], "Python.h"))
+
+
 def build_calls(verbose: bool = False) -> str:
     """The extension; without a C++ compiler or Python's headers there is none, and the binding makes its calls through ctypes."""
     include = sysconfig.get_paths()["include"]
-    if not shutil.which("g++") or not os.path.exists(os.path.join(include, "Python.h")):
+    if not can_build_calls():
         print(f"no g++ or no {include}/Python.h: built without {os.path.basename(CALLS)}", flush=True)
         return ""
     cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-Wall", "-Wno-missing-field-initializers", "-I", os.path.join(ROOT, "include"),
