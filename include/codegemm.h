@@ -323,7 +323,8 @@ int codegemm_dequant_gemm(const codegemm_desc *desc, const void *x, const uint8_
  * largest value 448), scale_block consecutive tokens of a page sharing a scale.
  * Places that hold no token of a sequence may hold anything, NaN too.
  * Arrays of int32 (page_table, kv_lens, cu_*, first) need 4-byte alignment, all else
- * 16.  Calls with 2^32 threads and more are refused (CODEGEMM_UNSUPPORTED).
+ * 16.  Calls whose launch has 2^32 threads and more in a dimension are refused
+ * (CODEGEMM_UNSUPPORTED); codegemm_kv_gather's has one for keys and one for values.
  * A page number outside 0..num_pages-1 stands for no page: nothing is written
  * there, and its tokens are not attended to and read as zeros.  The same holds for
  * positions from max_pages * page_size on.

@@ -94,7 +94,7 @@ inline float log2_scale(float scale)
     const double s = scale > 1e25f ? 1e25 : scale < -1e25f ? -1e25 : (double)scale;
     return (float)(s * 1.4426950408889634);
 }
-// A launch has fewer than 2^32 threads.
+// A launch has fewer than 2^32 threads in a dimension.
 inline bool too_many(long long blocks, int threads) { return blocks * threads > 0xffffffffll; }
 // A row stride of 0 stands for dense rows of `dense` elements.
 inline int row_stride(int stride, int dense) { return stride ? stride : dense; }
