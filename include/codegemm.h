@@ -428,7 +428,7 @@ typedef struct codegemm_attn_desc {
                                 /* how keys are split; longer ones are right all the same               */
     int32_t window;             /* 0, or keys that a query sees: the last `window` up to its position   */
     int32_t flags;              /* CODEGEMM_ATTN_*                                                      */
-    float scale;                /* of the scores, finite (usually 1 / sqrt(D))                          */
+    float scale;                /* of the scores, finite (usually 1 / sqrt(D)); from 1e25 on as 1e25    */
     int32_t q_stride, k_stride, v_stride, out_stride;   /* elements between tokens, multiples of 8 up   */
                                                         /* to 2^20; 0: heads * head_dim                 */
 } codegemm_attn_desc;

@@ -56,7 +56,7 @@ __device__ __forceinline__ int last_at_most(int n, int x, First first)
 }
 
 // What workgroups hand to each other: device-scope accesses of 16 (8) bytes, `at` bytes from the base of `parts`.  (By 8-byte atomics, single tokens
-// after 8000, 32 pieces, took 18.0 us, so 15.0; 512 queries behind 8000 keys 66.5, so 60.5.)
+// after 8000, 32 pieces, took 18.0 us, so 15.0.)
 constexpr int kDeviceScope = 16;            // the cache policy bit that device-scope atomics have (sc1)
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t parts_of(float* base) { return __builtin_amdgcn_make_buffer_rsrc(base, 0, 0x7fffffff, 0x00020000); }
 __device__ __forceinline__ void put16(__amdgpu_buffer_rsrc_t parts, int at, const float4_t& x)

@@ -4,7 +4,7 @@
 // and cut the items into pieces such that each has about one, whatever the lengths are; the last workgroup of an item to finish joins its
 // pieces.
 //
-// Each wavefront works on its own on every fourth step: scores as S^T = K Q^T on the matrix cores (rows: tokens, columns: query heads),
+// Each wavefront works on its own on every NW-th step (of 8, 4 or 2 wavefronts): scores as S^T = K Q^T on the matrix cores (rows: tokens, columns: query heads),
 // the softmax's running maximum and sum per column, and O^T += V^T P^T.  The right operand of the second product is what the score tiles
 // leave in the lanes, because a step's tokens are dealt out to the four lane groups g in runs of 8: row 4 g + r of score tile n is
 // token 8 g + 4 n + r, so lane group g holds 8 consecutive tokens of P^T, and the value pool has them next to each other for every
@@ -15,8 +15,11 @@
 // Bound by: the cache's bytes, where there are many.  32 sequences of 206 376 tokens, 64 and 8 heads of 128, 8 bits: 82 us, 5.2 TB/s; 3 of 240 551,
 // fp8: 86 us, 5.7 TB/s (a large copy: 4.85, read and written); loads that nothing is computed with take 81 and 87.  13 of twenty heads of 64 in fp16
 // with a window of 1500: 22.5 us, 4.0 TB/s.  Steps held in registers instead of LDS took 93 and 136 us at best.
-// Shortest: 700 tokens of one sequence, 10.2 us, of which 6.3 are one step of every wavefront (of 100 tokens) and 4 the exchange between workgroups;
-// three steps in one workgroup take 11.3.  8000 tokens: 15.0.
+// Shortest: 700 tokens of one sequence, 10.3 us, of which 6.3 are one step of every wavefront (of 100 tokens) and 4 the exchange between workgroups;
+// three steps in one workgroup take 11.3.  8000 tokens: 15.2.
+// Farthest from the bytes: long sequences with few key heads, whose pieces are as many as there are workgroups and are added up by one of them, 8 at a time:
+// 100 000 tokens with 8, 2 and 1 key heads take 45.7, 33.2 and 44.0 us for 205, 51 and 26 MB, 32 000 tokens 23.6, 26.6 and 25.7.
+// Heads of 80 are worked on as 128: 32 sequences of 206 376 tokens take 70 us for 265 MB, 3.8 TB/s; of 256, one wavefront a SIMD: 240 us for 848 MB, 3.5 TB/s.
 #include <cmath>
 #include <type_traits>
 

@@ -18,9 +18,13 @@
 // Why 32 rows a wavefront and four of those: S^T and O^T of 32 rows and 128 dimensions take 96 registers, Q^T and the weights 48, which
 // leaves room for two wavefronts on a SIMD; two workgroups on a compute unit fill each other's waits (one of 8 wavefronts: 1134 for 1117 us, of 2:
 // 1634), and 128 rows share a tile of keys and values in LDS.
-// Bound by: power, where sequences are long.  8192 causal queries, 64 and 8 heads of 128: 1140 to 1190 us from card to card, 0.92 to 0.96 PFLOP/s (a
-// library product of 8192^3 reaches 1.12), the matrix cores busy in 53 % of the cycles at 1.7 GHz; all zeros take 943 us.  Of ragged
-// prompts of 500 to 1100 tokens, 32 and 8 heads: 69 to 72 us, 0.65 to 0.68 PFLOP/s; a tile of rows costs some 7 us besides its keys.
+// Bound by: power, where sequences are long.  8192 causal queries, 64 and 8 heads of 128: 1095 to 1180 us from card to card, 0.93 to 1.00 PFLOP/s (a
+// library product of 8192^3 reaches 1.12; launches apart from each other, under a tracer, take up to 1270), the matrix cores busy in 52 % of the cycles at
+// 1.7 GHz; all zeros take 943 us.  Of ragged prompts of 500 to 1100 tokens, 32 and 8 heads: 69 to 76 us, 0.61 to 0.68 PFLOP/s; a tile of rows costs
+// some 7 us besides its keys.
+// Heads of 64: 640 to 680 us for 8192 queries of 64 heads, 0.81 to 0.86 PFLOP/s, 49 us for 4 x 2048 of 32, 0.52 (as many vector instructions a score as
+// for 128, for half the products).  Of 256: 3.10 ms and 0.71 PFLOP/s, 118 us for 4 x 2048 of 16, 0.43: one wavefront a SIMD, which has 512 registers
+// and spills 7.  Of 80, worked on as 128: 71 us for 4 x 2048 of 32, 0.45.
 #include "attn_common.h"
 
 namespace cg {
@@ -44,7 +48,7 @@ struct PromptParams {
 
 // Where there are fewer than kPromptItems tiles of queries and heads, as many workgroups as run at once share the keys of each, and the last of them
 // to end adds the parts up, in order.  A tile of keys takes about twice what adding a part does, so that sqrt(2 tiles) parts are best, of kLeastTiles
-// at least: 16 queries behind 8000 keys, 64 heads: 90 us in one, 30 in 32 parts, 26 in 16; a prompt of 953, 7 heads: 19.3 in parts
+// at least: 16 queries behind 8000 keys, 64 and 8 heads: 162 us in one, 38 in 32 parts, 31 in 16; a prompt of 953, 7 heads: 19.3 in parts
 // of 8 tiles, 17.5 of 3.
 constexpr int kPromptItems = 256, kLeastTiles = 3;
 constexpr int prompt_groups(int dp) { return dp == 256 ? 256 : 512; }        // that run at once

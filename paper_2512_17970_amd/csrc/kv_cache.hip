@@ -2,8 +2,9 @@
 //
 // Append: a team of 128 threads takes the queries of a token, a workgroup the keys (or values) of one head for the tokens that share a scale, so
 // that their largest |x| stays within it; a lane has 16 elements of a row, those that turn with each other, so that rotation needs no exchange and the norm a few.
-// Bound by the bytes: 8446 tokens, 64 and 8 heads of 128, 8 bits: 73 us for 346 MB, 4.7 TB/s; by launch and dependent loads where there are few: one
-// token of 32 heads 3.6 us, 32 sequences' 5.7 (lengths, page, old scale, tokens).
+// Bound by the bytes: 8446 tokens, 64 and 8 heads of 128, 8 bits: 73 us for 346 MB, 4.7 TB/s; by the launch and loads one after the other where there are few: one
+// token of 32 heads 3.7 us, 32 sequences' 5.8 (lengths, page, old scale; tokens too are asked for after those, which they do not depend on), 7.0 where
+// blocks get larger scales and the codes in them are converted.
 // Gather: a workgroup takes 16 tokens of one head, values by way of LDS, which turns them.  30087 tokens of 8 heads, 8 bits: 30 to 33 us for
 // 185 MB, 5.6 to 6.2 TB/s.
 #include "attn_common.h"
