@@ -181,3 +181,36 @@ def test_any_finite_scale(scale, dtype, block, dim):
         for beside in ([], EMPTY):
             got = prompt(q, k.half(), v.half(), [1] + beside, [n] + beside, scale=scale, causal=False)
             assert torch.equal(got[0].double(), want), "prompt"
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("window", [0, 300])
+def test_rows_of_all_sizes_beside_each_other(dim, window):
+    """Queries whose scores are of sizes from 0.01 to some millions lie in one tile, and each is right for itself.  With p the weights and o the result in 64 bits,
+    weights that are off by a factor of up to 1 + d each change it by 2 d / (1 - d) sum p |v - o| at most; d: a score's error, (D + 4) 2^-24 of its products'
+    sizes, a weight's rounding and its exponential's.  Sums in 32 bits add (n + 64) 2^-24 sum p |v|, weights under 2^-34 of the largest n 2^-33 max |v|."""
+    n, heads = 900, 2
+    g = torch.Generator().manual_seed(dim + window)
+    size = 10.0 ** (torch.arange(n * heads) % 9 - 4).view(n, heads, 1)
+    k, v = ((torch.randn(n, 1, dim, generator=g) * s).half().cuda() for s in (100.0, 1.0))
+    q = (torch.randn(n, heads, dim, generator=g) * size).half().cuda()
+    scale = dim ** -0.5
+    got = [prompt(q, k, v, [n] + beside, [n] + beside, scale=scale, window=window).double() for beside in ([], EMPTY)]
+    key, at = torch.arange(n, device="cuda"), torch.arange(n, device="cuda")[:, None]
+    seen, values = (key <= at) & ((key > at - window) if window else True), v[:, 0].double()
+    for h in range(heads):
+        s = (q[:, h].double() @ k[:, 0].double().t() * scale).masked_fill(~seen, -math.inf)
+        error = (dim + 4) * 2.0 ** -24 * (scale * q[:, h].double().abs() @ k[:, 0].double().abs().t()).masked_fill(~seen, 0).amax(1)
+        p = torch.softmax(s, dim=1)
+        want = p @ values
+        spread = torch.cat([(p[i:i + 50, :, None] * (values[None] - want[i:i + 50, None]).abs()).sum(1) for i in range(0, n, 50)])
+        known = error < 0.1                                                # .. where 32 bits say something of a score's fraction
+        d = (torch.expm1(error) + 2.0 ** -11 + 2.0 ** -16)[:, None]
+        bound_ = 2 * d / (1 - d) * spread + (n + 64) * 2.0 ** -24 * (p @ values.abs()) + n * 2.0 ** -33 * values.abs().max() + 2.0 ** -11 * want.abs() + 2.0 ** -25
+        first, second = s[1:].topk(2, dim=1).values.unbind(1)
+        alone = torch.cat([torch.ones(1, dtype=torch.bool, device="cuda"), first - second > 40 + 4 * error[1:]])
+        assert int(known.sum()) > n / 2 and int((alone & ~known).sum()) > n / 4
+        for out in got:
+            bad = (((out[:, h] - want).abs() > 1.01 * bound_) & known[:, None]).any(1)
+            assert not bool(bad.any()), f"head {h}: rows {bad.nonzero()[:8, 0].tolist()}"
+            assert torch.equal(out[alone, h], values[s.argmax(1)[alone]]), "rows of one key"
