@@ -321,6 +321,18 @@ int codegemm_dequant_gemm(const codegemm_desc *desc, const void *x, const uint8_
  * A cached value is its element for CODEGEMM_KV_FP16 and element * scale for
  * CODEGEMM_KV_INT8 (-127..127) and CODEGEMM_KV_FP8 (e4m3: 3 bits of mantissa,
  * largest value 448), scale_block consecutive tokens of a page sharing a scale.
+ * CODEGEMM_KV_INT4 has codes of 4 bits (0..15) and, for every token, a scale and an
+ * offset (fp16) for each run of scale_block dimensions of a head (R runs, R =
+ * ceil(head_dim / scale_block), the last one perhaps shorter): a cached value is
+ * (code + 16) * scale + offset, rounded once to fp16.  head_dim is a multiple of 32.
+ * Eight codes are a 32-bit word, little-endian, code j of them in bits
+ * 4 (j / 2) + 16 (j % 2) and the three above: of keys eight dimensions of a token,
+ * of values eight tokens of a dimension.
+ *     k         [num_pages][kv_heads][page_size][head_dim/8] words
+ *     v         [num_pages][kv_heads][page_size/16][head_dim][2] words
+ *     k_scales  [num_pages][kv_heads][page_size][R][2] fp16: scale, offset
+ *     v_scales  [num_pages][kv_heads][page_size/16][R][2][16] fp16: 16 tokens' scales, then
+ *               their offsets
  * Places that hold no token of a sequence may hold anything, NaN too.
  * Arrays of int32 (page_table, kv_lens, cu_*, first) need 4-byte alignment, all else
  * 16.  Calls whose launch has 2^32 threads and more in a dimension are refused
@@ -332,7 +344,8 @@ int codegemm_dequant_gemm(const codegemm_desc *desc, const void *x, const uint8_
 enum {
     CODEGEMM_KV_FP16 = 0,
     CODEGEMM_KV_INT8 = 1,
-    CODEGEMM_KV_FP8 = 2
+    CODEGEMM_KV_FP8 = 2,
+    CODEGEMM_KV_INT4 = 4
 };
 
 typedef struct codegemm_kv_cache {
@@ -342,11 +355,13 @@ typedef struct codegemm_kv_cache {
     int32_t page_size;          /* tokens: 16, 32, 64, 128 or 256                  */
     int32_t dtype;              /* CODEGEMM_KV_*                                   */
     int32_t scale_block;        /* tokens that share a scale: 1, 2, 4 .. page_size */
-                                /* (not read for CODEGEMM_KV_FP16)                 */
+                                /* (not read for CODEGEMM_KV_FP16); for            */
+                                /* CODEGEMM_KV_INT4 dimensions of a token that     */
+                                /* do: 32, 64, 128 or 256                          */
     int32_t num_seqs;           /* rows of page_table, 1..65535                    */
     int32_t max_pages;          /* entries of a row, max_pages * page_size <= 2^30 */
     void *k, *v;                /* device */
-    float *k_scales, *v_scales; /* device; NULL for CODEGEMM_KV_FP16 */
+    float *k_scales, *v_scales; /* device; NULL for CODEGEMM_KV_FP16; CODEGEMM_KV_INT4: fp16 pairs behind the same pointers */
     const int32_t *page_table;  /* device, [num_seqs][max_pages] */
     const int32_t *kv_lens;     /* device, [num_seqs]: tokens of each sequence, those of this step among them */
 } codegemm_kv_cache;
@@ -395,11 +410,27 @@ typedef struct codegemm_append_desc {
  *     have; where it is above, their codes c become round(c * s_old / s).  A block
  *     whose first token is new starts afresh.  A block that gets a NaN or an
  *     infinity has a NaN scale from then on: all its values read as NaN.
+ *     CODEGEMM_KV_INT4: of every run of a token, scale = fp16((max - min) (1 - 2^-11) / 15),
+ *     which is no more than a 15th of the range, offset = fp16(min - 16 scale) and the codes
+ *     round((x - offset) / scale - 16), not outside 0..15 (scale 0: codes 0).  Values
+ *     beyond +-20000 are held as that; a run with a NaN or an infinity reads as NaN.
  */
 int codegemm_kv_append(const codegemm_kv_cache *cache, const codegemm_append_desc *desc,
                        const int32_t *cu_seqlens, const void *q, const void *k, const void *v,
                        const void *q_norm, const void *k_norm, const float *rope,
                        void *q_out, void *k_out, void *stream);
+
+/*
+ * codegemm_kv_append where tokens have left the cache (codegemm_kv_evict): the new tokens
+ * of sequence i turn as at position kv_lens[i] - n_i + j + shift[i], shift [num_seqs] int32
+ * being the tokens that are gone; they lie in the cache where codegemm_kv_append puts them.
+ * Positions below 0 take the rope table's first row.  shift NULL: codegemm_kv_append.
+ */
+int codegemm_kv_append_shifted(const codegemm_kv_cache *cache, const codegemm_append_desc *desc,
+                               const int32_t *cu_seqlens, const int32_t *shift, const void *q,
+                               const void *k, const void *v, const void *q_norm,
+                               const void *k_norm, const float *rope, void *q_out, void *k_out,
+                               void *stream);
 
 /*
  * Cached keys and values as contiguous fp16: rows cu_rows[i] .. cu_rows[i+1]-1 of

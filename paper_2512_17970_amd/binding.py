@@ -25,7 +25,7 @@ _lib: Optional[ctypes.CDLL] = None
 
 FLAG_Y_FP32 = 1
 PSUM_FP32, PSUM_FP16 = 0, 1
-KV_FP16, KV_INT8, KV_FP8 = 0, 1, 2
+KV_FP16, KV_INT8, KV_FP8, KV_INT4 = 0, 1, 2, 4
 ROPE_INTERLEAVED = 1
 ATTN_CAUSAL = 1
 
@@ -37,7 +37,7 @@ EXPORTS = [
     "codegemm_psumbook_build", "codegemm_gemm", "codegemm_dequant_gemm", "codegemm_status_string",
     "codegemm_gemm_static", "codegemm_static_workspace_limit",
     "codegemm_gemm_grouped", "codegemm_grouped_workspace_bytes",
-    "codegemm_kv_pool_bytes", "codegemm_kv_scales_bytes", "codegemm_kv_append", "codegemm_kv_gather",
+    "codegemm_kv_pool_bytes", "codegemm_kv_scales_bytes", "codegemm_kv_append", "codegemm_kv_append_shifted", "codegemm_kv_gather",
     "codegemm_attn_decode", "codegemm_attn_decode_workspace_bytes", "codegemm_attn_prompt", "codegemm_attn_prompt_workspace_bytes",
 ]
 
@@ -192,6 +192,8 @@ def load() -> ctypes.CDLL:
         getattr(lib, name).restype = sz
     lib.codegemm_kv_append.argtypes = [cp, ap, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
     lib.codegemm_kv_append.restype = i
+    lib.codegemm_kv_append_shifted.argtypes = [cp, ap, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.codegemm_kv_append_shifted.restype = i
     lib.codegemm_kv_gather.argtypes = [cp, i32, vp, vp, vp, vp, vp]
     lib.codegemm_kv_gather.restype = i
     lib.codegemm_attn_decode_workspace_bytes.argtypes = [cp, tp]
@@ -355,6 +357,11 @@ def codegemm_kv_scales_bytes(cache: KvCache) -> int:
 def _kv_append(cache: KvCache, desc: AppendDesc, cu_seqlens, q, k, v, q_norm, k_norm, rope, q_out, k_out, stream: int = 0) -> None:
     _check(load().codegemm_kv_append(ctypes.byref(cache), ctypes.byref(desc), _ptr(cu_seqlens), _ptr(q), _ptr(k), _ptr(v), _ptr(q_norm),
                                      _ptr(k_norm), _ptr(rope), _ptr(q_out), _ptr(k_out), stream), "codegemm_kv_append")
+
+
+def codegemm_kv_append_shifted(cache: KvCache, desc: AppendDesc, cu_seqlens, shift, q, k, v, q_norm, k_norm, rope, q_out, k_out, stream: int = 0) -> None:
+    _check(load().codegemm_kv_append_shifted(ctypes.byref(cache), ctypes.byref(desc), _ptr(cu_seqlens), _ptr(shift), _ptr(q), _ptr(k), _ptr(v), _ptr(q_norm),
+                                             _ptr(k_norm), _ptr(rope), _ptr(q_out), _ptr(k_out), stream), "codegemm_kv_append_shifted")
 
 
 def _kv_gather(cache: KvCache, rows: int, cu_rows, first, k_out, v_out, stream: int = 0) -> None:

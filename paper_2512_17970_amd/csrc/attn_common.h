@@ -22,6 +22,8 @@ struct CacheView {
     int Hk, D, pages, max_pages, seqs;
     int page_shift;      // log2 of the page size
     int block_shift;     // log2 of the tokens that share a scale
+    int run_shift;       // 4 bits: log2 of the dimensions that share a token's scale and offset,
+    int runs;            // .. and how many such runs a head has
 };
 
 // Page of a position's page index, or -1.
@@ -81,6 +83,50 @@ __device__ __forceinline__ Pair get8(__amdgpu_buffer_rsrc_t parts, int at)
     const uint32_t a = w[0], b = w[1];
     return Pair{__builtin_bit_cast(float, a), __builtin_bit_cast(float, b)};
 }
+
+// 4 bits: eight codes of a word, code j in bits 4 (j / 2) + 16 (j % 2), so that shifts by whole words and one mask leave consecutive codes in the two
+// halves, at the place of the four leading mantissa bits: with the exponent of 16 that is 16 + code in fp16, and one packed multiply-add makes the values.
+__device__ __forceinline__ half2_t code_pair(uint32_t w, int i)
+{
+    const uint32_t at = i == 0 ? w << 6 : i == 1 ? w << 2 : i == 2 ? w >> 2 : w >> 6;
+    return __builtin_bit_cast(half2_t, (at & 0x03c003c0u) | 0x4c004c00u);
+}
+__device__ __forceinline__ half2_t halves_of(uint32_t w) { return __builtin_bit_cast(half2_t, w); }
+__device__ __forceinline__ half2_t both_low(uint32_t w) { return halves_of(__builtin_amdgcn_perm(w, w, 0x01000100u)); }
+__device__ __forceinline__ half2_t both_high(uint32_t w) { return halves_of(__builtin_amdgcn_perm(w, w, 0x03020302u)); }
+// .. of one scale and offset (a key's run of dimensions)
+__device__ __forceinline__ half8_t four_bits(uint32_t w, half2_t scale, half2_t offset)
+{
+    half8_t x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const half2_t y = __builtin_elementwise_fma(code_pair(w, i), scale, offset);
+        x[2 * i] = y[0];
+        x[2 * i + 1] = y[1];
+    }
+    return x;
+}
+// .. of eight (values of eight tokens)
+__device__ __forceinline__ half8_t four_bits(uint32_t w, const u32x4_t& scale, const u32x4_t& offset)
+{
+    half8_t x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const half2_t y = __builtin_elementwise_fma(code_pair(w, i), halves_of(scale[i]), halves_of(offset[i]));
+        x[2 * i] = y[0];
+        x[2 * i + 1] = y[1];
+    }
+    return x;
+}
+// The 8 dimensions that lane group g (of 16 lanes) has of a key in the i-th product of 32 dimensions, as one or two loads of 16 bytes leave them; heads are
+// worked on as DP dimensions.
+template <int TYPE, int DP>
+__device__ __forceinline__ constexpr int operand_dim(int i, int g)
+{
+    return TYPE != CODEGEMM_KV_INT4 || DP < 128 ? 64 * (i / 2) + 16 * g + 8 * (i % 2) : 128 * (i / 4) + 32 * g + 8 * (i % 4);
+}
+// First scale-and-offset word of a token's keys (of 16 tokens' values) at slot `slot`, a multiple of 16 for values: as many for both.
+__device__ __forceinline__ size_t runs_at(const CacheView& c, int page, int head, int slot) { return ((((size_t)page * c.Hk + head) << c.page_shift) + slot) * (size_t)c.runs; }
 
 int check_cache(const codegemm_kv_cache* c, bool pointers);     // status
 int check_attn(const codegemm_attn_desc* d);                     // status

@@ -76,6 +76,7 @@ __device__ __forceinline__ half8_t codes_to_half(uint32_t lo, uint32_t hi)
 
 typedef __attribute__((address_space(3))) u32x4_t lds_words4;
 typedef __attribute__((address_space(3))) u32x2_t lds_words2;
+typedef __attribute__((address_space(3))) uint32_t lds_word;
 typedef __attribute__((address_space(3))) float4_t lds_float4;
 typedef __attribute__((address_space(3))) float lds_float1;
 typedef __attribute__((address_space(4))) const int32_t const_int;
@@ -83,21 +84,24 @@ typedef __attribute__((address_space(4))) const int32_t const_int;
 // A step in LDS, per wavefront: keys, values, the tokens' scales.  A workgroup has a compute unit to itself, or, NARROW, half of one.
 template <int TYPE, int DP, bool NARROW>
 struct DecodeStep {
-    static constexpr bool kHalf = TYPE == CODEGEMM_KV_FP16;
+    static constexpr bool kHalf = TYPE == CODEGEMM_KV_FP16, kFour = TYPE == CODEGEMM_KV_INT4;
+    static constexpr bool kScaled = !kHalf && !kFour;                // scales go to scores and weights
     static constexpr int kSize = kHalf ? 2 : 1;
     static constexpr int kTokens = 32, kRun = 8, kTiles = 2;
-    static constexpr int kPart = kTokens * DP * kSize;               // bytes of the keys, and of the values
-    static constexpr int kScaleBytes = kHalf ? 0 : 256;              // [keys, values][32] fp32
+    static constexpr int kPart = kTokens * DP * kSize / (kFour ? 2 : 1);       // bytes of the keys, and of the values
+    static constexpr int kRuns = DP / 32;                            // 4 bits: scales and offsets of a token, at most
+    static constexpr int kRunBytes = 64 * kRuns;                     // .. of 16 tokens
+    static constexpr int kScaleBytes = kHalf ? 0 : !kFour ? 256 : DP == 256 ? 2048 : 1024;     // [keys, values][32] fp32; [keys, values][2][kRunBytes], and some more
     static constexpr int kBytes = 2 * kPart + kScaleBytes;
-    static constexpr int kRequests = 2 * kPart / 1024 + (kHalf ? 0 : 1);
+    static constexpr int kRequests = 2 * kPart / 1024 + (kHalf ? 0 : kFour ? kScaleBytes / 1024 : 1);
     static constexpr int kStages = 2;
     static constexpr int kPerCu = NARROW && kBytes <= 20 * 1024 ? 2 : 1;
-    static constexpr int kWaves = (kBytes > 20 * 1024 ? 2 : kBytes > 10 * 1024 ? 4 : 8) / kPerCu;
+    static constexpr int kWaves = (kBytes > 20 * 1024 ? 2 : kBytes > 9 * 1024 ? 4 : 8) / kPerCu;
     static constexpr int kRing = kWaves * kStages * kBytes;
     static constexpr int kSums = kWaves * kDecodeRows * 8;           // the wavefronts' maxima and weights
     static constexpr int kLds = kRing + kSums + 16;
     static constexpr int kBlocks = DP / 16 / kWaves > 0 ? DP / 16 / kWaves : 1;    // of 16 dimensions that a wavefront sums up in the end
-    static_assert(kBytes >= kDecodeRows * DP * 4, "a wavefront's sums fit into a stage");
+    static_assert(kStages * kBytes >= kDecodeRows * DP * 4, "a wavefront's sums fit into its part of the ring");
 };
 
 // The sum of the values up to the lane's own; all lanes' in the last lane.
@@ -218,8 +222,12 @@ attn_decode_kernel(const DecodeParams p)
     // where the lane's own operands lie in a stage
     const uint32_t ring = lds0 + (uint32_t)(wave * T::kStages * T::kBytes);
     const uint32_t k_read = ring + lane * 16;
-    const uint32_t v_read = T::kHalf ? k_read + T::kPart : ring + T::kPart + (uint32_t)((g >> 1) * 512 + col * 16 + (g & 1) * 8);
-    const uint32_t s_read = ring + 2 * T::kPart + g * 32;
+    const uint32_t v_read = T::kHalf ? k_read + T::kPart
+                          : T::kFour ? ring + T::kPart + (uint32_t)((g >> 1) * DP * 8 + col * 8 + (g & 1) * 4)
+                                     : ring + T::kPart + (uint32_t)((g >> 1) * 512 + col * 16 + (g & 1) * 8);
+    // .. its scales; 4 bits: those of its token's keys (tile 0), and of its 8 tokens' values
+    const uint32_t s_read = ring + 2 * T::kPart + (T::kFour ? (uint32_t)((col >> 3) * T::kRunBytes + (8 * ((col >> 2) & 1) + (col & 3)) * cv.runs * 4) : (uint32_t)(g * 32));
+    const uint32_t vs_read = ring + 2 * T::kPart + (uint32_t)((2 + (g >> 1)) * T::kRunBytes + (g & 1) * 16);
 
     for (unsigned piece = blockIdx.x;; piece += groups) {
         // Its sequence and item, and steps begin .. s_end - 1: the k-th of the item's `parts`.
@@ -264,6 +272,35 @@ attn_decode_kernel(const DecodeParams p)
                 page[x] = pages[t >> cv.page_shift];
             }
         };
+        // 4 bits.  Keys: as below, lane (col, g) reads dimensions 128 j + 32 g .. + 31; heads of up to 64: a lane both tiles' half of a token.  Values: the
+        // groups of 16 tokens as they lie.  Scales and offsets: those of keys and of values, 16 tokens' at a time; lanes past the last read that again.
+        auto request_four = [&](uint32_t to, const unsigned char* const (&kp)[2], const unsigned char* const (&vp)[2], const float* const (&ks)[2], const float* const (&vs)[2]) {
+            const unsigned char* k = (col >= 8 ? kp[1] : kp[0]) + (8 * ((col >> 2) & 1) + (col & 3)) * (D / 2);
+            if constexpr (DP == 64) {
+                const int d = 32 * (g & 1);
+                request16(to, k + (4 * (g >> 1) * D + (EXACT || d < D ? d : 0)) / 2);
+            } else {
+#pragma unroll
+                for (int n = 0; n < T::kTiles; ++n)
+#pragma unroll
+                    for (int j = 0; j < DP / 128; ++j) {
+                        const int d = 128 * j + 32 * g;
+                        request16(to + (uint32_t)((n * (DP / 128) + j) * 1024), k + (4 * n * D + (EXACT || d < D ? d : 0)) / 2);
+                    }
+            }
+#pragma unroll
+            for (int i = 0; i < T::kPart / 1024; ++i) {
+                const int at = i * kWave + lane, x = at / (DP / 2), d = 2 * (at % (DP / 2));
+                request16(to + (uint32_t)(T::kPart + i * 1024), (x ? vp[1] : vp[0]) + (EXACT || d < D ? d : 0) * 8);
+            }
+            constexpr int kLanes = T::kRunBytes / 16;               // of 16 tokens' scales
+#pragma unroll
+            for (int i = 0; i < T::kScaleBytes / 1024; ++i) {
+                const int at = (i * kWave + lane) / kLanes & 3, word = 4 * (lane % kLanes), last = 16 * cv.runs - 4;
+                const float* s = at & 2 ? (at & 1 ? vs[1] : vs[0]) : (at & 1 ? ks[1] : ks[0]);
+                request16(to + (uint32_t)(2 * T::kPart + i * 1024), reinterpret_cast<const unsigned char*>(s + (word < last ? word : last)));
+            }
+        };
         // bit x: group x has a page
         auto request = [&](int step, int stage) {
             const unsigned char *kp[2], *vp[2];
@@ -276,14 +313,26 @@ attn_decode_kernel(const DecodeParams p)
                 const bool in = (unsigned)page[x] < (unsigned)cv.pages;
                 ok |= in ? 1 << x : 0;
                 const int pg = in ? page[x] : 0, slot = t & ((1 << cv.page_shift) - 1);
+                if constexpr (T::kFour) {
+                    const size_t at = (page_at(cv, pg, head) + (size_t)slot * D) / 2;
+                    kp[x] = cv.k + at;
+                    vp[x] = cv.v + at;
+                    ks[x] = cv.k_scales + runs_at(cv, pg, head, slot);
+                    vs[x] = cv.v_scales + runs_at(cv, pg, head, slot);
+                    continue;
+                }
                 kp[x] = cv.k + (page_at(cv, pg, head) + (size_t)slot * D) * T::kSize;
                 vp[x] = cv.v + (page_at(cv, pg, head) + (size_t)slot * D) * T::kSize;
-                if constexpr (!T::kHalf) {
+                if constexpr (T::kScaled) {
                     ks[x] = cv.k_scales + scales_at(cv, pg, head) + (slot >> cv.block_shift);
                     vs[x] = cv.v_scales + scales_at(cv, pg, head) + (slot >> cv.block_shift);
                 }
             }
             const uint32_t to = ring + (uint32_t)(stage * T::kBytes);
+            if constexpr (T::kFour) {
+                request_four(to, kp, vp, ks, vs);
+                return ok;
+            }
             // keys: lane (col, g) reads dimensions 64 j + 16 g .. + 15 of token 8 (col / 4) + 4 n + col % 4
             const unsigned char* k = (col >= 8 ? kp[1] : kp[0]) + (size_t)((8 * ((col >> 2) & 1) + (col & 3)) * D) * T::kSize;
 #pragma unroll
@@ -315,17 +364,15 @@ attn_decode_kernel(const DecodeParams p)
             return ok;
         };
 
-        // Q^T: column `col`, dimensions 64 j + 16 g + 8 a .. + 7 for products 2 j + a; zeros beyond the head's rows and dimensions.
+        // Q^T: column `col`, for product i the 8 dimensions that a lane has of a key; zeros beyond the head's rows and dimensions.
         half8_t qf[DP / 32];
 #pragma unroll
-        for (int j = 0; j < DP / 64; ++j)
-#pragma unroll
-            for (int a = 0; a < 2; ++a) {
-                half8_t w = {0, 0, 0, 0, 0, 0, 0, 0};
-                const int d = 64 * j + 16 * g + 8 * a;
-                if (col < rows && d < D) w = *reinterpret_cast<const half8_t*>(p.q + (size_t)seq * p.q_stride + (size_t)(head * p.r + row0 + col) * D + d);
-                qf[2 * j + a] = w;
-            }
+        for (int i = 0; i < DP / 32; ++i) {
+            half8_t w = {0, 0, 0, 0, 0, 0, 0, 0};
+            const int d = operand_dim<TYPE, DP>(i, g);
+            if (col < rows && d < D) w = *reinterpret_cast<const half8_t*>(p.q + (size_t)seq * p.q_stride + (size_t)(head * p.r + row0 + col) * D + d);
+            qf[i] = w;
+        }
 
         float4_t o[DP / 16];
 #pragma unroll
@@ -340,6 +387,32 @@ attn_decode_kernel(const DecodeParams p)
 #pragma unroll
             for (int n = 0; n < T::kTiles; ++n) {
                 s[n] = float4_t{0, 0, 0, 0};
+                if constexpr (T::kFour) {
+#pragma unroll
+                    for (int j = 0; j < (DP + 127) / 128; ++j) {
+                        constexpr int kEach = DP < 128 ? DP / 32 : 4;       // words of a lane
+                        const int d = DP < 128 ? 16 * g : 128 * j + 32 * g;
+                        const bool in = EXACT || d < D;
+                        const uint32_t so = *(const lds_word*)(uintptr_t)(s_read + off + (uint32_t)(4 * n * cv.runs * 4 + ((in ? d : 0) >> cv.run_shift) * 4));
+                        const half2_t scale = both_low(so), offset = both_high(so);
+                        uint32_t w[kEach];
+                        if constexpr (DP < 128) {
+                            const u32x2_t x = *(const lds_words2*)(uintptr_t)(ring + off + (uint32_t)(((2 * n + (g >> 1)) * 16 + col) * 16 + (g & 1) * 8));
+                            w[0] = x[0]; w[1] = x[1];
+                        } else {
+                            const u32x4_t x = *(const lds_words4*)(uintptr_t)(k_read + off + (uint32_t)((n * (DP / 128) + j) * 1024));
+#pragma unroll
+                            for (int a = 0; a < kEach; ++a) w[a] = x[a];
+                        }
+#pragma unroll
+                        for (int a = 0; a < kEach; ++a) {
+                            half8_t kf = four_bits(w[a], scale, offset);
+                            if (!EXACT && !in) kf = half8_t{0, 0, 0, 0, 0, 0, 0, 0};
+                            s[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[kEach * j + a], s[n], 0, 0, 0);
+                        }
+                    }
+                    continue;
+                }
 #pragma unroll
                 for (int j = 0; j < DP / 64; ++j) {
                     const bool in = EXACT || 64 * j + 16 * g < D;
@@ -367,7 +440,7 @@ attn_decode_kernel(const DecodeParams p)
             float4_t vs[T::kTiles];
 #pragma unroll
             for (int n = 0; n < T::kTiles; ++n) {
-                if constexpr (T::kHalf) s[n] *= p.scale;
+                if constexpr (!T::kScaled) s[n] *= p.scale;
                 else {
                     s[n] *= *(const lds_float4*)(uintptr_t)(s_read + off + (uint32_t)(16 * n)) * p.scale;
                     vs[n] = *(const lds_float4*)(uintptr_t)(s_read + off + (uint32_t)(128 + 16 * n));
@@ -380,18 +453,18 @@ attn_decode_kernel(const DecodeParams p)
                     for (int r = 0; r < 4; ++r) {
                         const bool seen = 4 * n + r >= vlo && 4 * n + r < vhi;
                         s[n][r] = seen ? s[n][r] : -INFINITY;
-                        if constexpr (!T::kHalf) vs[n][r] = seen ? vs[n][r] : 0.0f;
+                        if constexpr (T::kScaled) vs[n][r] = seen ? vs[n][r] : 0.0f;
                     }
             }
             // The maximum is taken over score + log2 of the value's scale, so that weight times scale, rounded to fp16, is at most 2^kLift.
             float most = -INFINITY;
-            if (T::kHalf || (whole && cv.block_shift >= 3)) {           // one scale for the run
+            if (!T::kScaled || (whole && cv.block_shift >= 3)) {           // one scale for the run
 #pragma unroll
                 for (int n = 0; n < T::kTiles; ++n)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) most = fmaxf(most, s[n][r]);
-                if constexpr (!T::kHalf) most += fmaxf(__builtin_amdgcn_logf(vs[0][0]), kLeastLog);
-            } else if constexpr (!T::kHalf) {
+                if constexpr (T::kScaled) most += fmaxf(__builtin_amdgcn_logf(vs[0][0]), kLeastLog);
+            } else if constexpr (T::kScaled) {
 #pragma unroll
                 for (int n = 0; n < T::kTiles; ++n)
 #pragma unroll
@@ -409,7 +482,7 @@ attn_decode_kernel(const DecodeParams p)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const float w = __builtin_amdgcn_exp2f(s[n][r] - base);
-                    pf[4 * n + r] = (_Float16)(T::kHalf ? w : w * vs[n][r]);
+                    pf[4 * n + r] = (_Float16)(T::kScaled ? w * vs[n][r] : w);
                     if constexpr (!T::kHalf) add += w;                   // (unrounded, as products have scales: off by 2^-11 at most)
                 }
             if constexpr (T::kHalf) {                                    // the sum of the weights as they are rounded
@@ -423,7 +496,7 @@ attn_decode_kernel(const DecodeParams p)
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
                     if (!(i >= vlo && i < vhi)) {
-                        if constexpr (T::kHalf) mask[i / 2] &= i & 1 ? 0x0000ffffu : 0xffff0000u;
+                        if constexpr (!T::kScaled) mask[i / 2] &= i & 1 ? 0x0000ffffu : 0xffff0000u;
                         else mask[i / 4] &= ~(0xffu << (8 * (i & 3)));
                     }
             }
@@ -433,10 +506,19 @@ attn_decode_kernel(const DecodeParams p)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) o[b][r] *= keep;
             }
+            u32x4_t scale4, offset4;                                     // 4 bits: of the 8 tokens and 32 dimensions; without either, a code is zero
 #pragma unroll
             for (int b = 0; b < DP / 16; ++b) {
                 half8_t vf;
-                if constexpr (T::kHalf) {
+                if constexpr (T::kFour) {
+                    if (b % 2 == 0) {
+                        const uint32_t at = vs_read + off + (uint32_t)(((EXACT || 16 * b < D ? 16 * b : 0) >> cv.run_shift) * 64);
+                        scale4 = *(const lds_words4*)(uintptr_t)at;
+                        offset4 = *(const lds_words4*)(uintptr_t)(at + 32);
+                        if (!whole) { scale4 &= mask; offset4 &= mask; }
+                    }
+                    vf = four_bits(*(const lds_word*)(uintptr_t)(v_read + off + (uint32_t)(b * 128)), scale4, offset4);
+                } else if constexpr (T::kHalf) {
                     u32x4_t w = *(const lds_words4*)(uintptr_t)(v_read + off + (uint32_t)(b * 1024));
                     if (!whole) w &= mask;
                     vf = __builtin_bit_cast(half8_t, w);
@@ -700,5 +782,6 @@ extern "C" int codegemm_attn_decode(const codegemm_kv_cache* cache, const codege
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (cache->dtype == CODEGEMM_KV_FP16) return launch_decode_of<CODEGEMM_KV_FP16>(p, plan.narrow, plan.groups, s);
     if (cache->dtype == CODEGEMM_KV_INT8) return launch_decode_of<CODEGEMM_KV_INT8>(p, plan.narrow, plan.groups, s);
+    if (cache->dtype == CODEGEMM_KV_INT4) return launch_decode_of<CODEGEMM_KV_INT4>(p, plan.narrow, plan.groups, s);
     return launch_decode_of<CODEGEMM_KV_FP8>(p, plan.narrow, plan.groups, s);
 }

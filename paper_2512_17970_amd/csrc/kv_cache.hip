@@ -18,7 +18,7 @@ constexpr int kLastEnd = 0x7ffffe00;        // a length past every table, from w
 
 struct AppendParams {
     CacheView c;
-    const int32_t* cu;
+    const int32_t *cu, *shift;
     const _Float16 *q, *k, *v, *q_norm, *k_norm;
     const float* rope;
     _Float16 *q_out, *k_out;
@@ -87,9 +87,15 @@ struct Turn {
     float cs[16];       // cos and sin of the lane's 8 pairs
 };
 
-__device__ __forceinline__ Turn load_turn(const AppendParams& p, int position, int c)
+// Of a place in a sequence that `gone` tokens have left.
+__device__ __forceinline__ Turn load_turn(const AppendParams& p, int position, int gone, int c)
 {
-    const int at = position < p.positions ? position : p.positions - 1;
+    int at = position;
+    if (gone != 0) {
+        const long long turned = (long long)position + gone;
+        at = turned < 0 ? 0 : turned < p.positions ? (int)turned : p.positions - 1;
+    }
+    at = at < p.positions ? at : p.positions - 1;
     const float4_t* t = reinterpret_cast<const float4_t*>(p.rope + ((size_t)at * (p.R / 2) + 8 * c) * 2);
     Turn r;
 #pragma unroll
@@ -126,6 +132,7 @@ __device__ __forceinline__ void store_row(_Float16* row, const float (&x)[16], c
 template <int TYPE> struct KvType;
 template <> struct KvType<CODEGEMM_KV_FP16> { typedef _Float16 elem; static constexpr float kMax = 0.0f; };
 template <> struct KvType<CODEGEMM_KV_INT8> { typedef uint8_t elem; static constexpr float kMax = 127.0f; };
+template <> struct KvType<CODEGEMM_KV_INT4> { typedef uint8_t elem; static constexpr float kMax = 0.0f; };       // (half an element)
 template <> struct KvType<CODEGEMM_KV_FP8> { typedef uint8_t elem; static constexpr float kMax = 448.0f; };
 
 // x / scale as the cache holds it, ties to even; |x / scale| <= kMax but for the rounding of the scale's reciprocal.
@@ -169,7 +176,7 @@ __device__ void append_queries(const AppendParams& p, int team)
         return;
     }
     Turn t;
-    if (live && r.turns) t = load_turn(p, position, c);
+    if (live && r.turns) t = load_turn(p, position, p.shift ? p.shift[seq] : 0, c);
     for (int h0 = part * rows; h0 < p.Hq; h0 += rows * p.token_split) {          // uniform: the norm's exchanges need whole rows
         const int h = h0 + tid / lanes;
         const bool mine = live && h < p.Hq;
@@ -181,6 +188,27 @@ __device__ void append_queries(const AppendParams& p, int team)
     }
 }
 
+// A unit: the new tokens lo .. hi - 1 of one sequence among the `group` positions from pos0 on, which share a page.
+struct Unit {
+    int seq, row0, start, pos0, lo, hi, page;       // row0: of position `start`
+};
+__device__ __forceinline__ bool find_unit(const AppendParams& p, int unit, int G, Unit* u)
+{
+    const CacheView& cv = p.c;
+    int seq = unit;
+    if (p.cu) seq = last_at_most(cv.seqs, unit, [&](int i) { return p.cu[i] / G + 2 * i; });
+    int row0;
+    const int n = new_tokens(p, seq, &row0);
+    const int len = cv.lens[seq], end = len < 0 ? 0 : len < kLastEnd ? len : kLastEnd, start = end - n;         // positions of the new tokens: start .. end - 1
+    const int from = start < 0 ? 0 : start;
+    const int skip = p.cu ? unit - (p.cu[seq] / G + 2 * seq) : 0;
+    if (skip < 0 || from >= end || from / G + skip > (end - 1) / G) return false;
+    const int pos0 = (from / G + skip) * G;                                                // of the unit
+    const int lo = pos0 > from ? pos0 : from, hi = end - pos0 > G ? pos0 + G : end;        // its new tokens
+    *u = Unit{seq, row0, start, pos0, lo, hi, page_of(cv, seq, pos0 >> cv.page_shift)};
+    return true;
+}
+
 // Keys or values of one unit: up to `group` new tokens of one sequence and head that share a page, and their scales.
 template <int TYPE, bool TEAMS>
 __device__ void append_unit(const AppendParams& p, int unit, int head, bool values, unsigned char* lds)
@@ -189,17 +217,9 @@ __device__ void append_unit(const AppendParams& p, int unit, int head, bool valu
     const CacheView& cv = p.c;
     const int D = cv.D, G = p.group, lanes = p.row_lanes, teams = TEAMS ? p.teams : 1, threads = teams * kAppendThreads, tid = threadIdx.x;
     const int team = TEAMS ? __builtin_amdgcn_readfirstlane(tid / kAppendThreads) : 0, member = TEAMS ? tid % kAppendThreads : tid, c = member & (lanes - 1), rows = kAppendThreads / lanes;
-    int seq = unit;
-    if (p.cu) seq = last_at_most(cv.seqs, unit, [&](int i) { return p.cu[i] / G + 2 * i; });
-    int row0;
-    const int n = new_tokens(p, seq, &row0);
-    const int len = cv.lens[seq], end = len < 0 ? 0 : len < kLastEnd ? len : kLastEnd, start = end - n;         // positions of the new tokens: start .. end - 1
-    const int from = start < 0 ? 0 : start;
-    const int skip = p.cu ? unit - (p.cu[seq] / G + 2 * seq) : 0;
-    if (skip < 0 || from >= end || from / G + skip > (end - 1) / G) return;
-    const int pos0 = (from / G + skip) * G;                                                // of the unit
-    const int lo = pos0 > from ? pos0 : from, hi = end - pos0 > G ? pos0 + G : end;        // its new tokens
-    const int page = page_of(cv, seq, pos0 >> cv.page_shift);
+    Unit u;
+    if (!find_unit(p, unit, G, &u)) return;
+    const int seq = u.seq, row0 = u.row0, start = u.start, pos0 = u.pos0, lo = u.lo, hi = u.hi, page = u.page, gone = p.shift ? p.shift[seq] : 0;
     if (page < 0 && (values || !p.k_out)) return;
     const int slot0 = pos0 & ((1 << cv.page_shift) - 1);
     const bool live = c < D / 16;
@@ -214,7 +234,7 @@ __device__ void append_unit(const AppendParams& p, int unit, int head, bool valu
         load_row(x, src + row * stride, r, mine);
         if (values) return;
         if (p.k_norm) norm_row(x, p.k_norm, r, mine, lanes, D, p.eps);
-        if (mine && r.turns) rotate_row(x, load_turn(p, pos, c), p.interleaved != 0);
+        if (mine && r.turns) rotate_row(x, load_turn(p, pos, gone, c), p.interleaved != 0);
     };
 
     // The unit's groups of 16 tokens go round the teams; where each team has one at most and takes it at once, tokens stay in registers from the search
@@ -345,6 +365,125 @@ __device__ void append_unit(const AppendParams& p, int unit, int head, bool valu
     }
 }
 
+// The same in 4 bits, whose scales are a token's own: 16 tokens, each row in one pass from its load to its codes.  A lane has 16 consecutive dimensions when
+// it looks for the least and the largest of a run, which is a few exchanges with its neighbours then; keys that have turned get there by way of LDS.
+constexpr float kMost4 = 20000.0f;                      // |x|: so that min - 16 scale stays within fp16
+constexpr float kStep4 = (float)((1.0 - 1.0 / 2048) / 15.0);
+
+__device__ void append_unit4(const AppendParams& p, int unit, int head, bool values, unsigned char* lds)
+{
+    const CacheView& cv = p.c;
+    const int D = cv.D, lanes = p.row_lanes, tid = threadIdx.x, c = tid & (lanes - 1), rows = kAppendThreads / lanes;
+    Unit u;
+    if (!find_unit(p, unit, kTokenGroup, &u)) return;
+    const int gone = p.shift ? p.shift[u.seq] : 0, page = u.page;
+    if (page < 0 && (values || !p.k_out)) return;
+    const int slot0 = u.pos0 & ((1 << cv.page_shift) - 1);
+    const bool live = c < D / 16;
+    const Runs r = values ? runs_of(c, 0, false) : runs_of(c, p.R, p.interleaved != 0);
+    const bool apart = !values && p.R > 0 && !p.interleaved;
+    const _Float16* src = (values ? p.v : p.k) + head * D;
+    const size_t stride = values ? p.v_stride : p.k_stride;
+    const int run_lanes = 1 << (cv.run_shift - 4), over = run_lanes < lanes ? run_lanes : lanes, run = c >> (cv.run_shift - 4);
+    uint8_t* stage = lds;                                                                  // of values: [D][16] codes, 16 bytes more every 16 rows
+    for (int t0 = u.lo; t0 < u.hi; t0 += rows) {
+        const int pos = t0 + tid / lanes;
+        const bool mine = live && pos < u.hi;
+        const int row = mine ? u.row0 + pos - u.start : 0, slot = slot0 + pos - u.pos0;
+        float x[16];
+        load_row(x, src + row * stride, r, mine);
+        if (!values) {
+            if (p.k_norm) norm_row(x, p.k_norm, r, mine, lanes, D, p.eps);
+            if (mine && r.turns) rotate_row(x, load_turn(p, pos, gone, c), p.interleaved != 0);
+            if (mine && p.k_out) store_row(p.k_out + (size_t)row * p.k_out_stride + head * D, x, r);
+        }
+        if (page < 0) continue;                                                            // uniform
+        if (apart) {
+            float* turned = reinterpret_cast<float*>(lds) + tid / lanes * D;               // the rows of a wavefront are its own
+            if (live) {
+#pragma unroll
+                for (int e = 0; e < 8; e += 4) {
+                    *reinterpret_cast<float4_t*>(turned + r.a + e) = float4_t{x[e], x[e + 1], x[e + 2], x[e + 3]};
+                    *reinterpret_cast<float4_t*>(turned + r.b + e) = float4_t{x[8 + e], x[9 + e], x[10 + e], x[11 + e]};
+                }
+            }
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+            if (live) {
+#pragma unroll
+                for (int e = 0; e < 16; e += 4) {
+                    const float4_t y = *reinterpret_cast<const float4_t*>(turned + 16 * c + e);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[e + i] = y[i];
+                }
+            }
+        }
+        float low = INFINITY, high = -INFINITY;
+        int bad = 0;
+        if (mine) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                bad |= !(fabsf(x[e]) <= 3.402823466e38f);
+                x[e] = __builtin_amdgcn_fmed3f(x[e], -kMost4, kMost4);
+                low = fminf(low, x[e]);
+                high = fmaxf(high, x[e]);
+            }
+        }
+        for (int o = over >> 1; o > 0; o >>= 1) {
+            low = fminf(low, __shfl_xor(low, o));
+            high = fmaxf(high, __shfl_xor(high, o));
+            bad |= __shfl_xor(bad, o);
+        }
+        if (!mine) continue;
+        const _Float16 s = bad ? (_Float16)__builtin_nanf("") : (_Float16)((high - low) * kStep4);
+        const _Float16 off = bad ? (_Float16)__builtin_nanf("") : (_Float16)(low - 16.0f * (float)s);
+        const float by = (float)s > 0.0f ? 1.0f / (float)s : 0.0f;                         // a NaN scale: zeros
+        uint32_t code[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) code[e] = (uint32_t)(int)__builtin_amdgcn_fmed3f(rintf(by != 0.0f ? (x[e] - (float)off) * by - 16.0f : 0.0f), 0.0f, 15.0f);
+        const bool first = (c & (run_lanes - 1)) == 0;
+        if (!values) {
+            u32x2_t w = {0, 0};
+#pragma unroll
+            for (int e = 0; e < 16; ++e) w[e >> 3] |= code[e] << (4 * ((e & 7) >> 1) + 16 * (e & 1));
+            *reinterpret_cast<u32x2_t*>(cv.k + (page_at(cv, page, head) + (size_t)slot * D) / 2 + 8 * c) = w;
+            if (first) {
+                const half2_t both = {s, off};
+                reinterpret_cast<uint32_t*>(cv.k_scales)[runs_at(cv, page, head, slot) + run] = __builtin_bit_cast(uint32_t, both);
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) stage[(16 * c + e) * kTokenGroup + c * 16 + slot % kTokenGroup] = (uint8_t)code[e];
+            if (first) {
+                _Float16* to = reinterpret_cast<_Float16*>(cv.v_scales) + 2 * runs_at(cv, page, head, slot & ~(kTokenGroup - 1)) + 32 * run + slot % kTokenGroup;
+                to[0] = s;
+                to[kTokenGroup] = off;
+            }
+        }
+    }
+    if (!values) return;
+    __syncthreads();
+    // words of 8 tokens; those that hold earlier ones keep their codes
+    uint32_t* words = reinterpret_cast<uint32_t*>(cv.v + (page_at(cv, page, head) + (size_t)slot0 * D) / 2);
+    const int from = u.lo - u.pos0, to = u.hi - u.pos0;
+    for (int i = tid; i < 2 * D; i += kAppendThreads) {
+        const int d = i >> 1, t0 = 8 * (i & 1);
+        if (t0 + 8 <= from || t0 >= to) continue;
+        const u32x2_t bytes = *reinterpret_cast<const u32x2_t*>(stage + d * kTokenGroup + d / 16 * 16 + t0);
+        uint32_t w = 0, mask = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int at = 4 * (e >> 1) + 16 * (e & 1);
+            const bool is_new = t0 + e >= from && t0 + e < to;
+            w |= is_new ? (bytes[e >> 2] >> (8 * (e & 3)) & 15u) << at : 0u;
+            mask |= is_new ? 15u << at : 0u;
+        }
+        if (mask != ~0u) w |= words[i] & ~mask;
+        words[i] = w;
+    }
+}
+
 // Bytes of LDS of a workgroup.
 template <int TYPE>
 constexpr size_t append_lds(int teams, int D) { return 64 + (size_t)teams * (D * kTokenGroup * sizeof(typename KvType<TYPE>::elem) + D); }
@@ -361,15 +500,20 @@ __global__ void __launch_bounds__(TEAMS ? kMostTeams * kAppendThreads : kAppendT
     const int i = blk - p.token_blocks, half = p.units * p.c.Hk;
     const bool values = i >= half;
     const int j = values ? i - half : i;
-    append_unit<TYPE, TEAMS>(p, j / p.c.Hk, j % p.c.Hk, values, lds);
+    if constexpr (TYPE == CODEGEMM_KV_INT4) append_unit4(p, j / p.c.Hk, j % p.c.Hk, values, lds);
+    else append_unit<TYPE, TEAMS>(p, j / p.c.Hk, j % p.c.Hk, values, lds);
 }
 
 template <int TYPE>
 static void launch_append(const AppendParams& p, unsigned blocks, hipStream_t s)
 {
     const dim3 grid(blocks), threads(p.teams * kAppendThreads);
+    if constexpr (TYPE == CODEGEMM_KV_INT4) {
+        hipLaunchKernelGGL((kv_append_kernel<TYPE, false>), grid, threads, kAppendThreads * 16 * sizeof(float), s, p);
+        return;
+    }
     const size_t lds = append_lds<TYPE>(p.teams, p.c.D);
-    if constexpr (TYPE != CODEGEMM_KV_FP16) {
+    if constexpr (TYPE == CODEGEMM_KV_INT8 || TYPE == CODEGEMM_KV_FP8) {
         if (p.teams > 1) {
             hipLaunchKernelGGL((kv_append_kernel<TYPE, true>), grid, threads, lds, s, p);
             return;
@@ -385,12 +529,50 @@ struct GatherParams {
     int rows, row_lanes;
 };
 
+// .. in 4 bits: places from .. to - 1 of 16, of which those below `held` have a token; out: the row of place 0.
+__device__ __forceinline__ void gather_unit4(const CacheView& cv, bool values, int page, int head, int slot0, int from, int to, int held, int lanes, _Float16* out, uint32_t* stage)
+{
+    const int D = cv.D, tid = threadIdx.x, c = tid & (lanes - 1), per = kAppendThreads / lanes, run = c >> (cv.run_shift - 4);
+    const size_t at = page < 0 ? 0 : page_at(cv, page, head) + (size_t)slot0 * D, scale_at = page < 0 ? 0 : runs_at(cv, page, head, slot0);
+    constexpr int kPad = 4;                                             // words, every 16 dimensions
+    if (values && held > 0) {
+        for (int i = tid; i < D / 2; i += kAppendThreads)
+            *reinterpret_cast<u32x4_t*>(stage + 4 * i + i / 8 * kPad) = *reinterpret_cast<const u32x4_t*>(cv.v + at / 2 + 16 * i);
+        __syncthreads();
+    }
+    for (int t0 = from; t0 < to; t0 += per) {
+        const int t = t0 + tid / lanes;
+        if (t >= to || c >= D / 16) continue;
+        half8_t x[2] = {{0, 0, 0, 0, 0, 0, 0, 0}, {0, 0, 0, 0, 0, 0, 0, 0}};
+        if (t < held) {
+            if (!values) {
+                const u32x2_t w = *reinterpret_cast<const u32x2_t*>(cv.k + (at + (size_t)t * D) / 2 + 8 * c);
+                const uint32_t so = reinterpret_cast<const uint32_t*>(cv.k_scales)[scale_at + (size_t)t * cv.runs + run];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) x[i] = four_bits(w[i], both_low(so), both_high(so));
+            } else {
+                const _Float16* so = reinterpret_cast<const _Float16*>(cv.v_scales) + 2 * scale_at + 32 * run + t;
+                const _Float16 s = so[0], o = so[kTokenGroup];
+                const int by = 4 * ((t & 7) >> 1) + 16 * (t & 1);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const uint32_t code = stage[(16 * c + e) * 2 + c * kPad + (t >> 3)] >> by & 15u;
+                    x[e >> 3][e & 7] = __builtin_fmaf16((_Float16)(float)(code + 16u), s, o);
+                }
+            }
+        }
+        _Float16* dst = out + (ptrdiff_t)t * cv.Hk * D + 16 * c;
+        __builtin_nontemporal_store(x[0], reinterpret_cast<half8_t*>(dst));
+        __builtin_nontemporal_store(x[1], reinterpret_cast<half8_t*>(dst + 8));
+    }
+}
+
 // One group of 16 positions of a sequence and head: blockIdx.y 0 keys, 1 values.
 template <int TYPE>
 __global__ void __launch_bounds__(kAppendThreads) kv_gather_kernel(const GatherParams p)
 {
     typedef typename KvType<TYPE>::elem elem;
-    __shared__ __align__(16) unsigned char lds[(kMaxHeadDim * kTokenGroup + 256) * sizeof(elem)];
+    __shared__ __align__(16) unsigned char lds[(kMaxHeadDim * kTokenGroup + 256) * sizeof(elem) / (TYPE == CODEGEMM_KV_INT4 ? 2 : 1)];
     const CacheView& cv = p.c;
     const bool values = blockIdx.y != 0;
     _Float16* out = values ? p.v_out : p.k_out;
@@ -413,6 +595,10 @@ __global__ void __launch_bounds__(kAppendThreads) kv_gather_kernel(const GatherP
     const int page = held > 0 ? page_of(cv, seq, (int)(pos0 >> cv.page_shift)) : -1;
     if (page < 0) held = 0;
     const int slot0 = (int)(pos0 & ((1 << cv.page_shift) - 1));
+    if constexpr (TYPE == CODEGEMM_KV_INT4) {
+        gather_unit4(cv, values, page, head, slot0, from, to, held, lanes, out + ((size_t)(lo + (int)(pos0 - start)) * cv.Hk + head) * D, reinterpret_cast<uint32_t*>(lds));
+        return;
+    }
     const elem* pool = reinterpret_cast<const elem*>(values ? cv.v : cv.k) + (page < 0 ? 0 : page_at(cv, page, head) + (size_t)slot0 * D);
     const float* scales = TYPE == CODEGEMM_KV_FP16 || page < 0 ? nullptr : (values ? cv.v_scales : cv.k_scales) + scales_at(cv, page, head);
     elem* stage = reinterpret_cast<elem*>(lds);
@@ -453,11 +639,13 @@ int check_cache(const codegemm_kv_cache* c, bool pointers)
 {
     if (!c) return CODEGEMM_INVALID_ARG;
     if (c->kv_heads < 1 || c->head_dim < 1 || c->num_pages < 1 || c->num_seqs < 1 || c->max_pages < 1) return CODEGEMM_INVALID_ARG;
-    if (c->dtype < CODEGEMM_KV_FP16 || c->dtype > CODEGEMM_KV_FP8) return CODEGEMM_UNSUPPORTED;
+    const bool four = c->dtype == CODEGEMM_KV_INT4;
+    if (c->dtype != CODEGEMM_KV_FP16 && c->dtype != CODEGEMM_KV_INT8 && c->dtype != CODEGEMM_KV_FP8 && !four) return CODEGEMM_UNSUPPORTED;
     if (c->page_size < kTokenGroup || c->page_size > 256 || (c->page_size & (c->page_size - 1))) return CODEGEMM_UNSUPPORTED;
     if (c->head_dim % 16 || c->head_dim > kMaxHeadDim || c->kv_heads > kMaxHeads) return CODEGEMM_UNSUPPORTED;
     if (c->num_pages > 1 << 30 || c->num_seqs > kMaxSeqs || (long long)c->max_pages * c->page_size > 1ll << 30) return CODEGEMM_UNSUPPORTED;
-    if (c->dtype != CODEGEMM_KV_FP16 && (c->scale_block < 1 || c->scale_block > c->page_size || (c->scale_block & (c->scale_block - 1)))) return CODEGEMM_UNSUPPORTED;
+    if (four && (c->head_dim % 32 || (c->scale_block != 32 && c->scale_block != 64 && c->scale_block != 128 && c->scale_block != 256))) return CODEGEMM_UNSUPPORTED;
+    if (c->dtype != CODEGEMM_KV_FP16 && !four && (c->scale_block < 1 || c->scale_block > c->page_size || (c->scale_block & (c->scale_block - 1)))) return CODEGEMM_UNSUPPORTED;
     if (!pointers) return CODEGEMM_OK;
     if (!c->k || !c->v || !c->page_table || !c->kv_lens || misaligned(c->k) || misaligned(c->v) || misaligned_ints(c->page_table) || misaligned_ints(c->kv_lens))
         return CODEGEMM_INVALID_ARG;
@@ -483,7 +671,10 @@ CacheView cache_view(const codegemm_kv_cache& c)
     v.lens = c.kv_lens;
     v.Hk = c.kv_heads; v.D = c.head_dim; v.pages = c.num_pages; v.max_pages = c.max_pages; v.seqs = c.num_seqs;
     v.page_shift = log2_of(c.page_size);
-    v.block_shift = c.dtype == CODEGEMM_KV_FP16 ? v.page_shift : log2_of(c.scale_block);
+    const bool four = c.dtype == CODEGEMM_KV_INT4;
+    v.block_shift = c.dtype == CODEGEMM_KV_FP16 || four ? v.page_shift : log2_of(c.scale_block);
+    v.run_shift = four ? log2_of(c.scale_block) : 0;
+    v.runs = four ? ceil_div(c.head_dim, c.scale_block) : 0;
     return v;
 }
 
@@ -497,18 +688,26 @@ using namespace cg;
 extern "C" size_t codegemm_kv_pool_bytes(const codegemm_kv_cache* c)
 {
     if (check_cache(c, false)) return 0;
-    return (size_t)c->num_pages * c->kv_heads * c->page_size * c->head_dim * (c->dtype == CODEGEMM_KV_FP16 ? 2 : 1);
+    return (size_t)c->num_pages * c->kv_heads * c->page_size * c->head_dim * (c->dtype == CODEGEMM_KV_FP16 ? 2 : 1) / (c->dtype == CODEGEMM_KV_INT4 ? 2 : 1);
 }
 
 extern "C" size_t codegemm_kv_scales_bytes(const codegemm_kv_cache* c)
 {
     if (check_cache(c, false) || c->dtype == CODEGEMM_KV_FP16) return 0;
-    return (size_t)c->num_pages * c->kv_heads * (c->page_size / c->scale_block) * sizeof(float);
+    const int each = c->dtype == CODEGEMM_KV_INT4 ? c->page_size * ceil_div(c->head_dim, c->scale_block) : c->page_size / c->scale_block;     // of 4 bytes
+    return (size_t)c->num_pages * c->kv_heads * each * sizeof(float);
 }
 
 extern "C" int codegemm_kv_append(const codegemm_kv_cache* cache, const codegemm_append_desc* desc, const int32_t* cu_seqlens, const void* q,
                                   const void* k, const void* v, const void* q_norm, const void* k_norm, const float* rope, void* q_out, void* k_out,
                                   void* stream)
+{
+    return codegemm_kv_append_shifted(cache, desc, cu_seqlens, nullptr, q, k, v, q_norm, k_norm, rope, q_out, k_out, stream);
+}
+
+extern "C" int codegemm_kv_append_shifted(const codegemm_kv_cache* cache, const codegemm_append_desc* desc, const int32_t* cu_seqlens, const int32_t* shift,
+                                          const void* q, const void* k, const void* v, const void* q_norm, const void* k_norm, const float* rope, void* q_out,
+                                          void* k_out, void* stream)
 {
     const int st = check_cache(cache, true);
     if (st) return st;
@@ -518,7 +717,7 @@ extern "C" int codegemm_kv_append(const codegemm_kv_cache* cache, const codegemm
     if (d.tokens < 1 || d.q_heads < 0 || d.rotary_dim < 0 || d.rotary_dim > D || !(d.norm_eps >= 0.0f) || (d.flags & ~CODEGEMM_ROPE_INTERLEAVED)) return CODEGEMM_INVALID_ARG;
     if (d.tokens > kMaxTokens || d.q_heads > kMaxHeads || d.rotary_dim % 16) return CODEGEMM_UNSUPPORTED;
     if (!cu_seqlens && d.tokens != cache->num_seqs) return CODEGEMM_INVALID_ARG;
-    if (cu_seqlens && misaligned_ints(cu_seqlens)) return CODEGEMM_INVALID_ARG;
+    if ((cu_seqlens && misaligned_ints(cu_seqlens)) || (shift && misaligned_ints(shift))) return CODEGEMM_INVALID_ARG;
     if (d.q_heads > 0 && (!q || !q_out || misaligned(q) || misaligned(q_out))) return CODEGEMM_INVALID_ARG;
     if (d.rotary_dim > 0 && (!rope || misaligned(rope) || d.rope_positions < 1)) return CODEGEMM_INVALID_ARG;
     if ((q_norm && misaligned(q_norm)) || (k_norm && misaligned(k_norm)) || (k_out && misaligned(k_out))) return CODEGEMM_INVALID_ARG;
@@ -528,6 +727,7 @@ extern "C" int codegemm_kv_append(const codegemm_kv_cache* cache, const codegemm
     AppendParams p;
     p.c = cache_view(*cache);
     p.cu = cu_seqlens;
+    p.shift = shift;
     p.q = static_cast<const _Float16*>(q);
     p.k = static_cast<const _Float16*>(k);
     p.v = static_cast<const _Float16*>(v);
@@ -546,7 +746,7 @@ extern "C" int codegemm_kv_append(const codegemm_kv_cache* cache, const codegemm
     p.eps = d.norm_eps;
     p.row_lanes = row_lanes(D);
     const int block = 1 << p.c.block_shift;
-    p.group = cache->dtype == CODEGEMM_KV_FP16 || block < kTokenGroup ? kTokenGroup : block;
+    p.group = cache->dtype == CODEGEMM_KV_FP16 || cache->dtype == CODEGEMM_KV_INT4 || block < kTokenGroup ? kTokenGroup : block;
     // A sequence of n new tokens touches at most n / group + 2 units, its first unit being number cu / group + 2 i.
     p.units = cu_seqlens ? p.T / p.group + 2 * cache->num_seqs : cache->num_seqs;
     // Few tokens: their heads over several teams.  Many: a team keeps a token's cosines for all its heads.
@@ -564,6 +764,7 @@ extern "C" int codegemm_kv_append(const codegemm_kv_cache* cache, const codegemm
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (cache->dtype == CODEGEMM_KV_FP16) launch_append<CODEGEMM_KV_FP16>(p, (unsigned)blocks, s);
     else if (cache->dtype == CODEGEMM_KV_INT8) launch_append<CODEGEMM_KV_INT8>(p, (unsigned)blocks, s);
+    else if (cache->dtype == CODEGEMM_KV_INT4) launch_append<CODEGEMM_KV_INT4>(p, (unsigned)blocks, s);
     else launch_append<CODEGEMM_KV_FP8>(p, (unsigned)blocks, s);
     return hipGetLastError() == hipSuccess ? CODEGEMM_OK : CODEGEMM_LAUNCH_FAILED;
 }
@@ -590,6 +791,7 @@ extern "C" int codegemm_kv_gather(const codegemm_kv_cache* cache, int32_t rows, 
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (cache->dtype == CODEGEMM_KV_FP16) hipLaunchKernelGGL(kv_gather_kernel<CODEGEMM_KV_FP16>, grid, threads, 0, s, p);
     else if (cache->dtype == CODEGEMM_KV_INT8) hipLaunchKernelGGL(kv_gather_kernel<CODEGEMM_KV_INT8>, grid, threads, 0, s, p);
+    else if (cache->dtype == CODEGEMM_KV_INT4) hipLaunchKernelGGL(kv_gather_kernel<CODEGEMM_KV_INT4>, grid, threads, 0, s, p);
     else hipLaunchKernelGGL(kv_gather_kernel<CODEGEMM_KV_FP8>, grid, threads, 0, s, p);
     return hipGetLastError() == hipSuccess ? CODEGEMM_OK : CODEGEMM_LAUNCH_FAILED;
 }
