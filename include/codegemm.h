@@ -483,6 +483,40 @@ int codegemm_attn_decode(const codegemm_kv_cache *cache, const codegemm_attn_des
                          void *stream);
 
 /*
+ * How much the cached tokens are attended to, summed per token and key head: what says
+ * which of them a sequence can do without (codegemm_kv_evict).  The n_i queries cu_q[i] ..
+ * cu_q[i+1]-1 of q [total_q][q_heads][D] stand at the last positions kv_lens[i] - n_i ..
+ * kv_lens[i] - 1 of sequence i, whose keys are in the cache; a query sees the keys up to
+ * its own position (with a window W: the last W of these) that have a page, and
+ *     scores[page][h][place] = earlier[page][h][place] + sum of the softmax weights that the
+ *     key has from these queries in the query heads of key head h
+ * for every position t < kv_lens[i] with a page; without `earlier` from position first[i]
+ * on (first [num_seqs] int32; NULL: from kv_lens[i] - n_i on, the queries' own tokens).
+ * scores and earlier [num_pages][kv_heads][page_size] fp32; they may be one array, and
+ * earlier may be NULL.  Other places of scores stay as they are.  A page may belong to one
+ * sequence only.  cu_q NULL: one query each, total_q = num_seqs.  Queries at negative
+ * positions see nothing.  In fp32, in a fixed order.  total_kv, k_stride, v_stride and
+ * out_stride of desc are not read; kv_heads, head_dim and num_seqs are those of the cache.
+ * workspace: as for codegemm_attn_decode.  num_seqs * kv_heads < 2^24, total_q * q_heads < 2^31.
+ */
+size_t codegemm_attn_scores_workspace_bytes(const codegemm_kv_cache *cache, const codegemm_attn_desc *desc);
+int codegemm_attn_scores(const codegemm_kv_cache *cache, const codegemm_attn_desc *desc,
+                         const void *q, const int32_t *cu_q, const int32_t *first,
+                         const float *earlier, float *scores, void *workspace,
+                         size_t workspace_bytes, void *stream);
+
+/*
+ * codegemm_attn_decode and the scores of the same queries, which take the softmax's sums
+ * from it: keys are read twice, values once.  out: as codegemm_attn_decode's (for
+ * CODEGEMM_KV_FP16 divided by the weights' sum before their rounding instead of after it).
+ */
+size_t codegemm_attn_decode_scores_workspace_bytes(const codegemm_kv_cache *cache, const codegemm_attn_desc *desc);
+int codegemm_attn_decode_scores(const codegemm_kv_cache *cache, const codegemm_attn_desc *desc,
+                                const void *q, void *out, const int32_t *first,
+                                const float *earlier, float *scores, void *workspace,
+                                size_t workspace_bytes, void *stream);
+
+/*
  * Packed sequences: queries cu_q[i] .. cu_q[i+1]-1 (n of them) of q
  * [total_q][q_heads][D] attend to keys cu_kv[i] .. cu_kv[i+1]-1 (n_kv) of k and v
  * [total_kv][kv_heads][D], fp16; cu_q and cu_kv [num_seqs + 1] int32, ascending

@@ -38,7 +38,8 @@ EXPORTS = [
     "codegemm_gemm_static", "codegemm_static_workspace_limit",
     "codegemm_gemm_grouped", "codegemm_grouped_workspace_bytes",
     "codegemm_kv_pool_bytes", "codegemm_kv_scales_bytes", "codegemm_kv_append", "codegemm_kv_append_shifted", "codegemm_kv_gather",
-    "codegemm_attn_decode", "codegemm_attn_decode_workspace_bytes", "codegemm_attn_prompt", "codegemm_attn_prompt_workspace_bytes",
+    "codegemm_attn_decode", "codegemm_attn_decode_workspace_bytes", "codegemm_attn_scores", "codegemm_attn_scores_workspace_bytes",
+    "codegemm_attn_decode_scores", "codegemm_attn_decode_scores_workspace_bytes", "codegemm_attn_prompt", "codegemm_attn_prompt_workspace_bytes",
 ]
 
 
@@ -200,6 +201,11 @@ def load() -> ctypes.CDLL:
     lib.codegemm_attn_decode_workspace_bytes.restype = sz
     lib.codegemm_attn_decode.argtypes = [cp, tp, vp, vp, vp, sz, vp]
     lib.codegemm_attn_decode.restype = i
+    for name in ("codegemm_attn_scores", "codegemm_attn_decode_scores"):
+        getattr(lib, name + "_workspace_bytes").argtypes = [cp, tp]
+        getattr(lib, name + "_workspace_bytes").restype = sz
+        getattr(lib, name).argtypes = [cp, tp, vp, vp, vp, vp, vp, vp, sz, vp]
+        getattr(lib, name).restype = i
     lib.codegemm_attn_prompt_workspace_bytes.argtypes = [tp]
     lib.codegemm_attn_prompt_workspace_bytes.restype = sz
     lib.codegemm_attn_prompt.argtypes = [tp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
@@ -376,6 +382,24 @@ def codegemm_attn_decode_workspace_bytes(cache: KvCache, desc: AttnDesc) -> int:
 def _attn_decode(cache: KvCache, desc: AttnDesc, q, out, workspace, workspace_bytes: int, stream: int = 0) -> None:
     _check(load().codegemm_attn_decode(ctypes.byref(cache), ctypes.byref(desc), _ptr(q), _ptr(out), _ptr(workspace), workspace_bytes, stream),
            "codegemm_attn_decode")
+
+
+def codegemm_attn_scores_workspace_bytes(cache: KvCache, desc: AttnDesc) -> int:
+    return int(load().codegemm_attn_scores_workspace_bytes(ctypes.byref(cache), ctypes.byref(desc)))
+
+
+def codegemm_attn_scores(cache: KvCache, desc: AttnDesc, q, cu_q, first, earlier, scores, workspace, workspace_bytes: int, stream: int = 0) -> None:
+    _check(load().codegemm_attn_scores(ctypes.byref(cache), ctypes.byref(desc), _ptr(q), _ptr(cu_q), _ptr(first), _ptr(earlier), _ptr(scores),
+                                       _ptr(workspace), workspace_bytes, stream), "codegemm_attn_scores")
+
+
+def codegemm_attn_decode_scores_workspace_bytes(cache: KvCache, desc: AttnDesc) -> int:
+    return int(load().codegemm_attn_decode_scores_workspace_bytes(ctypes.byref(cache), ctypes.byref(desc)))
+
+
+def codegemm_attn_decode_scores(cache: KvCache, desc: AttnDesc, q, out, first, earlier, scores, workspace, workspace_bytes: int, stream: int = 0) -> None:
+    _check(load().codegemm_attn_decode_scores(ctypes.byref(cache), ctypes.byref(desc), _ptr(q), _ptr(out), _ptr(first), _ptr(earlier), _ptr(scores),
+                                              _ptr(workspace), workspace_bytes, stream), "codegemm_attn_decode_scores")
 
 
 def codegemm_attn_prompt_workspace_bytes(desc: AttnDesc) -> int:

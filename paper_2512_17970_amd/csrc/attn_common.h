@@ -57,6 +57,38 @@ __device__ __forceinline__ int last_at_most(int n, int x, First first)
     return __builtin_amdgcn_readfirstlane(base);
 }
 
+// 8 codes to fp16, exactly.
+template <int TYPE>
+__device__ __forceinline__ half8_t codes_to_half(uint32_t lo, uint32_t hi)
+{
+    if constexpr (TYPE == CODEGEMM_KV_INT8) {
+        // code + 128 in the low byte of 0x6400 is 1024 + code + 128
+        const half2_t off = {(_Float16)-1152.0f, (_Float16)-1152.0f};
+        lo ^= 0x80808080u;
+        hi ^= 0x80808080u;
+        const half2_t a = __builtin_bit_cast(half2_t, __builtin_amdgcn_perm(0x64646464u, lo, 0x04010400u)) + off;
+        const half2_t b = __builtin_bit_cast(half2_t, __builtin_amdgcn_perm(0x64646464u, lo, 0x04030402u)) + off;
+        const half2_t c = __builtin_bit_cast(half2_t, __builtin_amdgcn_perm(0x64646464u, hi, 0x04010400u)) + off;
+        const half2_t d = __builtin_bit_cast(half2_t, __builtin_amdgcn_perm(0x64646464u, hi, 0x04030402u)) + off;
+        return half8_t{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+    } else {
+        const half2_t a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)lo, 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)lo, 1.0f, true);
+        const half2_t c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)hi, 1.0f, false), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)hi, 1.0f, true);
+        return half8_t{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+    }
+}
+
+// Sum, maximum over the four lanes of a column: lanes l, l ^ 16, l ^ 32, l ^ 48.
+template <class Join>
+__device__ __forceinline__ float over_groups(float x, Join join)
+{
+    const uint32_t w = __builtin_bit_cast(uint32_t, x);
+    const auto a = __builtin_amdgcn_permlane16_swap(w, w, false, false);
+    const uint32_t y = __builtin_bit_cast(uint32_t, join(__builtin_bit_cast(float, (uint32_t)a[0]), __builtin_bit_cast(float, (uint32_t)a[1])));
+    const auto b = __builtin_amdgcn_permlane32_swap(y, y, false, false);
+    return join(__builtin_bit_cast(float, (uint32_t)b[0]), __builtin_bit_cast(float, (uint32_t)b[1]));
+}
+
 // What workgroups hand to each other: device-scope accesses of 16 (8) bytes, `at` bytes from the base of `parts`.  (By 8-byte atomics, single tokens
 // after 8000, 32 pieces, took 18.0 us, so 15.0.)
 constexpr int kDeviceScope = 16;            // the cache policy bit that device-scope atomics have (sc1)
@@ -128,6 +160,8 @@ __device__ __forceinline__ constexpr int operand_dim(int i, int g)
 // First scale-and-offset word of a token's keys (of 16 tokens' values) at slot `slot`, a multiple of 16 for values: as many for both.
 __device__ __forceinline__ size_t runs_at(const CacheView& c, int page, int head, int slot) { return ((((size_t)page * c.Hk + head) << c.page_shift) + slot) * (size_t)c.runs; }
 
+int attn_decode(const codegemm_kv_cache* cache, const codegemm_attn_desc* desc, const void* q, void* out, Pair* stats, void* workspace, size_t workspace_bytes, void* stream);
+int set_max_lds(const void* fn, size_t bytes);                    // status; gemm.hip
 int check_cache(const codegemm_kv_cache* c, bool pointers);     // status
 int check_attn(const codegemm_attn_desc* d);                     // status
 CacheView cache_view(const codegemm_kv_cache& c);

@@ -45,6 +45,7 @@ struct DecodeParams {
     _Float16* out;
     float* part;            // [piece of an item that has several][16 (D + 2)]: [D / 16][64 lanes][4] sums, [16] maximum and weight
     uint32_t* counters;     // of such an item: that of its first piece
+    Pair* stats;            // [sequence][query head], or NULL: what scores are a weight's logarithm above, and 1 / the weights' sum
     int slots;              // workgroups that run at once
     int r;                  // query heads of a key head
     int tiles;              // items of 16 of them
@@ -52,27 +53,6 @@ struct DecodeParams {
     int window;
     float scale;            // times log2(e)
 };
-
-// 8 codes to fp16, exactly.
-template <int TYPE>
-__device__ __forceinline__ half8_t codes_to_half(uint32_t lo, uint32_t hi)
-{
-    if constexpr (TYPE == CODEGEMM_KV_INT8) {
-        // code + 128 in the low byte of 0x6400 is 1024 + code + 128
-        const half2_t off = {(_Float16)-1152.0f, (_Float16)-1152.0f};
-        lo ^= 0x80808080u;
-        hi ^= 0x80808080u;
-        const half2_t a = __builtin_bit_cast(half2_t, __builtin_amdgcn_perm(0x64646464u, lo, 0x04010400u)) + off;
-        const half2_t b = __builtin_bit_cast(half2_t, __builtin_amdgcn_perm(0x64646464u, lo, 0x04030402u)) + off;
-        const half2_t c = __builtin_bit_cast(half2_t, __builtin_amdgcn_perm(0x64646464u, hi, 0x04010400u)) + off;
-        const half2_t d = __builtin_bit_cast(half2_t, __builtin_amdgcn_perm(0x64646464u, hi, 0x04030402u)) + off;
-        return half8_t{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
-    } else {
-        const half2_t a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)lo, 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)lo, 1.0f, true);
-        const half2_t c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)hi, 1.0f, false), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)hi, 1.0f, true);
-        return half8_t{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
-    }
-}
 
 typedef __attribute__((address_space(3))) u32x4_t lds_words4;
 typedef __attribute__((address_space(3))) u32x2_t lds_words2;
@@ -127,17 +107,6 @@ __device__ __forceinline__ unsigned wave_max(unsigned x)
 }
 __device__ __forceinline__ unsigned wave_sum(unsigned x) { return (unsigned)__builtin_amdgcn_readlane((int)wave_scan(x), kWave - 1); }
 
-// Sum, maximum over the four lanes of a column: lanes l, l ^ 16, l ^ 32, l ^ 48.
-template <class Join>
-__device__ __forceinline__ float over_groups(float x, Join join)
-{
-    const uint32_t w = __builtin_bit_cast(uint32_t, x);
-    const auto a = __builtin_amdgcn_permlane16_swap(w, w, false, false);
-    const uint32_t y = __builtin_bit_cast(uint32_t, join(__builtin_bit_cast(float, (uint32_t)a[0]), __builtin_bit_cast(float, (uint32_t)a[1])));
-    const auto b = __builtin_amdgcn_permlane32_swap(y, y, false, false);
-    return join(__builtin_bit_cast(float, (uint32_t)b[0]), __builtin_bit_cast(float, (uint32_t)b[1]));
-}
-
 // A sequence's tokens lo .. len - 1; its steps start at multiples of their length.  One without tokens has a step all the same, in
 // which nothing counts, and so gets its zeros.
 struct Span {
@@ -166,7 +135,8 @@ __device__ __forceinline__ void request4(uint32_t lds, const float* from)
 }
 
 // TYPE: of the cache.  DP: head_dim rounded up to 64, 128 or 256; EXACT: it is head_dim.
-template <int TYPE, int DP, bool EXACT, bool NARROW>
+// SUMS: of weights as they are, not as they are rounded, also in fp16 (there are `stats`).
+template <int TYPE, int DP, bool EXACT, bool NARROW, bool SUMS>
 __global__ void __launch_bounds__((DecodeStep<TYPE, DP, NARROW>::kWaves * kWave), (DecodeStep<TYPE, DP, NARROW>::kWaves * DecodeStep<TYPE, DP, NARROW>::kPerCu > 4 ? 2 : 1))
 attn_decode_kernel(const DecodeParams p)
 {
@@ -483,9 +453,9 @@ attn_decode_kernel(const DecodeParams p)
                 for (int r = 0; r < 4; ++r) {
                     const float w = __builtin_amdgcn_exp2f(s[n][r] - base);
                     pf[4 * n + r] = (_Float16)(T::kScaled ? w * vs[n][r] : w);
-                    if constexpr (!T::kHalf) add += w;                   // (unrounded, as products have scales: off by 2^-11 at most)
+                    if constexpr (!T::kHalf || SUMS) add += w;           // (unrounded, as products have scales: off by 2^-11 at most)
                 }
-            if constexpr (T::kHalf) {                                    // the sum of the weights as they are rounded
+            if constexpr (T::kHalf && !SUMS) {                                    // the sum of the weights as they are rounded
 #pragma unroll
                 for (int i = 0; i < 8; i += 2) add = __builtin_amdgcn_fdot2(half2_t{pf[i], pf[i + 1]}, half2_t{(_Float16)1.0f, (_Float16)1.0f}, add, false);
             }
@@ -609,8 +579,12 @@ attn_decode_kernel(const DecodeParams p)
             _Float16* out = p.out + (size_t)seq * p.out_stride + (size_t)(head * p.r + row0 + col) * D + 16 * b + 4 * g;
             if (col < rows && 16 * b < D) *reinterpret_cast<half4_t*>(out) = half4_t{(_Float16)(x[0] * inv), (_Float16)(x[1] * inv), (_Float16)(x[2] * inv), (_Float16)(x[3] * inv)};
         };
+        auto tell = [&](float upto, float all, float inv) {
+            if (p.stats && wave == 0 && g == 0 && col < rows) p.stats[(size_t)seq * cv.Hk * p.r + head * p.r + row0 + col] = Pair{all == 0.0f ? 0.0f : upto, inv};
+        };
         if (parts == 1) {
             const float inv = weight == 0.0f ? 0.0f : 1.0f / weight;
+            tell(top, weight, inv);
 #pragma unroll
             for (int i = 0; i < T::kBlocks; ++i) store(wave * T::kBlocks + i, mine_o[i], inv);
         } else {
@@ -662,7 +636,9 @@ attn_decode_kernel(const DecodeParams p)
                             x += f * w[k];
                         }
                     }
-                    store(b, x, all == 0.0f ? 0.0f : 1.0f / all);
+                    const float inv = all == 0.0f ? 0.0f : 1.0f / all;
+                    if (b == wave) tell(upto, all, inv);
+                    store(b, x, inv);
                 }
             }
         }
@@ -670,7 +646,6 @@ attn_decode_kernel(const DecodeParams p)
     }
 }
 
-int set_max_lds(const void* fn, size_t bytes);
 
 int check_attn(const codegemm_attn_desc* d)
 {
@@ -717,17 +692,26 @@ int decode_plan(const codegemm_kv_cache* cache, const codegemm_attn_desc* d, Dec
     return CODEGEMM_OK;
 }
 
-template <int TYPE, int DP, bool EXACT, bool NARROW>
-int launch_decode_one(DecodeParams& p, int groups, hipStream_t s)
+template <int TYPE, int DP, bool EXACT, bool NARROW, bool SUMS>
+int launch_decode_as(DecodeParams& p, int groups, hipStream_t s)
 {
     typedef DecodeStep<TYPE, DP, NARROW> T;
     static_assert(T::kLds * T::kPerCu <= kMaxLds, "LDS");
-    auto fn = attn_decode_kernel<TYPE, DP, EXACT, NARROW>;
+    auto fn = attn_decode_kernel<TYPE, DP, EXACT, NARROW, SUMS>;
     const int st = set_max_lds(reinterpret_cast<const void*>(fn), T::kLds);
     if (st) return st;
     p.slots = groups < kDecodeUnits * T::kPerCu ? groups : kDecodeUnits * T::kPerCu;
     hipLaunchKernelGGL(fn, dim3((unsigned)groups), dim3(T::kWaves * kWave), T::kLds, s, p);
     return hipGetLastError() == hipSuccess ? CODEGEMM_OK : CODEGEMM_LAUNCH_FAILED;
+}
+
+template <int TYPE, int DP, bool EXACT, bool NARROW>
+int launch_decode_one(DecodeParams& p, int groups, hipStream_t s)
+{
+    if constexpr (TYPE == CODEGEMM_KV_FP16) {
+        if (p.stats) return launch_decode_as<TYPE, DP, EXACT, NARROW, true>(p, groups, s);
+    }
+    return launch_decode_as<TYPE, DP, EXACT, NARROW, false>(p, groups, s);
 }
 
 template <int TYPE, int DP>
@@ -758,8 +742,10 @@ extern "C" size_t codegemm_attn_decode_workspace_bytes(const codegemm_kv_cache* 
     return decode_plan(cache, desc, &plan) ? 0 : plan.bytes;
 }
 
-extern "C" int codegemm_attn_decode(const codegemm_kv_cache* cache, const codegemm_attn_desc* desc, const void* q, void* out, void* workspace,
-                                    size_t workspace_bytes, void* stream)
+namespace cg {
+
+// stats: as the kernel leaves them, or NULL.
+int attn_decode(const codegemm_kv_cache* cache, const codegemm_attn_desc* desc, const void* q, void* out, Pair* stats, void* workspace, size_t workspace_bytes, void* stream)
 {
     DecodePlan plan;
     int st = decode_plan(cache, desc, &plan);
@@ -773,6 +759,7 @@ extern "C" int codegemm_attn_decode(const codegemm_kv_cache* cache, const codege
     p.out = static_cast<_Float16*>(out);
     p.counters = static_cast<uint32_t*>(workspace);
     p.part = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + (size_t)kCounterAreaWords * sizeof(uint32_t) + kPairAreaBytes);
+    p.stats = stats;
     p.r = plan.r;
     p.tiles = plan.tiles;
     p.q_stride = row_stride(desc->q_stride, desc->q_heads * desc->head_dim);
@@ -784,4 +771,12 @@ extern "C" int codegemm_attn_decode(const codegemm_kv_cache* cache, const codege
     if (cache->dtype == CODEGEMM_KV_INT8) return launch_decode_of<CODEGEMM_KV_INT8>(p, plan.narrow, plan.groups, s);
     if (cache->dtype == CODEGEMM_KV_INT4) return launch_decode_of<CODEGEMM_KV_INT4>(p, plan.narrow, plan.groups, s);
     return launch_decode_of<CODEGEMM_KV_FP8>(p, plan.narrow, plan.groups, s);
+}
+
+}  // namespace cg
+
+extern "C" int codegemm_attn_decode(const codegemm_kv_cache* cache, const codegemm_attn_desc* desc, const void* q, void* out, void* workspace,
+                                    size_t workspace_bytes, void* stream)
+{
+    return attn_decode(cache, desc, q, out, nullptr, workspace, workspace_bytes, stream);
 }
