@@ -443,6 +443,46 @@ int codegemm_kv_append_shifted(const codegemm_kv_cache *cache, const codegemm_ap
 int codegemm_kv_gather(const codegemm_kv_cache *cache, int32_t rows, const int32_t *cu_rows,
                        const int32_t *first, void *k_out, void *v_out, void *stream);
 
+/* Which tokens stay in a cache (host struct). */
+typedef struct codegemm_evict_desc {
+    int32_t budget;             /* tokens that a sequence keeps at most, >= 1                     */
+    int32_t keep_first;         /* of these the first ..                                          */
+    int32_t keep_last;          /* .. and the last ones of the sequence, whatever their scores;   */
+                                /* keep_first + keep_last <= budget                               */
+    int32_t max_kv;             /* keys of the longest sequence as far as the host knows, >= 1:   */
+                                /* how the work is split; longer ones are right all the same      */
+} codegemm_evict_desc;
+
+/*
+ * Eviction.  Of sequence i of the cache `from` every key head keeps, in their order, its
+ * first keep_first and last keep_last tokens and of those between the ones with the
+ * highest scores, so many that they are budget tokens together (all of a shorter
+ * sequence); equal scores: the lower position stays; a NaN is below all numbers.  They go
+ * to the positions 0, 1, .. of sequence i of `to`, the same for all heads in number,
+ * whatever tokens these are: keys keep the rotation that they have.
+ *   from, to    equal in kv_heads, head_dim, page_size, dtype, scale_block and num_seqs; the
+ *               same pools or others, but pages that `to` writes belong to no sequence of
+ *               `from`.  from->kv_lens counts; to->kv_lens is not read.
+ *   scores      [from->num_pages][kv_heads][page_size] fp32 (codegemm_attn_scores)
+ *   shift       [num_seqs] int32 or NULL: tokens that sequence i has lost already
+ *   to_scores   [to->num_pages][kv_heads][page_size] fp32 or NULL: the kept tokens' scores
+ *               (may be `scores` where the pools are the same)
+ *   to_lens     [num_seqs] int32: the tokens of sequence i that are kept (may be to->kv_lens, and
+ *               from->kv_lens)
+ *   to_shift    [num_seqs] int32 or NULL (may be shift): shift[i] (0) + kv_lens[i] -
+ *               to_lens[i], for codegemm_kv_append_shifted
+ * Positions without a page hold no token.  Kept tokens whose place in `to` has no page are
+ * lost.  Codes, scales and offsets are moved as they are, but for 8 bits with several
+ * tokens to a scale: a block gets the largest scale s of the tokens that come into it,
+ * and the codes c of others become round(c * s_old / s).  Other places of `to` stay as they
+ * are.  workspace: as for codegemm_gemm; num_seqs * kv_heads < 2^22.
+ */
+size_t codegemm_kv_evict_workspace_bytes(const codegemm_kv_cache *from, const codegemm_evict_desc *desc);
+int codegemm_kv_evict(const codegemm_kv_cache *from, const codegemm_kv_cache *to,
+                      const codegemm_evict_desc *desc, const float *scores, const int32_t *shift,
+                      float *to_scores, int32_t *to_lens, int32_t *to_shift, void *workspace,
+                      size_t workspace_bytes, void *stream);
+
 enum {
     CODEGEMM_ATTN_CAUSAL = 1        /* codegemm_attn_prompt: keys up to the query's own position */
 };

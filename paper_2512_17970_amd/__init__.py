@@ -15,7 +15,7 @@ from .binding import (  # noqa: F401
     codegemm_gemm_static, codegemm_static_workspace_limit,
     GroupMember, codegemm_gemm_grouped, codegemm_grouped_workspace_bytes,
     KV_FP16, KV_INT8, KV_FP8, KV_INT4, KvCache, codegemm_kv_pool_bytes, codegemm_kv_scales_bytes, AppendDesc, codegemm_kv_append,
-    codegemm_kv_append_shifted, codegemm_kv_gather,
+    codegemm_kv_append_shifted, codegemm_kv_gather, EvictDesc, codegemm_kv_evict, codegemm_kv_evict_workspace_bytes,
     AttnDesc, codegemm_attn_decode, codegemm_attn_decode_workspace_bytes,
     codegemm_attn_scores, codegemm_attn_scores_workspace_bytes, codegemm_attn_decode_scores, codegemm_attn_decode_scores_workspace_bytes,
     codegemm_attn_prompt, codegemm_attn_prompt_workspace_bytes,

@@ -38,6 +38,7 @@ EXPORTS = [
     "codegemm_gemm_static", "codegemm_static_workspace_limit",
     "codegemm_gemm_grouped", "codegemm_grouped_workspace_bytes",
     "codegemm_kv_pool_bytes", "codegemm_kv_scales_bytes", "codegemm_kv_append", "codegemm_kv_append_shifted", "codegemm_kv_gather",
+    "codegemm_kv_evict", "codegemm_kv_evict_workspace_bytes",
     "codegemm_attn_decode", "codegemm_attn_decode_workspace_bytes", "codegemm_attn_scores", "codegemm_attn_scores_workspace_bytes",
     "codegemm_attn_decode_scores", "codegemm_attn_decode_scores_workspace_bytes", "codegemm_attn_prompt", "codegemm_attn_prompt_workspace_bytes",
 ]
@@ -129,6 +130,15 @@ class AttnDesc(ctypes.Structure):
                    q_stride, k_stride, v_stride, out_stride)
 
 
+class EvictDesc(ctypes.Structure):
+    """codegemm_evict_desc"""
+    _fields_ = [("budget", ctypes.c_int32), ("keep_first", ctypes.c_int32), ("keep_last", ctypes.c_int32), ("max_kv", ctypes.c_int32)]
+
+    @classmethod
+    def make(cls, budget: int, *, keep_first: int = 0, keep_last: int = 0, max_kv: int):
+        return cls(budget, keep_first, keep_last, max_kv)
+
+
 def lib_path() -> str:
     return _LIB_PATH
 
@@ -197,6 +207,11 @@ def load() -> ctypes.CDLL:
     lib.codegemm_kv_append_shifted.restype = i
     lib.codegemm_kv_gather.argtypes = [cp, i32, vp, vp, vp, vp, vp]
     lib.codegemm_kv_gather.restype = i
+    ep = ctypes.POINTER(EvictDesc)
+    lib.codegemm_kv_evict_workspace_bytes.argtypes = [cp, ep]
+    lib.codegemm_kv_evict_workspace_bytes.restype = sz
+    lib.codegemm_kv_evict.argtypes = [cp, cp, ep, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.codegemm_kv_evict.restype = i
     lib.codegemm_attn_decode_workspace_bytes.argtypes = [cp, tp]
     lib.codegemm_attn_decode_workspace_bytes.restype = sz
     lib.codegemm_attn_decode.argtypes = [cp, tp, vp, vp, vp, sz, vp]
@@ -373,6 +388,15 @@ def codegemm_kv_append_shifted(cache: KvCache, desc: AppendDesc, cu_seqlens, shi
 def _kv_gather(cache: KvCache, rows: int, cu_rows, first, k_out, v_out, stream: int = 0) -> None:
     _check(load().codegemm_kv_gather(ctypes.byref(cache), rows, _ptr(cu_rows), _ptr(first), _ptr(k_out), _ptr(v_out), stream),
            "codegemm_kv_gather")
+
+
+def codegemm_kv_evict_workspace_bytes(source: KvCache, desc: EvictDesc) -> int:
+    return int(load().codegemm_kv_evict_workspace_bytes(ctypes.byref(source), ctypes.byref(desc)))
+
+
+def codegemm_kv_evict(source: KvCache, to: KvCache, desc: EvictDesc, scores, shift, to_scores, to_lens, to_shift, workspace, workspace_bytes: int, stream: int = 0) -> None:
+    _check(load().codegemm_kv_evict(ctypes.byref(source), ctypes.byref(to), ctypes.byref(desc), _ptr(scores), _ptr(shift), _ptr(to_scores), _ptr(to_lens),
+                                    _ptr(to_shift), _ptr(workspace), workspace_bytes, stream), "codegemm_kv_evict")
 
 
 def codegemm_attn_decode_workspace_bytes(cache: KvCache, desc: AttnDesc) -> int:

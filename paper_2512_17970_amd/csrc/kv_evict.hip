@@ -1,0 +1,455 @@
+// Eviction: of every sequence and key head the tokens with the highest scores go, in order, to pages of another table.
+//
+// Selecting: a workgroup for a sequence and key head looks for the lowest score that stays, digit by digit of its bits (11, 11 and 10) from the top, with a
+// histogram in LDS; scores are there too, up to kKeptKeys of them.  Then it writes down the positions that stay, each wavefront a stretch of them behind those of
+// the wavefronts before it.
+// Moving: a workgroup takes 64 places of a head (or a block's, where those are more), keys or values.  Keys are rows; a value's row holds 16 tokens of a
+// dimension, so a lane picks its dimension's codes out of up to 16 rows, which are the same for the whole wavefront.
+#include "attn_common.h"
+
+namespace cg {
+
+constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / kWave;
+constexpr int kKeptKeys = 32768;            // 128 KB, at most
+constexpr int kBins = 2048;
+constexpr int kMoveThreads = 256;
+constexpr int kMoveTokens = 64;
+
+struct EvictParams {
+    CacheView from, to;
+    const float* scores;
+    float* to_scores;
+    const int32_t* shift;
+    int32_t *to_lens, *to_shift;
+    int32_t* list;          // [sequence][head][most]: positions that stay
+    int2* info;             // [sequence][head]: tokens that stay, the sequence's length
+    int budget, first, last, most;
+    int kept_keys;          // in LDS, a multiple of 4
+    int unit;               // places of a workgroup that moves
+    int units;              // .. of a sequence
+};
+
+// Scores as numbers that order as they do: NaN below all, -0 as 0.  0 is for what is no candidate.
+__device__ __forceinline__ uint32_t key_of(float score)
+{
+    const uint32_t w = __builtin_bit_cast(uint32_t, score + 0.0f);
+    const uint32_t k = w & 0x80000000u ? ~w : w | 0x80000000u;
+    return score == score ? k : 1u;
+}
+
+__global__ void __launch_bounds__(kSelectThreads) kv_select_kernel(const EvictParams p)
+{
+    extern __shared__ __align__(16) unsigned char smem[];
+    uint32_t* kept_keys = reinterpret_cast<uint32_t*>(smem);                            // [p.kept_keys]
+    uint32_t* bins = kept_keys + p.kept_keys;                                           // [kBins]
+    uint32_t* shared = bins + kBins;                                                    // [2 kSelectWaves]
+    const CacheView& c = p.from;
+    const int seq = blockIdx.x / c.Hk, head = blockIdx.x % c.Hk;
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    const int held = c.max_pages << c.page_shift, given = c.lens[seq], len = given < 0 ? 0 : given, n = len < held ? len : held;
+    const int last = len > p.last ? len - p.last : 0;                                   // the last tokens' first position
+    int32_t* list = p.list + ((size_t)seq * c.Hk + head) * p.most;
+
+    // The four tokens from t on (a multiple of 4): their keys; ~0 for those that stay whatever they have, 0 for those that are none.
+    auto look = [&](int t) {
+        u32x4_t k = {0, 0, 0, 0};
+        if (t >= n) return k;
+        const int page = page_of(c, seq, t >> c.page_shift);
+        if (page < 0) return k;
+        const float4_t x = *reinterpret_cast<const float4_t*>(p.scores + ((((size_t)page * c.Hk + head) << c.page_shift) + (t & ((1 << c.page_shift) - 1))));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const bool always = t + i < p.first || t + i >= last;
+            k[i] = t + i >= n ? 0u : always ? ~0u : key_of(x[i]);
+        }
+        return k;
+    };
+    auto keys_at = [&](int t) {
+        if (t + 4 <= p.kept_keys) return *reinterpret_cast<const u32x4_t*>(kept_keys + t);
+        return look(t);
+    };
+    auto total = [&](unsigned x) {                                                      // over the workgroup
+        for (int o = 1; o < kWave; o <<= 1) x += (unsigned)__shfl_xor((int)x, o);
+        __syncthreads();
+        if (lane == 0) shared[wave] = x;
+        __syncthreads();
+        unsigned sum = 0;
+        for (int w = 0; w < kSelectWaves; ++w) sum += shared[w];
+        return sum;
+    };
+
+    // Those that stay anyhow, and those there are.
+    unsigned always = 0, there = 0;
+    for (int t = 4 * tid; t < n; t += 4 * kSelectThreads) {
+        const u32x4_t k = look(t);
+        if (t + 4 <= p.kept_keys) *reinterpret_cast<u32x4_t*>(kept_keys + t) = k;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { always += k[i] == ~0u; there += k[i] != 0u; }
+    }
+    always = total(always);
+    there = total(there);
+    // The keys above `least` stay, and of those that are it the first `equal`.
+    uint32_t least = 0;
+    unsigned equal = 0;
+    if (there > (unsigned)p.budget) {
+        unsigned room = (unsigned)p.budget - always;
+        uint32_t prefix = 0, mask = 0;
+        if (room == 0) least = ~0u - 1;                                                 // (no candidate's key is that)
+        else {
+#pragma unroll
+            for (int digit = 0; digit < 3; ++digit) {
+                const int at = digit == 0 ? 21 : digit == 1 ? 10 : 0, width = digit == 2 ? 10 : 11;
+                __syncthreads();
+                for (int i = tid; i < kBins; i += kSelectThreads) bins[i] = 0;
+                __syncthreads();
+                for (int t = 4 * tid; t < n; t += 4 * kSelectThreads) {
+                    const u32x4_t k = keys_at(t);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (k[i] != 0u && k[i] != ~0u && (k[i] & mask) == prefix) atomicAdd(&bins[k[i] >> at & ((1u << width) - 1)], 1u);
+                }
+                __syncthreads();
+                // the bin in which the room ends, from the top: thread i has bins 2 i and 2 i + 1 from the top
+                const int b0 = kBins - 1 - 2 * tid;
+                const unsigned c0 = bins[b0], c1 = bins[b0 - 1];
+                unsigned upto = c0 + c1;
+                for (int o = 1; o < kWave; o <<= 1) {
+                    const unsigned x = (unsigned)__shfl_up((int)upto, o);
+                    upto += lane >= o ? x : 0u;
+                }
+                if (lane == kWave - 1) shared[wave] = upto;
+                __syncthreads();
+                for (int w = 0; w < wave; ++w) upto += shared[w];
+                const unsigned before = upto - c0 - c1;
+                if (before < room && room <= upto) {                                    // one thread
+                    const bool second = room > before + c0;
+                    shared[kSelectWaves] = (uint32_t)(second ? b0 - 1 : b0);
+                    shared[kSelectWaves + 1] = room - before - (second ? c0 : 0u);
+                }
+                __syncthreads();
+                prefix |= shared[kSelectWaves] << at;
+                room = shared[kSelectWaves + 1];
+                mask |= ((1u << width) - 1) << at;
+            }
+            least = prefix;
+            equal = room;
+        }
+    }
+    // Each wavefront's stretch: how many are above, and are, the least; then their places.
+    const int stretch = ceil_div(ceil_div(n, 4 * kWave), kSelectWaves) * 4 * kWave, begin = wave * stretch, end = begin + stretch < n ? begin + stretch : n;
+    unsigned above = 0, same = 0;
+    for (int t = begin + 4 * lane; t < end; t += 4 * kWave) {
+        const u32x4_t k = keys_at(t);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { above += k[i] > least; same += least != 0u && k[i] == least; }
+    }
+    for (int o = 1; o < kWave; o <<= 1) { above += (unsigned)__shfl_xor((int)above, o); same += (unsigned)__shfl_xor((int)same, o); }
+    __syncthreads();
+    if (lane == 0) { shared[wave] = above; shared[kSelectWaves + wave] = same; }
+    __syncthreads();
+    unsigned places = 0, sames = 0, all = 0;                                            // of the wavefronts before this one; of all
+    {
+        unsigned seen = 0;
+        for (int w = 0; w < kSelectWaves; ++w) {
+            const unsigned a = shared[w], s = shared[kSelectWaves + w], taken = seen >= equal ? 0u : equal - seen < s ? equal - seen : s;
+            if (w == wave) { places = all; sames = seen; }
+            all += a + taken;
+            seen += s;
+        }
+    }
+    for (int t0 = begin; t0 < end; t0 += 4 * kWave) {
+        const int t = t0 + 4 * lane;
+        u32x4_t k = {0, 0, 0, 0};
+        if (t < end) k = keys_at(t);
+        unsigned s4 = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s4 += least != 0u && k[i] == least;
+        auto upto = [&](unsigned x) {                                                   // over the wavefront, up to the lane
+            for (int o = 1; o < kWave; o <<= 1) {
+                const unsigned y = (unsigned)__shfl_up((int)x, o);
+                x += lane >= o ? y : 0u;
+            }
+            return x;
+        };
+        const unsigned s_upto = upto(s4);
+        unsigned s_before = sames + s_upto - s4, stays = 0;
+        bool stay[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const bool is_same = least != 0u && k[i] == least;
+            stay[i] = k[i] > least || (is_same && s_before < equal);
+            s_before += is_same;
+            stays += stay[i];
+        }
+        const unsigned p_upto = upto(stays);
+        unsigned at = places + p_upto - stays;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (stay[i] && at < (unsigned)p.most) list[at] = t + i;
+            at += stay[i];
+        }
+        places += (unsigned)__builtin_amdgcn_readlane((int)p_upto, kWave - 1);
+        sames += (unsigned)__builtin_amdgcn_readlane((int)s_upto, kWave - 1);
+    }
+    if (tid == 0) p.info[(size_t)seq * c.Hk + head] = int2{(int)all, len};
+}
+
+// 8 bits: a code in another scale.
+template <int TYPE>
+__device__ __forceinline__ uint32_t again(uint32_t code, float ratio)
+{
+    if constexpr (TYPE == CODEGEMM_KV_INT8) return (uint32_t)(uint8_t)(int8_t)(int)rintf(__builtin_amdgcn_fmed3f((float)(int8_t)code * ratio, -127.0f, 127.0f));
+    else {
+        const float x = __builtin_amdgcn_fmed3f((float)__builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)code, 1.0f, false)[0] * ratio, -448.0f, 448.0f);
+        return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x, x, 0, false) & 255u;
+    }
+}
+
+// The four bits of token j of a word's eight.
+__device__ __forceinline__ constexpr int bit_of(int j) { return 4 * (j >> 1) + 16 * (j & 1); }
+
+// Units of places of a sequence and key head, keys or values.
+template <int TYPE>
+__global__ void __launch_bounds__(kMoveThreads) kv_move_kernel(const EvictParams p)
+{
+    constexpr bool FOUR = TYPE == CODEGEMM_KV_INT4, SCALED = TYPE == CODEGEMM_KV_INT8 || TYPE == CODEGEMM_KV_FP8;
+    __shared__ int2 source[kMoveThreads];                       // [token]: page and slot
+    __shared__ float old[kMoveThreads];                         // [token]: its scale so far
+    __shared__ uint32_t largest[kMoveThreads];                  // [block]: the bits of its scale
+    const CacheView &a = p.from, &b = p.to;
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave), D = a.D;
+    const int head = blockIdx.x % a.Hk, item = blockIdx.x / a.Hk, seq = item / p.units;
+    const bool values = blockIdx.y != 0;
+    const int2 info = p.info[(size_t)seq * a.Hk + head];
+    if (item % p.units == 0 && head == 0 && !values && tid == 0) {
+        p.to_lens[seq] = info.x;
+        if (p.to_shift) p.to_shift[seq] = (p.shift ? p.shift[seq] : 0) + info.y - info.x;
+    }
+    const int mask = (1 << a.page_shift) - 1;
+    for (int unit = item % p.units;; unit += p.units) {
+        const int first = unit * p.unit, count = info.x - first < p.unit ? info.x - first : p.unit;
+        if (count <= 0) return;
+        __syncthreads();
+        if (tid < p.unit) largest[tid] = 0;
+        __syncthreads();
+        if (tid < count) {
+            const int t = p.list[((size_t)seq * a.Hk + head) * p.most + first + tid], page = page_of(a, seq, t >> a.page_shift), slot = t & mask;       // (there is a page)
+            source[tid] = int2{page, slot};
+            if constexpr (SCALED) {
+                const float s = (values ? a.v_scales : a.k_scales)[scales_at(a, page, head) + (slot >> a.block_shift)];
+                old[tid] = s;
+                atomicMax(&largest[tid >> a.block_shift], __builtin_bit_cast(uint32_t, s));         // (bits order as scales do, a NaN above all)
+            }
+            if (!values && p.to_scores) {
+                const int to = page_of(b, seq, (first + tid) >> b.page_shift);
+                if (to >= 0)
+                    p.to_scores[(((size_t)to * b.Hk + head) << b.page_shift) + ((first + tid) & mask)] = p.scores[(((size_t)page * a.Hk + head) << a.page_shift) + slot];
+            }
+        }
+        __syncthreads();
+        auto ratio_of = [&](int token) {                        // 1: codes stay
+            const float s = old[token], now = __builtin_bit_cast(float, largest[token >> a.block_shift]);
+            return s == now ? 1.0f : s > 0.0f && s < now ? s / now : 0.0f;
+        };
+        if constexpr (SCALED) {
+            const int block = tid << b.block_shift, to = block < count ? page_of(b, seq, (first + block) >> b.page_shift) : -1;
+            if (to >= 0) (values ? b.v_scales : b.k_scales)[scales_at(b, to, head) + (((first + block) & mask) >> b.block_shift)] = __builtin_bit_cast(float, largest[tid]);
+        }
+        if (!values) {
+            const int pieces = TYPE == CODEGEMM_KV_FP16 ? D / 8 : FOUR ? D / 32 : D / 16;           // of 16 bytes, of a token
+            constexpr int AT_ONCE = 4;
+            for (int i0 = tid; i0 < count * pieces; i0 += AT_ONCE * kMoveThreads) {
+                u32x4_t x[AT_ONCE];
+#pragma unroll
+                for (int k = 0; k < AT_ONCE; ++k) {
+                    const int i = i0 + k * kMoveThreads, token = i / pieces;
+                    if (i < count * pieces) x[k] = reinterpret_cast<const u32x4_t*>(a.k)[((((size_t)source[token].x * a.Hk + head) << a.page_shift) + source[token].y) * pieces + i % pieces];
+                }
+#pragma unroll
+                for (int k = 0; k < AT_ONCE; ++k) {
+                    const int i = i0 + k * kMoveThreads, token = i / pieces, t = first + token;
+                    const int to = i < count * pieces ? page_of(b, seq, t >> b.page_shift) : -1;
+                    if (to < 0) continue;
+                    if constexpr (SCALED) {
+                        const float ratio = ratio_of(token);
+                        if (ratio != 1.0f) {
+#pragma unroll
+                            for (int w = 0; w < 4; ++w) {
+                                uint32_t y = 0;
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) y |= again<TYPE>(x[k][w] >> (8 * e) & 255u, ratio) << (8 * e);
+                                x[k][w] = y;
+                            }
+                        }
+                    }
+                    reinterpret_cast<u32x4_t*>(b.k)[((((size_t)to * b.Hk + head) << b.page_shift) + (t & mask)) * pieces + i % pieces] = x[k];
+                }
+            }
+            if constexpr (FOUR) {
+                for (int i = tid; i < count * a.runs; i += kMoveThreads) {
+                    const int token = i / a.runs, run = i % a.runs, t = first + token, to = page_of(b, seq, t >> b.page_shift);
+                    if (to >= 0)
+                        reinterpret_cast<uint32_t*>(b.k_scales)[runs_at(b, to, head, t & mask) + run] =
+                            reinterpret_cast<const uint32_t*>(a.k_scales)[runs_at(a, source[token].x, head, source[token].y) + run];
+                }
+            }
+            continue;
+        }
+        for (int group = wave; 16 * group < count; group += kMoveThreads / kWave) {
+            const int t = first + 16 * group, here = count - 16 * group < 16 ? count - 16 * group : 16;
+            const int to = __builtin_amdgcn_readfirstlane(page_of(b, seq, t >> b.page_shift));
+            if (to < 0) continue;
+            int2 from[16];                                      // of the group's tokens; the same for all lanes
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const int2 s = source[16 * group + (j < here ? j : 0)];
+                from[j] = int2{__builtin_amdgcn_readfirstlane(s.x), __builtin_amdgcn_readfirstlane(s.y)};
+            }
+            const size_t at = page_at(b, to, head) + (size_t)(t & mask) * D;
+            auto row = [&](int j) { return page_at(a, from[j].x, head) + (size_t)(from[j].y & ~15) * D; };
+            for (int d = lane; d < D; d += kWave) {
+                if constexpr (FOUR) {
+                    uint32_t x[16], w[2] = {0, 0}, taken[2] = {0, 0};
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) x[j] = reinterpret_cast<const uint32_t*>(a.v + row(j) / 2)[2 * d + (from[j].y >> 3 & 1)];
+#pragma unroll
+                    for (int j = 0; j < 16; ++j)
+                        if (j < here) {
+                            w[j >> 3] |= (x[j] >> bit_of(from[j].y & 7) & 15u) << bit_of(j & 7);
+                            taken[j >> 3] |= 15u << bit_of(j & 7);
+                        }
+                    u32x2_t* dst = reinterpret_cast<u32x2_t*>(b.v + at / 2) + d;
+                    if (here < 16) {
+                        const u32x2_t was = *dst;
+                        w[0] |= was[0] & ~taken[0];
+                        w[1] |= was[1] & ~taken[1];
+                    }
+                    *dst = u32x2_t{w[0], w[1]};
+                } else if constexpr (SCALED) {
+                    uint32_t x[16];
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) x[j] = a.v[row(j) + (size_t)d * 16 + (from[j].y & 15)];
+                    u32x4_t* dst = reinterpret_cast<u32x4_t*>(b.v + at) + d;
+                    u32x4_t w = {0, 0, 0, 0};
+                    if (here < 16) w = *dst;
+#pragma unroll
+                    for (int j = 0; j < 16; ++j)
+                        if (j < here) {
+                            const float ratio = ratio_of(16 * group + j);
+                            const uint32_t code = ratio == 1.0f ? x[j] : again<TYPE>(x[j], ratio);
+                            w[j >> 2] = (w[j >> 2] & ~(255u << (8 * (j & 3)))) | code << (8 * (j & 3));
+                        }
+                    *dst = w;
+                } else {
+                    uint32_t x[16];
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) x[j] = reinterpret_cast<const uint16_t*>(a.v)[row(j) + (size_t)d * 16 + (from[j].y & 15)];
+                    u32x4_t* dst = reinterpret_cast<u32x4_t*>(reinterpret_cast<uint16_t*>(b.v) + at) + 2 * d;
+                    u32x4_t w[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+                    if (here < 16) { w[0] = dst[0]; w[1] = dst[1]; }
+#pragma unroll
+                    for (int j = 0; j < 16; ++j)
+                        if (j < here) w[j >> 3][j / 2 & 3] = j & 1 ? (w[j >> 3][j / 2 & 3] & 0xffffu) | x[j] << 16 : (w[j >> 3][j / 2 & 3] & 0xffff0000u) | x[j];
+                    dst[0] = w[0];
+                    dst[1] = w[1];
+                }
+            }
+        }
+        if constexpr (FOUR) {
+            for (int i = tid; i < count * a.runs; i += kMoveThreads) {
+                const int token = i / a.runs, run = i % a.runs, t = first + token, to = page_of(b, seq, t >> b.page_shift), slot = source[token].y;
+                if (to < 0) continue;
+                const uint16_t* src = reinterpret_cast<const uint16_t*>(a.v_scales) + 2 * runs_at(a, source[token].x, head, slot & ~15) + 32 * run + (slot & 15);
+                uint16_t* dst = reinterpret_cast<uint16_t*>(b.v_scales) + 2 * runs_at(b, to, head, t & mask & ~15) + 32 * run + (t & 15);
+                dst[0] = src[0];
+                dst[16] = src[16];
+            }
+        }
+    }
+}
+
+namespace {
+
+constexpr size_t kFixedArea = (size_t)kCounterAreaWords * sizeof(uint32_t) + kPairAreaBytes;       // that other calls keep their counters in
+
+struct EvictPlan {
+    int most, unit, units, kept_keys;
+    size_t info, bytes;
+};
+
+int evict_plan(const codegemm_kv_cache* from, const codegemm_evict_desc* d, EvictPlan* p)
+{
+    const int st = check_cache(from, false);
+    if (st) return st;
+    if (!d || d->budget < 1 || d->keep_first < 0 || d->keep_last < 0 || (long long)d->keep_first + d->keep_last > d->budget || d->max_kv < 1) return CODEGEMM_INVALID_ARG;
+    const long long items = (long long)from->num_seqs * from->kv_heads;
+    if (too_many(items, kSelectThreads)) return CODEGEMM_UNSUPPORTED;
+    const int held = from->max_pages * from->page_size, known = d->max_kv < held ? d->max_kv : held;
+    p->most = d->budget < held ? d->budget : held;
+    const bool scaled = from->dtype == CODEGEMM_KV_INT8 || from->dtype == CODEGEMM_KV_FP8;
+    p->unit = scaled && from->scale_block > kMoveTokens ? from->scale_block : kMoveTokens;
+    const int kept = p->most < known ? p->most : known;
+    p->units = ceil_div(kept, p->unit);
+    // (whatever the host knows: fewer workgroups have more units each)
+    const long long room = 0xffffffffll / kMoveThreads / items;
+    if (p->units > room) p->units = (int)room;
+    p->kept_keys = known < kKeptKeys ? ceil_div(known, 4) * 4 : kKeptKeys;
+    p->info = kFixedArea + ((size_t)items * p->most * sizeof(int32_t) + 255) / 256 * 256;
+    p->bytes = p->info + (size_t)items * sizeof(int2);
+    return CODEGEMM_OK;
+}
+
+template <int TYPE>
+void launch_move(const EvictParams& p, hipStream_t s)
+{
+    hipLaunchKernelGGL(kv_move_kernel<TYPE>, dim3((unsigned)p.units * (unsigned)(p.from.seqs * p.from.Hk), 2), dim3(kMoveThreads), 0, s, p);
+}
+
+}  // namespace
+}  // namespace cg
+
+using namespace cg;
+
+extern "C" size_t codegemm_kv_evict_workspace_bytes(const codegemm_kv_cache* from, const codegemm_evict_desc* desc)
+{
+    EvictPlan plan;
+    return evict_plan(from, desc, &plan) ? 0 : plan.bytes;
+}
+
+extern "C" int codegemm_kv_evict(const codegemm_kv_cache* from, const codegemm_kv_cache* to, const codegemm_evict_desc* desc, const float* scores, const int32_t* shift,
+                                 float* to_scores, int32_t* to_lens, int32_t* to_shift, void* workspace, size_t workspace_bytes, void* stream)
+{
+    EvictPlan plan;
+    int st = evict_plan(from, desc, &plan);
+    if (!st) st = check_cache(from, true);
+    if (!st) st = check_cache(to, true);
+    if (st) return st;
+    if (from->kv_heads != to->kv_heads || from->head_dim != to->head_dim || from->page_size != to->page_size || from->dtype != to->dtype || from->num_seqs != to->num_seqs ||
+        (from->dtype != CODEGEMM_KV_FP16 && from->scale_block != to->scale_block))
+        return CODEGEMM_INVALID_ARG;
+    if (!scores || !to_lens || !workspace || misaligned(scores) || misaligned(workspace) || (to_scores && misaligned(to_scores))) return CODEGEMM_INVALID_ARG;
+    if (misaligned_ints(to_lens) || (shift && misaligned_ints(shift)) || (to_shift && misaligned_ints(to_shift))) return CODEGEMM_INVALID_ARG;
+    if (workspace_bytes < plan.bytes) return CODEGEMM_WORKSPACE_TOO_SMALL;
+    EvictParams p;
+    p.from = cache_view(*from);
+    p.to = cache_view(*to);
+    p.scores = scores;
+    p.to_scores = to_scores;
+    p.shift = shift;
+    p.to_lens = to_lens;
+    p.to_shift = to_shift;
+    p.list = reinterpret_cast<int32_t*>(static_cast<unsigned char*>(workspace) + kFixedArea);
+    p.info = reinterpret_cast<int2*>(static_cast<unsigned char*>(workspace) + plan.info);
+    p.budget = desc->budget; p.first = desc->keep_first; p.last = desc->keep_last;
+    p.most = plan.most; p.kept_keys = plan.kept_keys; p.unit = plan.unit; p.units = plan.units;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const size_t lds = ((size_t)plan.kept_keys + kBins + 2 * kSelectWaves) * sizeof(uint32_t);
+    st = set_max_lds(reinterpret_cast<const void*>(kv_select_kernel), lds);
+    if (st) return st;
+    hipLaunchKernelGGL(kv_select_kernel, dim3((unsigned)(p.from.seqs * p.from.Hk)), dim3(kSelectThreads), lds, s, p);
+    if (from->dtype == CODEGEMM_KV_FP16) launch_move<CODEGEMM_KV_FP16>(p, s);
+    else if (from->dtype == CODEGEMM_KV_INT8) launch_move<CODEGEMM_KV_INT8>(p, s);
+    else if (from->dtype == CODEGEMM_KV_INT4) launch_move<CODEGEMM_KV_INT4>(p, s);
+    else launch_move<CODEGEMM_KV_FP8>(p, s);
+    return hipGetLastError() == hipSuccess ? CODEGEMM_OK : CODEGEMM_LAUNCH_FAILED;
+}
