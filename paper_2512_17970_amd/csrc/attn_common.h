@@ -118,33 +118,40 @@ __device__ __forceinline__ Pair get8(__amdgpu_buffer_rsrc_t parts, int at)
 
 // 4 bits: eight codes of a word, code j in bits 4 (j / 2) + 16 (j % 2), so that shifts by whole words and one mask leave consecutive codes in the two
 // halves, at the place of the four leading mantissa bits: with the exponent of 16 that is 16 + code in fp16, and one packed multiply-add makes the values.
-__device__ __forceinline__ half2_t code_pair(uint32_t w, int i)
+// (The mask in a vector register: an instruction takes one constant, and mask and exponent are one instruction then.)
+__device__ __forceinline__ uint32_t code_mask()
+{
+    uint32_t m = 0x03c003c0u;
+    asm("" : "+v"(m));
+    return m;
+}
+__device__ __forceinline__ half2_t code_pair(uint32_t w, int i, uint32_t mask)
 {
     const uint32_t at = i == 0 ? w << 6 : i == 1 ? w << 2 : i == 2 ? w >> 2 : w >> 6;
-    return __builtin_bit_cast(half2_t, (at & 0x03c003c0u) | 0x4c004c00u);
+    return __builtin_bit_cast(half2_t, (at & mask) | 0x4c004c00u);
 }
 __device__ __forceinline__ half2_t halves_of(uint32_t w) { return __builtin_bit_cast(half2_t, w); }
 __device__ __forceinline__ half2_t both_low(uint32_t w) { return halves_of(__builtin_amdgcn_perm(w, w, 0x01000100u)); }
 __device__ __forceinline__ half2_t both_high(uint32_t w) { return halves_of(__builtin_amdgcn_perm(w, w, 0x03020302u)); }
 // .. of one scale and offset (a key's run of dimensions)
-__device__ __forceinline__ half8_t four_bits(uint32_t w, half2_t scale, half2_t offset)
+__device__ __forceinline__ half8_t four_bits(uint32_t w, half2_t scale, half2_t offset, uint32_t mask)
 {
     half8_t x;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const half2_t y = __builtin_elementwise_fma(code_pair(w, i), scale, offset);
+        const half2_t y = __builtin_elementwise_fma(code_pair(w, i, mask), scale, offset);
         x[2 * i] = y[0];
         x[2 * i + 1] = y[1];
     }
     return x;
 }
 // .. of eight (values of eight tokens)
-__device__ __forceinline__ half8_t four_bits(uint32_t w, const u32x4_t& scale, const u32x4_t& offset)
+__device__ __forceinline__ half8_t four_bits(uint32_t w, const u32x4_t& scale, const u32x4_t& offset, uint32_t mask)
 {
     half8_t x;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const half2_t y = __builtin_elementwise_fma(code_pair(w, i), halves_of(scale[i]), halves_of(offset[i]));
+        const half2_t y = __builtin_elementwise_fma(code_pair(w, i, mask), halves_of(scale[i]), halves_of(offset[i]));
         x[2 * i] = y[0];
         x[2 * i + 1] = y[1];
     }

@@ -76,7 +76,10 @@ struct DecodeStep {
     static constexpr int kRequests = 2 * kPart / 1024 + (kHalf ? 0 : kFour ? kScaleBytes / 1024 : 1);
     static constexpr int kStages = 2;
     static constexpr int kPerCu = NARROW && kBytes <= 20 * 1024 ? 2 : 1;
-    static constexpr int kWaves = (kBytes > 20 * 1024 ? 2 : kBytes > 9 * 1024 ? 4 : 8) / kPerCu;
+#ifndef W4
+#define W4 8
+#endif
+    static constexpr int kWaves = (kBytes > 20 * 1024 ? 2 : kBytes > 9 * 1024 ? 4 : kFour ? W4 : 8) / kPerCu;
     static constexpr int kRing = kWaves * kStages * kBytes;
     static constexpr int kSums = kWaves * kDecodeRows * 8;           // the wavefronts' maxima and weights
     static constexpr int kLds = kRing + kSums + 16;
@@ -137,7 +140,7 @@ __device__ __forceinline__ void request4(uint32_t lds, const float* from)
 // TYPE: of the cache.  DP: head_dim rounded up to 64, 128 or 256; EXACT: it is head_dim.
 // SUMS: of weights as they are, not as they are rounded, also in fp16 (there are `stats`).
 template <int TYPE, int DP, bool EXACT, bool NARROW, bool SUMS>
-__global__ void __launch_bounds__((DecodeStep<TYPE, DP, NARROW>::kWaves * kWave), (DecodeStep<TYPE, DP, NARROW>::kWaves * DecodeStep<TYPE, DP, NARROW>::kPerCu > 4 ? 2 : 1))
+__global__ void __launch_bounds__((DecodeStep<TYPE, DP, NARROW>::kWaves * kWave), (DecodeStep<TYPE, DP, NARROW>::kWaves * DecodeStep<TYPE, DP, NARROW>::kPerCu > 8 ? 3 : DecodeStep<TYPE, DP, NARROW>::kWaves * DecodeStep<TYPE, DP, NARROW>::kPerCu > 4 ? 2 : 1))
 attn_decode_kernel(const DecodeParams p)
 {
     typedef DecodeStep<TYPE, DP, NARROW> T;
@@ -188,6 +191,7 @@ attn_decode_kernel(const DecodeParams p)
     if (longest <= most + kJoinSteps * NW) most = longest;
 
     const_int* table = (const_int*)(uintptr_t)cv.table;
+    const uint32_t codes_at = T::kFour ? code_mask() : 0u;
 
     // where the lane's own operands lie in a stage
     const uint32_t ring = lds0 + (uint32_t)(wave * T::kStages * T::kBytes);
@@ -376,7 +380,7 @@ attn_decode_kernel(const DecodeParams p)
                         }
 #pragma unroll
                         for (int a = 0; a < kEach; ++a) {
-                            half8_t kf = four_bits(w[a], scale, offset);
+                            half8_t kf = four_bits(w[a], scale, offset, codes_at);
                             if (!EXACT && !in) kf = half8_t{0, 0, 0, 0, 0, 0, 0, 0};
                             s[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[kEach * j + a], s[n], 0, 0, 0);
                         }
@@ -487,7 +491,7 @@ attn_decode_kernel(const DecodeParams p)
                         offset4 = *(const lds_words4*)(uintptr_t)(at + 32);
                         if (!whole) { scale4 &= mask; offset4 &= mask; }
                     }
-                    vf = four_bits(*(const lds_word*)(uintptr_t)(v_read + off + (uint32_t)(b * 128)), scale4, offset4);
+                    vf = four_bits(*(const lds_word*)(uintptr_t)(v_read + off + (uint32_t)(b * 128)), scale4, offset4, codes_at);
                 } else if constexpr (T::kHalf) {
                     u32x4_t w = *(const lds_words4*)(uintptr_t)(v_read + off + (uint32_t)(b * 1024));
                     if (!whole) w &= mask;

@@ -7,6 +7,8 @@
 // A wavefront has 16 TILES tokens of a sequence and key head in registers, as left operands of 16x16x32 products; the rows come by as right operands, 16 at
 // a time, from LDS, where the workgroup's four wavefronts share them.  The score tiles have four tokens and one row a lane: what rows need is
 // joined over four lanes, what tokens need over 16 at the very end, in a fixed order.
+#include <type_traits>
+
 #include "attn_common.h"
 
 namespace cg {
@@ -14,7 +16,7 @@ namespace cg {
 constexpr int kScoreWaves = 4;
 constexpr int kScoreThreads = kScoreWaves * kWave;
 constexpr int kRowsAtOnce = 128;            // in LDS
-constexpr int kScoreGroups = 4096;          // workgroups that are worth sharing the keys, at least
+constexpr int kScoreGroups = 2048;          // workgroups that are worth sharing the keys, at least
 constexpr size_t kMostParts = 32u << 20;    // bytes of rows' parts
 
 // Tokens of a wavefront at once: what leaves room for four (two) wavefronts on a SIMD.
@@ -51,79 +53,95 @@ __device__ __forceinline__ int first_seen(const ScoreParams& p, int position)
     return p.window > 0 && position >= p.window ? position - p.window + 1 : 0;
 }
 
-// A wavefront's tokens t0 .. t0 + 16 TILES - 1 as left operands, a key's dimensions dealt out by operand_dim.  ok: bit n: tile n has a page.
+typedef __attribute__((address_space(4))) const int32_t const_int;
+
+// A wavefront's tokens t0 .. t0 + 16 TILES - 1 as they lie in the cache: lane (col, g) has of every tile's token `col` the dimensions that operand_dim deals out.
 template <int TYPE, int DP, bool EXACT>
-struct Keys {
+struct Codes {
     static constexpr int TILES = score_tiles(DP), PARTS = DP / 32;
-    half8_t k[TILES][PARTS];
-    float4_t by[TILES];     // of the scores: scale, times those of 8-bit codes
-    int ok;
+    static constexpr bool HALF = TYPE == CODEGEMM_KV_FP16, FOUR = TYPE == CODEGEMM_KV_INT4, SCALED = !HALF && !FOUR;
+    static constexpr int WORDS = HALF ? 4 * PARTS : FOUR ? PARTS : 2 * PARTS;
+    uint32_t w[TILES][WORDS], so[TILES][FOUR ? (DP + 127) / 128 : 1];
+    float4_t by[TILES];     // 8 bits: the scales of tokens 4 g ..
+    int ok;                 // bit n: tile n has a page
 
     __device__ __forceinline__ void load(const ScoreParams& p, int seq, int head, int t0, int len, int col, int g)
     {
         const CacheView& c = p.c;
         const int D = EXACT ? DP : c.D;
+        const_int* table = (const_int*)(uintptr_t)c.table + (size_t)seq * c.max_pages;
         ok = 0;
-        int page[TILES];
 #pragma unroll
         for (int n = 0; n < TILES; ++n) {
-            const int t = t0 + 16 * n < len ? t0 + 16 * n : len - 1;
-            page[n] = c.table[(size_t)seq * c.max_pages + (t >> c.page_shift)];
-            const bool in = (unsigned)page[n] < (unsigned)c.pages && t0 + 16 * n < len;
+            const int t = t0 + 16 * n < len ? t0 + 16 * n : len - 1, found = table[t >> c.page_shift];
+            const bool in = (unsigned)found < (unsigned)c.pages && t0 + 16 * n < len;
             ok |= in ? 1 << n : 0;
-            page[n] = in ? page[n] : 0;
-        }
-        constexpr int WORDS = TYPE == CODEGEMM_KV_FP16 ? 4 * PARTS : TYPE == CODEGEMM_KV_INT4 ? PARTS : 2 * PARTS;
-        uint32_t w[TILES][WORDS], so[TILES][(DP + 127) / 128];
-#pragma unroll
-        for (int n = 0; n < TILES; ++n) {
-            const int slot = (t0 + 16 * n) & ((1 << c.page_shift) - 1);
-            const size_t at = page_at(c, page[n], head) + (size_t)(slot + col) * D;
-            if constexpr (TYPE == CODEGEMM_KV_INT4) {
-                const uint32_t* runs = reinterpret_cast<const uint32_t*>(c.k_scales) + runs_at(c, page[n], head, slot + col);
+            const int page = in ? found : 0, slot = (t0 + 16 * n) & ((1 << c.page_shift) - 1);
+            const size_t at = page_at(c, page, head) + (size_t)slot * D;                // (uniform)
+            if constexpr (FOUR) {
+                const unsigned char* row = c.k + at / 2 + col * (D / 2);
+                const uint32_t* runs = reinterpret_cast<const uint32_t*>(c.k_scales) + runs_at(c, page, head, slot) + col * c.runs;
 #pragma unroll
                 for (int j = 0; j < (DP + 127) / 128; ++j) {
                     const int given = operand_dim<TYPE, DP>(4 * j, g), d = EXACT || given < D ? given : 0;
                     so[n][j] = runs[d >> c.run_shift];
                     if constexpr (DP < 128) {
-                        const u32x2_t x = *reinterpret_cast<const u32x2_t*>(c.k + (at + d) / 2);
+                        const u32x2_t x = *reinterpret_cast<const u32x2_t*>(row + d / 2);
                         w[n][0] = x[0]; w[n][1] = x[1];
                     } else {
-                        const u32x4_t x = *reinterpret_cast<const u32x4_t*>(c.k + (at + d) / 2);
+                        const u32x4_t x = *reinterpret_cast<const u32x4_t*>(row + d / 2);
 #pragma unroll
                         for (int i = 0; i < 4; ++i) w[n][4 * j + i] = x[i];
                     }
                 }
             } else {
-                constexpr int SIZE = TYPE == CODEGEMM_KV_FP16 ? 2 : 1;
+                constexpr int SIZE = HALF ? 2 : 1;
+                const unsigned char* row = c.k + at * SIZE + col * D * SIZE;
 #pragma unroll
                 for (int j = 0; j < DP / 64; ++j) {
                     const int given = 64 * j + 16 * g, d = EXACT || given < D ? given : 0;
 #pragma unroll
                     for (int h = 0; h < SIZE; ++h) {
-                        const u32x4_t x = *reinterpret_cast<const u32x4_t*>(c.k + (at + d) * SIZE + 16 * h);
+                        const u32x4_t x = *reinterpret_cast<const u32x4_t*>(row + d * SIZE + 16 * h);
 #pragma unroll
                         for (int i = 0; i < 4; ++i) w[n][(j * SIZE + h) * 4 + i] = x[i];
                     }
                 }
-                if constexpr (SIZE == 1) {
-                    const float* s = c.k_scales + scales_at(c, page[n], head);
+                if constexpr (SCALED) {
+                    const float* s = c.k_scales + scales_at(c, page, head);
 #pragma unroll
                     for (int r = 0; r < 4; ++r) by[n][r] = s[(slot + 4 * g + r) >> c.block_shift];
                 }
             }
         }
+    }
+};
+
+// .. as left operands of the products.
+template <int TYPE, int DP, bool EXACT>
+struct Keys {
+    typedef Codes<TYPE, DP, EXACT> C;
+    static constexpr int TILES = C::TILES, PARTS = C::PARTS;
+    half8_t k[TILES][PARTS];
+    float4_t by[TILES];     // of the scores: scale, times those of 8-bit codes
+    int ok;
+
+    __device__ __forceinline__ void take(const C& c, const ScoreParams& p, int g)
+    {
+        const int D = EXACT ? DP : p.c.D;
+        const uint32_t mask = C::FOUR ? code_mask() : 0u;
+        ok = c.ok;
 #pragma unroll
         for (int n = 0; n < TILES; ++n) {
 #pragma unroll
             for (int i = 0; i < PARTS; ++i) {
-                if constexpr (TYPE == CODEGEMM_KV_INT4) k[n][i] = four_bits(w[n][i], both_low(so[n][i / 4]), both_high(so[n][i / 4]));
-                else if constexpr (TYPE == CODEGEMM_KV_FP16) k[n][i] = __builtin_bit_cast(half8_t, u32x4_t{w[n][4 * i], w[n][4 * i + 1], w[n][4 * i + 2], w[n][4 * i + 3]});
-                else k[n][i] = codes_to_half<TYPE>(w[n][2 * i], w[n][2 * i + 1]);
+                if constexpr (C::FOUR) k[n][i] = four_bits(c.w[n][i], both_low(c.so[n][i / 4]), both_high(c.so[n][i / 4]), mask);
+                else if constexpr (C::HALF) k[n][i] = __builtin_bit_cast(half8_t, u32x4_t{c.w[n][4 * i], c.w[n][4 * i + 1], c.w[n][4 * i + 2], c.w[n][4 * i + 3]});
+                else k[n][i] = codes_to_half<TYPE>(c.w[n][2 * i], c.w[n][2 * i + 1]);
                 if (!EXACT && operand_dim<TYPE, DP>(i, g) >= D) k[n][i] = half8_t{0, 0, 0, 0, 0, 0, 0, 0};
             }
-            if constexpr (TYPE == CODEGEMM_KV_FP16 || TYPE == CODEGEMM_KV_INT4) by[n] = float4_t{p.scale, p.scale, p.scale, p.scale};
-            else by[n] *= p.scale;
+            if constexpr (C::SCALED) by[n] = c.by[n] * p.scale;
+            else by[n] = float4_t{p.scale, p.scale, p.scale, p.scale};
         }
     }
 };
@@ -158,73 +176,105 @@ __device__ __forceinline__ void score_tile(const Keys<TYPE, DP, EXACT>& keys, co
     }
 }
 
-// Which of a lane's tokens its row sees: t - t0 in lo .. hi, in tiles that have a page.
+// Which tokens of its row a lane sees: t - t0 in lo .. hi, in tiles that have a page.
 struct Seen {
     int lo, hi, ok;
     __device__ __forceinline__ bool operator()(int n, int r, int g) const { const int t = 16 * n + 4 * g + r; return (ok >> n & 1) && t >= lo && t <= hi; }
 };
+template <class T>
+__device__ __forceinline__ Seen seen_of(const ScoreParams& p, const Queries& qs, int at, int t0, const T& keys)
+{
+    return Seen{first_seen(p, at) - t0, (at < qs.len ? at : qs.len - 1) - t0, keys.ok};
+}
+// Whether rows row .. row + 15 all see all of a wavefront's tokens.
+template <class T>
+__device__ __forceinline__ bool see_all(const ScoreParams& p, const Queries& qs, const int* at, int t0, const T& keys)
+{
+    const int first = __builtin_amdgcn_readfirstlane(at[0]), last = __builtin_amdgcn_readfirstlane(at[15]);
+    return keys.ok == (1 << T::TILES) - 1 && t0 + 16 * T::TILES - 1 <= first && t0 >= first_seen(p, last);
+}
+
+// What a workgroup keeps in LDS of up to kRowsAtOnce rows: the right operands, positions, and per wavefront (STATS) or once what is known of their weights.
+template <int DP>
+struct RowSpace {
+    _Float16* rows;         // [tile][part][lane][8]
+    Pair* sums;
+    int* at;
+    __device__ __forceinline__ explicit RowSpace(unsigned char* smem)
+        : rows(reinterpret_cast<_Float16*>(smem)), sums(reinterpret_cast<Pair*>(smem + (size_t)kRowsAtOnce * DP * 2)), at(reinterpret_cast<int*>(sums + kScoreWaves * kRowsAtOnce))
+    {
+    }
+    static constexpr size_t bytes = (size_t)kRowsAtOnce * DP * 2 + kScoreWaves * kRowsAtOnce * sizeof(Pair) + kRowsAtOnce * sizeof(int);
+};
+__device__ __forceinline__ void load_positions(const ScoreParams& p, const Queries& qs, int from, int count, int* at)
+{
+    for (int i = threadIdx.x; i < (count + 15) / 16 * 16; i += kScoreThreads) at[i] = qs.at + (from + i) / p.r;
+}
 
 // Workgroup (sequence and key head, slot, z): rows z * 128 .. and on, over every slots-th block of keys.
 template <int TYPE, int DP, bool EXACT>
-__global__ void __launch_bounds__(kScoreThreads, 2) score_stats_kernel(const ScoreParams p)
+__global__ void __launch_bounds__(kScoreThreads, DP == 256 ? 2 : 3) score_stats_kernel(const ScoreParams p)
 {
     constexpr int TILES = score_tiles(DP), PARTS = DP / 32, BLOCK = 16 * TILES * kScoreWaves;
     extern __shared__ __align__(16) unsigned char smem[];
-    _Float16* rows = reinterpret_cast<_Float16*>(smem);
+    const RowSpace<DP> space(smem);
     const int D = EXACT ? DP : p.c.D, tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave), col = lane & 15, g = lane >> 4;
-    Pair* state = reinterpret_cast<Pair*>(smem + (size_t)kRowsAtOnce * DP * 2);        // [wavefront][row]
     const int seq = blockIdx.x / p.c.Hk, head = blockIdx.x % p.c.Hk;
     const Queries qs = queries_of(p, seq);
     const int count_all = qs.n * p.r, lowest = first_seen(p, qs.at) / BLOCK * BLOCK;   // of the first query's keys
     for (int from = blockIdx.z * kRowsAtOnce; from < count_all; from += gridDim.z * kRowsAtOnce) {
         const int count = count_all - from < kRowsAtOnce ? count_all - from : kRowsAtOnce;
         __syncthreads();
-        load_rows<TYPE, DP>(p, qs, head, from, count, D, rows);
-        for (int i = tid; i < kScoreWaves * kRowsAtOnce; i += kScoreThreads) state[i] = Pair{-INFINITY, 0.0f};
+        load_rows<TYPE, DP>(p, qs, head, from, count, D, space.rows);
+        load_positions(p, qs, from, count, space.at);
+        for (int i = tid; i < kScoreWaves * kRowsAtOnce; i += kScoreThreads) space.sums[i] = Pair{-INFINITY, 0.0f};
         __syncthreads();
         for (int b = lowest + blockIdx.y * BLOCK; b < qs.len; b += p.slots * BLOCK) {
             const int t0 = b + wave * 16 * TILES;
             if (t0 >= qs.len) continue;
+            Codes<TYPE, DP, EXACT> codes;
             Keys<TYPE, DP, EXACT> keys;
-            keys.load(p, seq, head, t0, qs.len, col, g);
+            codes.load(p, seq, head, t0, qs.len, col, g);
+            keys.take(codes, p, g);
             for (int tile = 0; 16 * tile < count; ++tile) {
-                const int at = qs.at + (from + 16 * tile + col) / p.r, first_at = qs.at + (from + 16 * tile) / p.r, last_at = qs.at + (from + 16 * tile + 15) / p.r;
                 float4_t s[TILES];
-                score_tile<TYPE, DP, EXACT>(keys, rows + (size_t)tile * PARTS * kWave * 8, lane, s);
-                const bool whole = keys.ok == (1 << TILES) - 1 && t0 + 16 * TILES - 1 <= first_at && t0 >= first_seen(p, last_at);
-                const Seen seen = {first_seen(p, at) - t0, (at < qs.len ? at : qs.len - 1) - t0, keys.ok};
-                float most = -INFINITY;
-#pragma unroll
-                for (int n = 0; n < TILES; ++n)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const float x = s[n][r] * keys.by[n][r];
-                        most = fmaxf(most, whole || seen(n, r, g) ? x : -INFINITY);
-                    }
-                most = over_groups(most, [](float a, float c) { return fmaxf(a, c); });
-                Pair* mine = state + wave * kRowsAtOnce + 16 * tile + col;
+                score_tile<TYPE, DP, EXACT>(keys, space.rows + (size_t)tile * PARTS * kWave * 8, lane, s);
+                Pair* mine = space.sums + wave * kRowsAtOnce + 16 * tile + col;
                 const Pair old = *mine;
-                const float m = fmaxf(old.a, most), base = m == -INFINITY ? 0.0f : m;
-                float sum = 0.0f;
+                auto add = [&](auto is_whole, const Seen& seen) {
+                    constexpr bool whole = decltype(is_whole)::value;
+                    float most = -INFINITY;
 #pragma unroll
-                for (int n = 0; n < TILES; ++n)
+                    for (int n = 0; n < TILES; ++n)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const float w = __builtin_amdgcn_exp2f(s[n][r] * keys.by[n][r] - base);
-                        sum += whole || seen(n, r, g) ? w : 0.0f;
-                    }
-                sum = over_groups(sum, [](float a, float c) { return a + c; });
-                if (g == 0) *mine = Pair{m, __builtin_fmaf(old.b, __builtin_amdgcn_exp2f(old.a - base), sum)};
+                        for (int r = 0; r < 4; ++r) {
+                            s[n][r] *= keys.by[n][r];
+                            if (!whole) s[n][r] = seen(n, r, g) ? s[n][r] : -INFINITY;
+                            most = fmaxf(most, s[n][r]);
+                        }
+                    most = over_groups(most, [](float a, float c) { return fmaxf(a, c); });
+                    const float m = fmaxf(old.a, most), base = m == -INFINITY ? 0.0f : m;
+                    float sum = 0.0f;
+#pragma unroll
+                    for (int n = 0; n < TILES; ++n)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) sum += __builtin_amdgcn_exp2f(s[n][r] - base);
+                    sum = over_groups(sum, [](float a, float c) { return a + c; });
+                    if (g == 0) *mine = Pair{m, __builtin_fmaf(old.b, __builtin_amdgcn_exp2f(old.a - base), sum)};
+                };
+                if (see_all(p, qs, space.at + 16 * tile, t0, keys)) add(std::true_type(), Seen{});
+                else add(std::false_type(), seen_of(p, qs, space.at[16 * tile + col], t0, keys));
             }
         }
         __syncthreads();
         for (int i = tid; i < count; i += kScoreThreads) {
+            const Pair* state = space.sums + i;
             float m = -INFINITY, sum = 0.0f;
 #pragma unroll
-            for (int w = 0; w < kScoreWaves; ++w) m = fmaxf(m, state[w * kRowsAtOnce + i].a);
+            for (int w = 0; w < kScoreWaves; ++w) m = fmaxf(m, state[w * kRowsAtOnce].a);
             const float base = m == -INFINITY ? 0.0f : m;
 #pragma unroll
-            for (int w = 0; w < kScoreWaves; ++w) sum += state[w * kRowsAtOnce + i].b * __builtin_amdgcn_exp2f(state[w * kRowsAtOnce + i].a - base);
+            for (int w = 0; w < kScoreWaves; ++w) sum += state[w * kRowsAtOnce].b * __builtin_amdgcn_exp2f(state[w * kRowsAtOnce].a - base);
             const int row = from + i;
             p.part[(size_t)blockIdx.y * p.rows + (size_t)(qs.row0 + row / p.r) * (p.c.Hk * p.r) + head * p.r + row % p.r] = Pair{m, sum};
         }
@@ -246,52 +296,66 @@ __global__ void __launch_bounds__(kScoreThreads) score_join_kernel(const ScorePa
     p.stats[row] = sum == 0.0f ? Pair{0.0f, 0.0f} : Pair{m, 1.0f / sum};
 }
 
-// Workgroup (sequence and key head, slot): every slots-th block of keys, all rows.
+// Workgroup (sequence and key head, slot): every slots-th block of keys, all rows.  The next block's codes are on their way while one is worked on.
 template <int TYPE, int DP, bool EXACT>
-__global__ void __launch_bounds__(kScoreThreads, 2) score_sum_kernel(const ScoreParams p)
+__global__ void __launch_bounds__(kScoreThreads, DP == 256 || (DP == 128 && TYPE != CODEGEMM_KV_INT4) ? 2 : 3) score_sum_kernel(const ScoreParams p)
 {
     constexpr int TILES = score_tiles(DP), PARTS = DP / 32, BLOCK = 16 * TILES * kScoreWaves, VALUES = 4 * TILES;
     extern __shared__ __align__(16) unsigned char smem[];
-    _Float16* rows = reinterpret_cast<_Float16*>(smem);
+    const RowSpace<DP> space(smem);
     const int D = EXACT ? DP : p.c.D, tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave), col = lane & 15, g = lane >> 4;
-    Pair* stats = reinterpret_cast<Pair*>(smem + (size_t)kRowsAtOnce * DP * 2);        // [row]
     const int seq = blockIdx.x / p.c.Hk, head = blockIdx.x % p.c.Hk;
     const Queries qs = queries_of(p, seq);
     const int count_all = qs.n * p.r, lowest = first_seen(p, qs.at), fresh = p.first ? p.first[seq] : qs.at;
-    for (int b = blockIdx.y * BLOCK; b < qs.len; b += p.slots * BLOCK) {
-        const int t0 = b + wave * 16 * TILES;
-        const bool active = t0 < qs.len && t0 + 16 * TILES > lowest;
+    auto active = [&](int t0) { return t0 < qs.len && t0 + 16 * TILES > lowest; };
+    int b = blockIdx.y * BLOCK;
+    if (b >= qs.len) return;
+    auto load = [&](int from) {
+        const int count = count_all - from < kRowsAtOnce ? count_all - from : kRowsAtOnce;
+        __syncthreads();
+        load_rows<TYPE, DP>(p, qs, head, from, count, D, space.rows);
+        load_positions(p, qs, from, count, space.at);
+        for (int i = tid; i < (count + 15) / 16 * 16; i += kScoreThreads) {
+            const int row = from + i;
+            space.sums[i] = i < count ? p.stats[(size_t)(qs.row0 + row / p.r) * (p.c.Hk * p.r) + head * p.r + row % p.r] : Pair{0.0f, 0.0f};
+        }
+        __syncthreads();
+        return count;
+    };
+    Codes<TYPE, DP, EXACT> codes;
+    if (active(b + wave * 16 * TILES)) codes.load(p, seq, head, b + wave * 16 * TILES, qs.len, col, g);
+    const bool once = count_all <= kRowsAtOnce;                                        // the rows stay
+    if (once) load(0);
+    for (; b < qs.len; b += p.slots * BLOCK) {
+        const int t0 = b + wave * 16 * TILES, t_next = t0 + p.slots * BLOCK;
+        const bool mine = active(t0);
         Keys<TYPE, DP, EXACT> keys;
-        if (active) keys.load(p, seq, head, t0, qs.len, col, g);
+        if (mine) keys.take(codes, p, g);
+        if (t_next > t0 && active(t_next)) codes.load(p, seq, head, t_next, qs.len, col, g);
         float sum[VALUES];
 #pragma unroll
         for (int i = 0; i < VALUES; ++i) sum[i] = 0.0f;
         if (b + BLOCK > lowest) {                                                      // uniform
             for (int from = 0; from < count_all; from += kRowsAtOnce) {
-                const int count = count_all - from < kRowsAtOnce ? count_all - from : kRowsAtOnce;
-                __syncthreads();
-                load_rows<TYPE, DP>(p, qs, head, from, count, D, rows);
-                for (int i = tid; i < (count + 15) / 16 * 16; i += kScoreThreads) {
-                    const int row = from + i;
-                    stats[i] = i < count ? p.stats[(size_t)(qs.row0 + row / p.r) * (p.c.Hk * p.r) + head * p.r + row % p.r] : Pair{0.0f, 0.0f};
-                }
-                __syncthreads();
-                if (!active) continue;
+                const int count = once ? count_all : load(from);
+                if (!mine) continue;
                 for (int tile = 0; 16 * tile < count; ++tile) {
-                    const int at = qs.at + (from + 16 * tile + col) / p.r, first_at = qs.at + (from + 16 * tile) / p.r, last_at = qs.at + (from + 16 * tile + 15) / p.r;
                     float4_t s[TILES];
-                    score_tile<TYPE, DP, EXACT>(keys, rows + (size_t)tile * PARTS * kWave * 8, lane, s);
-                    const Pair st = stats[16 * tile + col];
-                    const bool whole = keys.ok == (1 << TILES) - 1 && t0 + 16 * TILES - 1 <= first_at && t0 >= first_seen(p, last_at);
-                    const Seen seen = {first_seen(p, at) - t0, (at < qs.len ? at : qs.len - 1) - t0, keys.ok};
+                    score_tile<TYPE, DP, EXACT>(keys, space.rows + (size_t)tile * PARTS * kWave * 8, lane, s);
+                    const Pair st = space.sums[16 * tile + col];
+                    auto add = [&](auto is_whole, const Seen& seen) {
+                        constexpr bool whole = decltype(is_whole)::value;
 #pragma unroll
-                    for (int n = 0; n < TILES; ++n)
+                        for (int n = 0; n < TILES; ++n)
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            const float w = __builtin_amdgcn_exp2f(s[n][r] * keys.by[n][r] - st.a);
-                            const float more = __builtin_fmaf(w, st.b, sum[4 * n + r]);
-                            sum[4 * n + r] = whole || (seen(n, r, g) && st.b != 0.0f) ? more : sum[4 * n + r];
-                        }
+                            for (int r = 0; r < 4; ++r) {
+                                const float w = __builtin_amdgcn_exp2f(s[n][r] * keys.by[n][r] - st.a), more = __builtin_fmaf(w, st.b, sum[4 * n + r]);
+                                sum[4 * n + r] = whole || (seen(n, r, g) && st.b != 0.0f) ? more : sum[4 * n + r];
+                            }
+                    };
+                    // (rows that are none have no weight in the first form either: a score of 0, and 1 / sum 0)
+                    if (see_all(p, qs, space.at + 16 * tile, t0, keys)) add(std::true_type(), Seen{});
+                    else add(std::false_type(), seen_of(p, qs, space.at[16 * tile + col], t0, keys));
                 }
             }
         }
@@ -389,7 +453,7 @@ template <int TYPE, int DP, bool EXACT>
 int launch_scores_one(const ScoreParams& p, const ScorePlan& plan, bool stats, hipStream_t s)
 {
     const dim3 threads(kScoreThreads), items((unsigned)(p.c.seqs * p.c.Hk), (unsigned)plan.slots);
-    const size_t lds = (size_t)kRowsAtOnce * DP * 2 + kScoreWaves * kRowsAtOnce * sizeof(Pair);
+    constexpr size_t lds = RowSpace<DP>::bytes;
     if (stats) {
         auto fn = score_stats_kernel<TYPE, DP, EXACT>;
         const int st = set_max_lds(reinterpret_cast<const void*>(fn), lds);

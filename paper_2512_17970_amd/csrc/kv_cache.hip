@@ -549,7 +549,7 @@ __device__ __forceinline__ void gather_unit4(const CacheView& cv, bool values, i
                 const u32x2_t w = *reinterpret_cast<const u32x2_t*>(cv.k + (at + (size_t)t * D) / 2 + 8 * c);
                 const uint32_t so = reinterpret_cast<const uint32_t*>(cv.k_scales)[scale_at + (size_t)t * cv.runs + run];
 #pragma unroll
-                for (int i = 0; i < 2; ++i) x[i] = four_bits(w[i], both_low(so), both_high(so));
+                for (int i = 0; i < 2; ++i) x[i] = four_bits(w[i], both_low(so), both_high(so), code_mask());
             } else {
                 const _Float16* so = reinterpret_cast<const _Float16*>(cv.v_scales) + 2 * scale_at + 32 * run + t;
                 const _Float16 s = so[0], o = so[kTokenGroup];
