@@ -38,6 +38,7 @@ constexpr float kLeastLog = -40.0f;         // of a scale's logarithm in the run
 // the weight and values near zero, thousands of others with little weight each make the result.  (With 1 for the largest, the weights of the keys that share
 // a wavefront with such a key were off by 2.6 % at 15 nats below it, by 44 % at 17, and zero at 18.)  Not from scores of kFine on, which may have no place for it.
 constexpr float kLift = 14.0f, kFine = 1048576.0f;
+constexpr float kLowLift = 10.0f, kReach = 5.5f;       // 4 bits: the largest weight lies between 2^10 and 2^15.5
 
 struct DecodeParams {
     CacheView c;
@@ -76,10 +77,9 @@ struct DecodeStep {
     static constexpr int kRequests = 2 * kPart / 1024 + (kHalf ? 0 : kFour ? kScaleBytes / 1024 : 1);
     static constexpr int kStages = 2;
     static constexpr int kPerCu = NARROW && kBytes <= 20 * 1024 ? 2 : 1;
-#ifndef W4
-#define W4 8
-#endif
-    static constexpr int kWaves = (kBytes > 20 * 1024 ? 2 : kBytes > 9 * 1024 ? 4 : kFour ? W4 : 8) / kPerCu;
+    // (4 bits, heads of 64, 32 sequences of 8 heads: 12 wavefronts 21.5 us, 8 23.3, 16 22.6; 13 of twenty heads: 2 x 8 19.6, 2 x 4 20.5.  Heads of 128: 12 hide no more than 8,
+    // 56.4 for 58.8 us at 206 000 tokens, and cost short sequences 1.4 us; 2 x 6 are slower than 2 x 4, 78 for 62.)
+    static constexpr int kWaves = kFour && DP == 64 ? (NARROW ? 8 : 12) : (kBytes > 20 * 1024 ? 2 : kBytes > 9 * 1024 ? 4 : 8) / kPerCu;
     static constexpr int kRing = kWaves * kStages * kBytes;
     static constexpr int kSums = kWaves * kDecodeRows * 8;           // the wavefronts' maxima and weights
     static constexpr int kLds = kRing + kSums + 16;
@@ -132,6 +132,11 @@ __device__ __forceinline__ void request16(uint32_t lds, const unsigned char* fro
 {
     asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" :: "{m0}"(lds), "v"(from) : "memory");
 }
+// .. the lane's address as 32 bits from a common one
+__device__ __forceinline__ void request16(uint32_t lds, const unsigned char* base, uint32_t from)
+{
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" :: "{m0}"(lds), "v"(from), "s"(base) : "memory");
+}
 __device__ __forceinline__ void request4(uint32_t lds, const float* from)
 {
     asm volatile("s_nop 0\n\tglobal_load_lds_dword %1, off" :: "{m0}"(lds), "v"(from) : "memory");
@@ -140,7 +145,7 @@ __device__ __forceinline__ void request4(uint32_t lds, const float* from)
 // TYPE: of the cache.  DP: head_dim rounded up to 64, 128 or 256; EXACT: it is head_dim.
 // SUMS: of weights as they are, not as they are rounded, also in fp16 (there are `stats`).
 template <int TYPE, int DP, bool EXACT, bool NARROW, bool SUMS>
-__global__ void __launch_bounds__((DecodeStep<TYPE, DP, NARROW>::kWaves * kWave), (DecodeStep<TYPE, DP, NARROW>::kWaves * DecodeStep<TYPE, DP, NARROW>::kPerCu > 8 ? 3 : DecodeStep<TYPE, DP, NARROW>::kWaves * DecodeStep<TYPE, DP, NARROW>::kPerCu > 4 ? 2 : 1))
+__global__ void __launch_bounds__((DecodeStep<TYPE, DP, NARROW>::kWaves * kWave), (DecodeStep<TYPE, DP, NARROW>::kWaves * DecodeStep<TYPE, DP, NARROW>::kPerCu > 12 ? 4 : DecodeStep<TYPE, DP, NARROW>::kWaves * DecodeStep<TYPE, DP, NARROW>::kPerCu > 8 ? 3 : DecodeStep<TYPE, DP, NARROW>::kWaves * DecodeStep<TYPE, DP, NARROW>::kPerCu > 4 ? 2 : 1))
 attn_decode_kernel(const DecodeParams p)
 {
     typedef DecodeStep<TYPE, DP, NARROW> T;
@@ -201,6 +206,23 @@ attn_decode_kernel(const DecodeParams p)
                                      : ring + T::kPart + (uint32_t)((g >> 1) * 512 + col * 16 + (g & 1) * 8);
     // .. its scales; 4 bits: those of its token's keys (tile 0), and of its 8 tokens' values
     const uint32_t s_read = ring + 2 * T::kPart + (T::kFour ? (uint32_t)((col >> 3) * T::kRunBytes + (8 * ((col >> 2) & 1) + (col & 3)) * cv.runs * 4) : (uint32_t)(g * 32));
+    // 4 bits: what lanes ask for, from where a step's keys, values and scales begin in its page (as request_four does for groups of 16 tokens)
+    uint32_t k_from[T::kFour ? T::kPart / 1024 : 1] = {0}, v_from[T::kFour ? T::kPart / 1024 : 1] = {0};
+    long long s_from = 0;
+    if constexpr (T::kFour) {
+        const int token = 8 * (col >> 2) + (col & 3);
+#pragma unroll
+        for (int i = 0; i < T::kPart / 1024; ++i) {
+            const int n = DP == 64 ? g >> 1 : i / ((DP + 127) / 128), d = DP == 64 ? 32 * (g & 1) : 128 * (i % ((DP + 127) / 128)) + 32 * g;
+            k_from[i] = (uint32_t)((token + 4 * n) * (D / 2) + (EXACT || d < D ? d : 0) / 2);
+            const int at = i * kWave + lane, x = at / (DP / 2), dv = 2 * (at % (DP / 2));
+            v_from[i] = (uint32_t)(x * 8 * D + (EXACT || dv < D ? dv : 0) * 8);
+        }
+        constexpr int kLanes = T::kRunBytes / 16;
+        const int at = lane / kLanes & 3, word = 4 * (lane % kLanes), last = 16 * cv.runs - 4;
+        s_from = 4 * ((at & 1) * 16 * cv.runs + (word < last ? word : last));
+        if (T::kScaleBytes == 1024 && (at & 2)) s_from += (long long)(reinterpret_cast<uintptr_t>(cv.v_scales) - reinterpret_cast<uintptr_t>(cv.k_scales));
+    }
     const uint32_t vs_read = ring + 2 * T::kPart + (uint32_t)((2 + (g >> 1)) * T::kRunBytes + (g & 1) * 16);
 
     for (unsigned piece = blockIdx.x;; piece += groups) {
@@ -275,8 +297,31 @@ attn_decode_kernel(const DecodeParams p)
                 request16(to + (uint32_t)(2 * T::kPart + i * 1024), reinterpret_cast<const unsigned char*>(s + (word < last ? word : last)));
             }
         };
+        // .. where a page has a step's 32 tokens (those behind the last one lie in it too, and do not count)
+        auto request_page = [&](int step, int stage) {
+            const int t = sp.len > 0 ? sp.first + step * 32 : 0;
+            const bool in = (unsigned)page[0] < (unsigned)cv.pages;
+            const size_t token = (((size_t)(in ? page[0] : 0) * cv.Hk + head) << cv.page_shift) + (size_t)(t & ((1 << cv.page_shift) - 1));
+            const size_t at = token * (size_t)(D / 2), runs_from = token * (size_t)cv.runs * 4;
+            const uint32_t to = ring + (uint32_t)(stage * T::kBytes);
+#pragma unroll
+            for (int i = 0; i < T::kPart / 1024; ++i) request16(to + (uint32_t)(i * 1024), cv.k + at, k_from[i]);
+#pragma unroll
+            for (int i = 0; i < T::kPart / 1024; ++i) request16(to + (uint32_t)(T::kPart + i * 1024), cv.v + at, v_from[i]);
+            if constexpr (T::kScaleBytes == 1024) {
+                const unsigned char* both = reinterpret_cast<const unsigned char*>(cv.k_scales) + runs_from;
+                request16(to + (uint32_t)(2 * T::kPart), both + s_from);
+            } else {
+                request16(to + (uint32_t)(2 * T::kPart), reinterpret_cast<const unsigned char*>(cv.k_scales) + runs_from, (uint32_t)s_from);
+                request16(to + (uint32_t)(2 * T::kPart + 1024), reinterpret_cast<const unsigned char*>(cv.v_scales) + runs_from, (uint32_t)s_from);
+            }
+            return in ? 3 : 0;
+        };
         // bit x: group x has a page
         auto request = [&](int step, int stage) {
+            if constexpr (T::kFour) {
+                if (cv.page_shift >= 5) return request_page(step, stage);
+            }
             const unsigned char *kp[2], *vp[2];
             const float *ks[2], *vs[2];
             int ok = 0;
@@ -445,8 +490,18 @@ attn_decode_kernel(const DecodeParams p)
                     for (int r = 0; r < 4; ++r) most = fmaxf(most, s[n][r] + fmaxf(__builtin_amdgcn_logf(vs[n][r]), kLeastLog));
             }
             most = over_groups(most, [](float a, float b) { return fmaxf(a, b); });
-            most -= fabsf(most) < kFine ? kLift : 0.0f;
-            const float m_new = fmaxf(m, most), base = m_new == -INFINITY ? 0.0f : m_new;
+            float m_new;
+            if constexpr (T::kFour) {
+                // (Followed where a weight would pass 2^(kLowLift + kReach) only, so that sums are seldom rescaled: they are, in nearly every step, for one of the
+                // heads or another, where every new maximum is followed.)
+                const bool fine = fabsf(most) < kFine;
+                const float from = most - (fine ? kLowLift : 0.0f);
+                m_new = from > m + (fine ? kReach : 0.0f) ? from : m;
+            } else {
+                most -= fabsf(most) < kFine ? kLift : 0.0f;
+                m_new = fmaxf(m, most);
+            }
+            const float base = m_new == -INFINITY ? 0.0f : m_new;
             const float keep = __builtin_amdgcn_exp2f(m - base);
             m = m_new;
             float add = 0.0f;
