@@ -15,8 +15,16 @@ namespace cg {
 
 constexpr int kScoreWaves = 4;
 constexpr int kScoreThreads = kScoreWaves * kWave;
-constexpr int kRowsAtOnce = 128;            // in LDS
-constexpr int kScoreGroups = 2048;          // workgroups that are worth sharing the keys, at least
+constexpr int rows_at_once(int dp, bool stats) { return stats || dp == 256 ? 128 : 256; }       // in LDS, at most
+#ifndef SB4
+#define SB4 2
+#endif
+#ifndef GST
+#define GST 512
+#define GSU 512
+#define GSD 2048
+#endif
+constexpr int kStatsGroups = GST, kSumGroups = GSU, kFewGroups = GSD;          // workgroups that are worth sharing the keys, at least
 constexpr size_t kMostParts = 32u << 20;    // bytes of rows' parts
 
 // Tokens of a wavefront at once: what leaves room for four (two) wavefronts on a SIMD.
@@ -33,6 +41,7 @@ struct ScoreParams {
     int rows;               // total_q * query heads
     int total_q, r, q_stride, window;
     int slots;              // workgroups that share the keys
+    int many;               // rows that LDS has room for
     float scale;            // times log2(e)
 };
 
@@ -63,13 +72,30 @@ struct Codes {
     static constexpr int WORDS = HALF ? 4 * PARTS : FOUR ? PARTS : 2 * PARTS;
     uint32_t w[TILES][WORDS], so[TILES][FOUR ? (DP + 127) / 128 : 1];
     float4_t by[TILES];     // 8 bits: the scales of tokens 4 g ..
+    size_t token[TILES];    // of a tile's first token, in [page][head][slot]; the same for all lanes
     int ok;                 // bit n: tile n has a page
 
-    __device__ __forceinline__ void load(const ScoreParams& p, int seq, int head, int t0, int len, int col, int g)
+    // (Wherever t0 lies: what is asked for is in the cache, and `ok` says what of it counts.)
+    __device__ __forceinline__ void load(const ScoreParams& p, int seq, int head, int from, int len, int col, int g)
     {
         const CacheView& c = p.c;
+        const int t0 = from < len ? from : (len - 1) / (16 * TILES) * (16 * TILES);
         const int D = EXACT ? DP : c.D;
         const_int* table = (const_int*)(uintptr_t)c.table + (size_t)seq * c.max_pages;
+        if ((16 * TILES - 1) >> c.page_shift == 0) {                                    // (t0 is a multiple of 16 TILES: one page)
+            const int found = table[t0 >> c.page_shift];
+            const bool in = (unsigned)found < (unsigned)c.pages;
+            const int tiles = (len - t0 + 15) / 16;
+            ok = in ? tiles < TILES ? (1 << tiles) - 1 : (1 << TILES) - 1 : 0;          // (places behind the last token are in the page too)
+            const int page = in ? found : 0, slot = t0 & ((1 << c.page_shift) - 1);
+            const size_t at = (((size_t)page * c.Hk + head) << c.page_shift) + slot;
+#pragma unroll
+            for (int n = 0; n < TILES; ++n) {
+                token[n] = at + 16 * n;
+                take_tile(c, D, n, at, 16 * n, scales_at(c, page, head), slot, col, g);
+            }
+            return;
+        }
         ok = 0;
 #pragma unroll
         for (int n = 0; n < TILES; ++n) {
@@ -77,40 +103,54 @@ struct Codes {
             const bool in = (unsigned)found < (unsigned)c.pages && t0 + 16 * n < len;
             ok |= in ? 1 << n : 0;
             const int page = in ? found : 0, slot = (t0 + 16 * n) & ((1 << c.page_shift) - 1);
-            const size_t at = page_at(c, page, head) + (size_t)slot * D;                // (uniform)
-            if constexpr (FOUR) {
-                const unsigned char* row = c.k + at / 2 + col * (D / 2);
-                const uint32_t* runs = reinterpret_cast<const uint32_t*>(c.k_scales) + runs_at(c, page, head, slot) + col * c.runs;
+            token[n] = (((size_t)page * c.Hk + head) << c.page_shift) + slot;
+            take_tile(c, D, n, token[n], 0, scales_at(c, page, head), slot - 16 * n, col, g);
+        }
+    }
+
+    // Tile n: its first token is the `ahead`-th behind token `at` of the pool, at slot slot0 + 16 n of its page, whose scales begin at scale0.  (at, scale0 and
+    // slot0 are the same for all lanes, what is added to them fits into 32 bits.)
+    __device__ __forceinline__ void take_tile(const CacheView& c, int D, int n, size_t at, int ahead, size_t scale0, int slot0, int col, int g)
+    {
+        if constexpr (FOUR) {
+            const unsigned char* rows = c.k + at * (size_t)(D / 2);
+            const unsigned char* runs = reinterpret_cast<const unsigned char*>(c.k_scales) + at * (size_t)(4 * c.runs);
 #pragma unroll
-                for (int j = 0; j < (DP + 127) / 128; ++j) {
-                    const int given = operand_dim<TYPE, DP>(4 * j, g), d = EXACT || given < D ? given : 0;
-                    so[n][j] = runs[d >> c.run_shift];
-                    if constexpr (DP < 128) {
-                        const u32x2_t x = *reinterpret_cast<const u32x2_t*>(row + d / 2);
-                        w[n][0] = x[0]; w[n][1] = x[1];
-                    } else {
-                        const u32x4_t x = *reinterpret_cast<const u32x4_t*>(row + d / 2);
+            for (int j = 0; j < (DP + 127) / 128; ++j) {
+                const int given = operand_dim<TYPE, DP>(4 * j, g), d = EXACT || given < D ? given : 0;
+                so[n][j] = *reinterpret_cast<const uint32_t*>(runs + (uint32_t)(((ahead + col) * c.runs + (d >> c.run_shift)) * 4));
+                const unsigned char* from = rows + (uint32_t)(((ahead + col) * D + d) / 2);
+                if constexpr (DP < 128) {
+                    const u32x2_t x = *reinterpret_cast<const u32x2_t*>(from);
+                    w[n][0] = x[0]; w[n][1] = x[1];
+                } else {
+                    const u32x4_t x = *reinterpret_cast<const u32x4_t*>(from);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) w[n][4 * j + i] = x[i];
-                    }
+                    for (int i = 0; i < 4; ++i) w[n][4 * j + i] = x[i];
                 }
-            } else {
-                constexpr int SIZE = HALF ? 2 : 1;
-                const unsigned char* row = c.k + at * SIZE + col * D * SIZE;
+            }
+        } else {
+            constexpr int SIZE = HALF ? 2 : 1;
+            const unsigned char* rows = c.k + at * (size_t)(D * SIZE);
 #pragma unroll
-                for (int j = 0; j < DP / 64; ++j) {
-                    const int given = 64 * j + 16 * g, d = EXACT || given < D ? given : 0;
+            for (int j = 0; j < DP / 64; ++j) {
+                const int given = 64 * j + 16 * g, d = EXACT || given < D ? given : 0;
 #pragma unroll
-                    for (int h = 0; h < SIZE; ++h) {
-                        const u32x4_t x = *reinterpret_cast<const u32x4_t*>(row + d * SIZE + 16 * h);
+                for (int h = 0; h < SIZE; ++h) {
+                    const u32x4_t x = *reinterpret_cast<const u32x4_t*>(rows + (uint32_t)(((ahead + col) * D + d) * SIZE + 16 * h));
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) w[n][(j * SIZE + h) * 4 + i] = x[i];
-                    }
+                    for (int i = 0; i < 4; ++i) w[n][(j * SIZE + h) * 4 + i] = x[i];
                 }
-                if constexpr (SCALED) {
-                    const float* s = c.k_scales + scales_at(c, page, head);
+            }
+            if constexpr (SCALED) {
+                const float* s = c.k_scales + scale0;
+                const int slot = slot0 + 16 * n + 4 * g;
+                if (c.block_shift >= 2) {
+                    const float x = s[slot >> c.block_shift];
+                    by[n] = float4_t{x, x, x, x};
+                } else {
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) by[n][r] = s[(slot + 4 * g + r) >> c.block_shift];
+                    for (int r = 0; r < 4; ++r) by[n][r] = s[(slot + r) >> c.block_shift];
                 }
             }
         }
@@ -146,34 +186,63 @@ struct Keys {
     }
 };
 
-// Rows from .. from + count - 1 of the queries in query heads `head` r .. + r - 1 into LDS, as right operands [tile][part][lane][8]; rows of queries that are none are zeros.
-template <int TYPE, int DP>
-__device__ __forceinline__ void load_rows(const ScoreParams& p, const Queries& qs, int head, int from, int count, int D, _Float16* to)
+// Rows are worked on 32 at a time: two tiles, so that one's instructions fill the other's waits.
+constexpr int kPair = 2, kPairRows = 16 * kPair;
+
+// A row of a sequence and key head: query row / r of the sequence, query head `head` r + row % r.  Stepping on by 16 rows takes no division.
+struct Row {
+    int query, head;
+    __device__ __forceinline__ Row(int row, int r) : query(row / r), head(row - row / r * r) {}
+    __device__ __forceinline__ void next(int rows_q, int rows_h, int r)
+    {
+        query += rows_q;
+        head += rows_h;
+        const bool past = head >= r;
+        query += past ? 1 : 0;
+        head -= past ? r : 0;
+    }
+};
+
+// Rows from .. from + count - 1 into LDS, as right operands [tile][part][lane][8]; rows of queries that are none are zeros.
+template <int DP>
+__device__ __forceinline__ void load_rows(const ScoreParams& p, const Queries& qs, int head, int from, int count, int D, int type_is_four, _Float16* to)
 {
-    constexpr int PARTS = DP / 32;
-    const int pieces = (count + 15) / 16 * PARTS * kWave;
-    for (int i = threadIdx.x; i < pieces; i += kScoreThreads) {
-        const int lane = i % kWave, part = i / kWave % PARTS, row = from + i / (kWave * PARTS) * 16 + (lane & 15), d = operand_dim<TYPE, DP>(part, lane >> 4);
-        half8_t x = {0, 0, 0, 0, 0, 0, 0, 0};
-        if (row < from + count && d < D) x = *reinterpret_cast<const half8_t*>(p.q + (size_t)(qs.row0 + row / p.r) * p.q_stride + (size_t)(head * p.r + row % p.r) * D + d);
-        *reinterpret_cast<half8_t*>(to + (size_t)i * 8) = x;
+    constexpr int PARTS = DP / 32, TILES = kScoreWaves / (PARTS < kScoreWaves ? PARTS : kScoreWaves);      // that the workgroup takes at once
+    const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), col = lane & 15, g = lane >> 4;
+    const int tile0 = wave / PARTS, step = 16 * TILES;
+    Row row(from + 16 * tile0 + col, p.r);
+    for (int i = 16 * tile0 + col; i < ceil_div(count, kPairRows) * kPairRows; i += step) {
+        const _Float16* q = p.q + (size_t)(qs.row0 + row.query) * p.q_stride + (size_t)(head * p.r + row.head) * D;
+#pragma unroll
+        for (int k = 0; k < (PARTS + kScoreWaves - 1) / kScoreWaves; ++k) {
+            const int part = wave % PARTS + k * kScoreWaves;
+            const int d = type_is_four ? operand_dim<CODEGEMM_KV_INT4, DP>(part, g) : operand_dim<CODEGEMM_KV_FP16, DP>(part, g);
+            half8_t x = {0, 0, 0, 0, 0, 0, 0, 0};
+            if (i < count && d < D) x = *reinterpret_cast<const half8_t*>(q + d);
+            *reinterpret_cast<half8_t*>(to + ((size_t)(i / 16 * PARTS + part) * kWave + lane) * 8) = x;
+        }
+        row.next(step / p.r, step % p.r, p.r);
     }
 }
 
-// 16 rows against the wavefront's keys; a lane's scores are those of row `col` for tokens 4 g + r of every tile, before they are scaled.  (Scaled scores are rounded
-// before a maximum is taken off, everywhere alike: fused, the largest score's own weight would be off by what large scores are rounded by.)
+// 32 rows against the wavefront's keys; a lane's scores are those of rows `col` and 16 + `col` for tokens 4 g + r of every tile of keys, before they are scaled.  (Scaled scores are
+// rounded before a maximum is taken off, everywhere alike: fused, the largest score's own weight would be off by what large scores are rounded by.)
 template <int TYPE, int DP, bool EXACT>
-__device__ __forceinline__ void score_tile(const Keys<TYPE, DP, EXACT>& keys, const _Float16* rows, int lane, float4_t (&s)[score_tiles(DP)])
+__device__ __forceinline__ void score_pair(const Keys<TYPE, DP, EXACT>& keys, const _Float16* rows, int lane, float4_t (&s)[kPair][score_tiles(DP)])
 {
     constexpr int TILES = score_tiles(DP), PARTS = DP / 32;
 #pragma unroll
-    for (int n = 0; n < TILES; ++n) s[n] = float4_t{0, 0, 0, 0};
+    for (int k = 0; k < kPair; ++k)
 #pragma unroll
-    for (int i = 0; i < PARTS; ++i) {
-        const half8_t q = *reinterpret_cast<const half8_t*>(rows + (size_t)(i * kWave + lane) * 8);
+        for (int n = 0; n < TILES; ++n) s[k][n] = float4_t{0, 0, 0, 0};
 #pragma unroll
-        for (int n = 0; n < TILES; ++n) s[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(keys.k[n][i], q, s[n], 0, 0, 0);
-    }
+    for (int i = 0; i < PARTS; ++i)
+#pragma unroll
+        for (int k = 0; k < kPair; ++k) {
+            const half8_t q = *reinterpret_cast<const half8_t*>(rows + (size_t)((k * PARTS + i) * kWave + lane) * 8);
+#pragma unroll
+            for (int n = 0; n < TILES; ++n) s[k][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(keys.k[n][i], q, s[k][n], 0, 0, 0);
+        }
 }
 
 // Which tokens of its row a lane sees: t - t0 in lo .. hi, in tiles that have a page.
@@ -186,84 +255,107 @@ __device__ __forceinline__ Seen seen_of(const ScoreParams& p, const Queries& qs,
 {
     return Seen{first_seen(p, at) - t0, (at < qs.len ? at : qs.len - 1) - t0, keys.ok};
 }
-// Whether rows row .. row + 15 all see all of a wavefront's tokens.
+// Whether 32 rows all see all of a wavefront's tokens.
 template <class T>
 __device__ __forceinline__ bool see_all(const ScoreParams& p, const Queries& qs, const int* at, int t0, const T& keys)
 {
-    const int first = __builtin_amdgcn_readfirstlane(at[0]), last = __builtin_amdgcn_readfirstlane(at[15]);
+    const int first = __builtin_amdgcn_readfirstlane(at[0]), last = __builtin_amdgcn_readfirstlane(at[kPairRows - 1]);
     return keys.ok == (1 << T::TILES) - 1 && t0 + 16 * T::TILES - 1 <= first && t0 >= first_seen(p, last);
 }
 
-// What a workgroup keeps in LDS of up to kRowsAtOnce rows: the right operands, positions, and per wavefront (STATS) or once what is known of their weights.
+// What a workgroup keeps in LDS of up to `many` rows: the right operands, positions, and once, or (stats) for every wavefront, what is known of their weights.
 template <int DP>
 struct RowSpace {
     _Float16* rows;         // [tile][part][lane][8]
     Pair* sums;
     int* at;
-    __device__ __forceinline__ explicit RowSpace(unsigned char* smem)
-        : rows(reinterpret_cast<_Float16*>(smem)), sums(reinterpret_cast<Pair*>(smem + (size_t)kRowsAtOnce * DP * 2)), at(reinterpret_cast<int*>(sums + kScoreWaves * kRowsAtOnce))
+    __device__ __forceinline__ RowSpace(unsigned char* smem, int many, int copies)
+        : rows(reinterpret_cast<_Float16*>(smem)), sums(reinterpret_cast<Pair*>(smem + (size_t)many * DP * 2)), at(reinterpret_cast<int*>(sums + many * copies))
     {
     }
-    static constexpr size_t bytes = (size_t)kRowsAtOnce * DP * 2 + kScoreWaves * kRowsAtOnce * sizeof(Pair) + kRowsAtOnce * sizeof(int);
+    static size_t bytes(int many, int copies) { return (size_t)many * (DP * 2 + copies * sizeof(Pair) + sizeof(int)); }
 };
 __device__ __forceinline__ void load_positions(const ScoreParams& p, const Queries& qs, int from, int count, int* at)
 {
-    for (int i = threadIdx.x; i < (count + 15) / 16 * 16; i += kScoreThreads) at[i] = qs.at + (from + i) / p.r;
+    for (int i = threadIdx.x; i < ceil_div(count, kPairRows) * kPairRows; i += kScoreThreads) at[i] = qs.at + (from + i) / p.r;
 }
 
 // Workgroup (sequence and key head, slot, z): rows z * 128 .. and on, over every slots-th block of keys.
 template <int TYPE, int DP, bool EXACT>
-__global__ void __launch_bounds__(kScoreThreads, DP == 256 ? 2 : 3) score_stats_kernel(const ScoreParams p)
+__global__ void __launch_bounds__(kScoreThreads, 2) score_stats_kernel(const ScoreParams p)
 {
-    constexpr int TILES = score_tiles(DP), PARTS = DP / 32, BLOCK = 16 * TILES * kScoreWaves;
+    constexpr int TILES = score_tiles(DP), BLOCK = 16 * TILES * kScoreWaves;
     extern __shared__ __align__(16) unsigned char smem[];
-    const RowSpace<DP> space(smem);
+    constexpr bool AHEAD = TYPE == CODEGEMM_KV_INT4;                                   // wider codes would not fit into the registers beside the operands
+    const int many = p.many;
+    const RowSpace<DP> space(smem, many, kScoreWaves);
     const int D = EXACT ? DP : p.c.D, tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave), col = lane & 15, g = lane >> 4;
     const int seq = blockIdx.x / p.c.Hk, head = blockIdx.x % p.c.Hk;
     const Queries qs = queries_of(p, seq);
     const int count_all = qs.n * p.r, lowest = first_seen(p, qs.at) / BLOCK * BLOCK;   // of the first query's keys
-    for (int from = blockIdx.z * kRowsAtOnce; from < count_all; from += gridDim.z * kRowsAtOnce) {
-        const int count = count_all - from < kRowsAtOnce ? count_all - from : kRowsAtOnce;
+    for (int from = blockIdx.z * many; from < count_all; from += gridDim.z * many) {
+        const int count = count_all - from < many ? count_all - from : many;
+        int b = lowest + blockIdx.y * BLOCK;
+        Codes<TYPE, DP, EXACT> codes;
+        if (b < qs.len) codes.load(p, seq, head, b + wave * 16 * TILES, qs.len, col, g);
         __syncthreads();
-        load_rows<TYPE, DP>(p, qs, head, from, count, D, space.rows);
+        load_rows<DP>(p, qs, head, from, count, D, TYPE == CODEGEMM_KV_INT4, space.rows);
         load_positions(p, qs, from, count, space.at);
-        for (int i = tid; i < kScoreWaves * kRowsAtOnce; i += kScoreThreads) space.sums[i] = Pair{-INFINITY, 0.0f};
+        for (int i = tid; i < kScoreWaves * many; i += kScoreThreads) space.sums[i] = Pair{-INFINITY, 0.0f};
         __syncthreads();
-        for (int b = lowest + blockIdx.y * BLOCK; b < qs.len; b += p.slots * BLOCK) {
+        for (; b < qs.len; b += p.slots * BLOCK) {
             const int t0 = b + wave * 16 * TILES;
-            if (t0 >= qs.len) continue;
-            Codes<TYPE, DP, EXACT> codes;
             Keys<TYPE, DP, EXACT> keys;
-            codes.load(p, seq, head, t0, qs.len, col, g);
+            if (!AHEAD && b != lowest + (int)blockIdx.y * BLOCK) codes.load(p, seq, head, t0, qs.len, col, g);
             keys.take(codes, p, g);
-            for (int tile = 0; 16 * tile < count; ++tile) {
-                float4_t s[TILES];
-                score_tile<TYPE, DP, EXACT>(keys, space.rows + (size_t)tile * PARTS * kWave * 8, lane, s);
-                Pair* mine = space.sums + wave * kRowsAtOnce + 16 * tile + col;
-                const Pair old = *mine;
-                auto add = [&](auto is_whole, const Seen& seen) {
+            if (AHEAD) {
+                __builtin_amdgcn_sched_barrier(0);                                     // (the next codes come into the same registers)
+                if (qs.len - b > p.slots * BLOCK) codes.load(p, seq, head, t0 + p.slots * BLOCK, qs.len, col, g);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (t0 >= qs.len) continue;
+            for (int row = 0; row < count; row += kPairRows) {
+                float4_t s[kPair][TILES];
+                score_pair<TYPE, DP, EXACT>(keys, space.rows + (size_t)row * DP, lane, s);
+                Pair* mine = space.sums + wave * many + row + col;
+                const Pair old[kPair] = {mine[0], mine[16]};
+                auto add = [&](auto is_whole) {
                     constexpr bool whole = decltype(is_whole)::value;
-                    float most = -INFINITY;
+                    float most[kPair], sum[kPair], base[kPair], m[kPair];
+#pragma unroll
+                    for (int k = 0; k < kPair; ++k) {
+                        const Seen seen = whole ? Seen{} : seen_of(p, qs, space.at[row + 16 * k + col], t0, keys);
+                        most[k] = -INFINITY;
+#pragma unroll
+                        for (int n = 0; n < TILES; ++n)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) {
+                                s[k][n][r] *= keys.by[n][r];
+                                if (!whole) s[k][n][r] = seen(n, r, g) ? s[k][n][r] : -INFINITY;
+                                most[k] = fmaxf(most[k], s[k][n][r]);
+                            }
+                    }
+#pragma unroll
+                    for (int k = 0; k < kPair; ++k) {
+                        most[k] = over_groups(most[k], [](float a, float c) { return fmaxf(a, c); });
+                        m[k] = fmaxf(old[k].a, most[k]);
+                        base[k] = m[k] == -INFINITY ? 0.0f : m[k];
+                        sum[k] = 0.0f;
+                    }
 #pragma unroll
                     for (int n = 0; n < TILES; ++n)
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            s[n][r] *= keys.by[n][r];
-                            if (!whole) s[n][r] = seen(n, r, g) ? s[n][r] : -INFINITY;
-                            most = fmaxf(most, s[n][r]);
-                        }
-                    most = over_groups(most, [](float a, float c) { return fmaxf(a, c); });
-                    const float m = fmaxf(old.a, most), base = m == -INFINITY ? 0.0f : m;
-                    float sum = 0.0f;
+                        for (int r = 0; r < 4; ++r)
 #pragma unroll
-                    for (int n = 0; n < TILES; ++n)
+                            for (int k = 0; k < kPair; ++k) sum[k] += __builtin_amdgcn_exp2f(s[k][n][r] - base[k]);
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) sum += __builtin_amdgcn_exp2f(s[n][r] - base);
-                    sum = over_groups(sum, [](float a, float c) { return a + c; });
-                    if (g == 0) *mine = Pair{m, __builtin_fmaf(old.b, __builtin_amdgcn_exp2f(old.a - base), sum)};
+                    for (int k = 0; k < kPair; ++k) {
+                        sum[k] = over_groups(sum[k], [](float a, float c) { return a + c; });
+                        if (g == 0) mine[16 * k] = Pair{m[k], __builtin_fmaf(old[k].b, __builtin_amdgcn_exp2f(old[k].a - base[k]), sum[k])};
+                    }
                 };
-                if (see_all(p, qs, space.at + 16 * tile, t0, keys)) add(std::true_type(), Seen{});
-                else add(std::false_type(), seen_of(p, qs, space.at[16 * tile + col], t0, keys));
+                if (see_all(p, qs, space.at + row, t0, keys)) add(std::true_type());
+                else add(std::false_type());
             }
         }
         __syncthreads();
@@ -271,14 +363,42 @@ __global__ void __launch_bounds__(kScoreThreads, DP == 256 ? 2 : 3) score_stats_
             const Pair* state = space.sums + i;
             float m = -INFINITY, sum = 0.0f;
 #pragma unroll
-            for (int w = 0; w < kScoreWaves; ++w) m = fmaxf(m, state[w * kRowsAtOnce].a);
+            for (int w = 0; w < kScoreWaves; ++w) m = fmaxf(m, state[w * many].a);
             const float base = m == -INFINITY ? 0.0f : m;
 #pragma unroll
-            for (int w = 0; w < kScoreWaves; ++w) sum += state[w * kRowsAtOnce].b * __builtin_amdgcn_exp2f(state[w * kRowsAtOnce].a - base);
+            for (int w = 0; w < kScoreWaves; ++w) sum += state[w * many].b * __builtin_amdgcn_exp2f(state[w * many].a - base);
             const int row = from + i;
             p.part[(size_t)blockIdx.y * p.rows + (size_t)(qs.row0 + row / p.r) * (p.c.Hk * p.r) + head * p.r + row % p.r] = Pair{m, sum};
         }
     }
+}
+
+// x of the lane whose `col` has another bit 8, 4, 2 or 1.
+template <int BIT>
+__device__ __forceinline__ float other_column(float x)
+{
+    const int w = __builtin_bit_cast(int, x);
+    if constexpr (BIT == 8) return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, w, 0x128, 0xf, 0xf, false));        // row_ror 8
+    else if constexpr (BIT == 4) return __builtin_bit_cast(float, __builtin_amdgcn_ds_swizzle(w, 0x101f));                        // xor 4
+    else if constexpr (BIT == 2) return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, w, 0x4e, 0xf, 0xf, false));    // quad_perm 2 3 0 1
+    else return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, w, 0xb1, 0xf, 0xf, false));                             // quad_perm 1 0 3 2
+}
+// Sums of N (8 or 16) values over the 16 columns: value i in the lanes of column i (and i + 8).
+template <int N, int BIT = 8>
+__device__ __forceinline__ void over_columns(float (&x)[N], int col)
+{
+    if constexpr (BIT >= N) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] += other_column<BIT>(x[i]);
+    } else {
+        const bool up = col & BIT;
+#pragma unroll
+        for (int i = 0; i < BIT; ++i) {
+            const float keep = up ? x[i + BIT] : x[i], give = up ? x[i] : x[i + BIT];
+            x[i] = keep + other_column<BIT>(give);
+        }
+    }
+    if constexpr (BIT > 1) over_columns<N, BIT / 2>(x, col);
 }
 
 // A row's parts, in order.
@@ -287,10 +407,18 @@ __global__ void __launch_bounds__(kScoreThreads) score_join_kernel(const ScorePa
     const int row = blockIdx.x * kScoreThreads + threadIdx.x;
     if (row >= p.rows) return;
     float m = -INFINITY, sum = 0.0f;
-    for (int i = 0; i < p.slots; ++i) {
-        const Pair x = p.part[(size_t)i * p.rows + row];
-        const float now = fmaxf(m, x.a), base = now == -INFINITY ? 0.0f : now;
-        sum = sum * __builtin_amdgcn_exp2f(m - base) + x.b * __builtin_amdgcn_exp2f(x.a - base);
+    constexpr int AT_ONCE = 8;
+    for (int i0 = 0; i0 < p.slots; i0 += AT_ONCE) {
+        Pair x[AT_ONCE];
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) x[i] = p.part[(size_t)(i0 + i < p.slots ? i0 + i : i0) * p.rows + row];
+        float now = m;
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) now = fmaxf(now, x[i].a);
+        const float base = now == -INFINITY ? 0.0f : now;
+        sum *= __builtin_amdgcn_exp2f(m - base);
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) sum += i0 + i < p.slots ? x[i].b * __builtin_amdgcn_exp2f(x[i].a - base) : 0.0f;
         m = now;
     }
     p.stats[row] = sum == 0.0f ? Pair{0.0f, 0.0f} : Pair{m, 1.0f / sum};
@@ -298,11 +426,12 @@ __global__ void __launch_bounds__(kScoreThreads) score_join_kernel(const ScorePa
 
 // Workgroup (sequence and key head, slot): every slots-th block of keys, all rows.  The next block's codes are on their way while one is worked on.
 template <int TYPE, int DP, bool EXACT>
-__global__ void __launch_bounds__(kScoreThreads, DP == 256 || (DP == 128 && TYPE != CODEGEMM_KV_INT4) ? 2 : 3) score_sum_kernel(const ScoreParams p)
+__global__ void __launch_bounds__(kScoreThreads, DP == 256 || (DP == 128 && TYPE != CODEGEMM_KV_INT4) ? 2 : SB4) score_sum_kernel(const ScoreParams p)
 {
-    constexpr int TILES = score_tiles(DP), PARTS = DP / 32, BLOCK = 16 * TILES * kScoreWaves, VALUES = 4 * TILES;
+    constexpr int TILES = score_tiles(DP), BLOCK = 16 * TILES * kScoreWaves, VALUES = 4 * TILES;
     extern __shared__ __align__(16) unsigned char smem[];
-    const RowSpace<DP> space(smem);
+    const int many = p.many;
+    const RowSpace<DP> space(smem, many, 1);
     const int D = EXACT ? DP : p.c.D, tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave), col = lane & 15, g = lane >> 4;
     const int seq = blockIdx.x / p.c.Hk, head = blockIdx.x % p.c.Hk;
     const Queries qs = queries_of(p, seq);
@@ -311,87 +440,179 @@ __global__ void __launch_bounds__(kScoreThreads, DP == 256 || (DP == 128 && TYPE
     int b = blockIdx.y * BLOCK;
     if (b >= qs.len) return;
     auto load = [&](int from) {
-        const int count = count_all - from < kRowsAtOnce ? count_all - from : kRowsAtOnce;
+        const int count = count_all - from < many ? count_all - from : many;
         __syncthreads();
-        load_rows<TYPE, DP>(p, qs, head, from, count, D, space.rows);
+        load_rows<DP>(p, qs, head, from, count, D, TYPE == CODEGEMM_KV_INT4, space.rows);
         load_positions(p, qs, from, count, space.at);
-        for (int i = tid; i < (count + 15) / 16 * 16; i += kScoreThreads) {
+        for (int i = tid; i < ceil_div(count, kPairRows) * kPairRows; i += kScoreThreads) {
             const int row = from + i;
             space.sums[i] = i < count ? p.stats[(size_t)(qs.row0 + row / p.r) * (p.c.Hk * p.r) + head * p.r + row % p.r] : Pair{0.0f, 0.0f};
         }
         __syncthreads();
         return count;
     };
+    // what a lane's token had before (where nothing says so: what lies in its place, which is not looked at) comes with its block's codes
+    const float* earlier = p.earlier ? p.earlier : p.scores;
+    const int tile_of = (col >> 2) & (TILES - 1), in_tile = 4 * g + (col & 3);
     Codes<TYPE, DP, EXACT> codes;
-    if (active(b + wave * 16 * TILES)) codes.load(p, seq, head, b + wave * 16 * TILES, qs.len, col, g);
-    const bool once = count_all <= kRowsAtOnce;                                        // the rows stay
+    size_t place_next;
+    float had_next;
+    auto ask = [&](int from) {
+        codes.load(p, seq, head, from, qs.len, col, g);
+        place_next = codes.token[0];
+#pragma unroll
+        for (int n = 1; n < TILES; ++n) place_next = tile_of == n ? codes.token[n] : place_next;
+        place_next += in_tile;
+        had_next = earlier[place_next];
+    };
+    ask(b + wave * 16 * TILES);
+    const bool once = count_all <= many;                                               // the rows stay
     if (once) load(0);
+    // A block's result is stored after the next block's codes have come: the wait for these is one for all that is under way.
+    size_t place_last = 0;
+    float last = 0.0f;
+    bool to_store = false;
     for (; b < qs.len; b += p.slots * BLOCK) {
-        const int t0 = b + wave * 16 * TILES, t_next = t0 + p.slots * BLOCK;
+        const int t0 = b + wave * 16 * TILES, t = t0 + 16 * tile_of + in_tile;
         const bool mine = active(t0);
         Keys<TYPE, DP, EXACT> keys;
-        if (mine) keys.take(codes, p, g);
-        if (t_next > t0 && active(t_next)) codes.load(p, seq, head, t_next, qs.len, col, g);
+        keys.take(codes, p, g);
+        const size_t place = place_next;
+        const float had = had_next;
+        __builtin_amdgcn_sched_barrier(0);                                             // (the next codes come into the same registers)
+        if (to_store) p.scores[place_last] = last;
+        if (qs.len - b > p.slots * BLOCK) ask(t0 + p.slots * BLOCK);
+        __builtin_amdgcn_sched_barrier(0);
         float sum[VALUES];
 #pragma unroll
         for (int i = 0; i < VALUES; ++i) sum[i] = 0.0f;
         if (b + BLOCK > lowest) {                                                      // uniform
-            for (int from = 0; from < count_all; from += kRowsAtOnce) {
+            for (int from = 0; from < count_all; from += many) {
                 const int count = once ? count_all : load(from);
                 if (!mine) continue;
-                for (int tile = 0; 16 * tile < count; ++tile) {
-                    float4_t s[TILES];
-                    score_tile<TYPE, DP, EXACT>(keys, space.rows + (size_t)tile * PARTS * kWave * 8, lane, s);
-                    const Pair st = space.sums[16 * tile + col];
-                    auto add = [&](auto is_whole, const Seen& seen) {
+                for (int row = 0; row < count; row += kPairRows) {
+                    float4_t s[kPair][TILES];
+                    score_pair<TYPE, DP, EXACT>(keys, space.rows + (size_t)row * DP, lane, s);
+                    const Pair st[kPair] = {space.sums[row + col], space.sums[row + 16 + col]};
+                    auto add = [&](auto is_whole) {
                         constexpr bool whole = decltype(is_whole)::value;
 #pragma unroll
-                        for (int n = 0; n < TILES; ++n)
+                        for (int k = 0; k < kPair; ++k) {
+                            const Seen seen = whole ? Seen{} : seen_of(p, qs, space.at[row + 16 * k + col], t0, keys);
 #pragma unroll
-                            for (int r = 0; r < 4; ++r) {
-                                const float w = __builtin_amdgcn_exp2f(s[n][r] * keys.by[n][r] - st.a), more = __builtin_fmaf(w, st.b, sum[4 * n + r]);
-                                sum[4 * n + r] = whole || (seen(n, r, g) && st.b != 0.0f) ? more : sum[4 * n + r];
-                            }
+                            for (int n = 0; n < TILES; ++n)
+#pragma unroll
+                                for (int r = 0; r < 4; ++r) {
+                                    const float w = __builtin_amdgcn_exp2f(s[k][n][r] * keys.by[n][r] - st[k].a), more = __builtin_fmaf(w, st[k].b, sum[4 * n + r]);
+                                    sum[4 * n + r] = whole || (seen(n, r, g) && st[k].b != 0.0f) ? more : sum[4 * n + r];
+                                }
+                        }
                     };
                     // (rows that are none have no weight in the first form either: a score of 0, and 1 / sum 0)
-                    if (see_all(p, qs, space.at + 16 * tile, t0, keys)) add(std::true_type(), Seen{});
-                    else add(std::false_type(), seen_of(p, qs, space.at[16 * tile + col], t0, keys));
+                    if (see_all(p, qs, space.at + row, t0, keys)) add(std::true_type());
+                    else add(std::false_type());
                 }
             }
         }
         // Over the 16 rows: lanes that differ in a bit of `col` share out the tokens by it, as long as there are several.
-        int left = VALUES;
-#pragma unroll
-        for (int bit = 8; bit > 0; bit >>= 1) {
-            if (VALUES > bit) {
-                left = bit;
-#pragma unroll
-                for (int i = 0; i < VALUES; ++i) {
-                    if (i >= left) break;
-                    const float keep = col & bit ? sum[i + bit] : sum[i], give = col & bit ? sum[i] : sum[i + bit];
-                    sum[i] = keep + __shfl_xor(give, bit);
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < VALUES; ++i) sum[i] += __shfl_xor(sum[i], bit);
-            }
-        }
-        // token: tile col / 4, row 4 g + col % 4
-        const int t = t0 + 16 * (col >> 2) + 4 * g + (col & 3);
-        if (t0 < qs.len && t < qs.len && col < VALUES) {
-            const int page = page_of(p.c, seq, t >> p.c.page_shift);
-            if (page >= 0) {
-                const size_t at = (((size_t)page * p.c.Hk + head) << p.c.page_shift) + (t & ((1 << p.c.page_shift) - 1));
-                p.scores[at] = (p.earlier && t < fresh ? p.earlier[at] : 0.0f) + sum[0];
-            }
-        }
+        over_columns<VALUES>(sum, col);
+        to_store = t < qs.len && col < VALUES && (keys.ok >> tile_of & 1);
+        place_last = place;
+        last = (p.earlier && t < fresh ? had : 0.0f) + sum[0];
     }
+    if (to_store) p.scores[place_last] = last;
+}
+
+// Up to 16 rows, as single tokens have where a key head serves no more query heads: they stay in registers, and a wavefront goes through its blocks of keys by
+// itself, the next one's codes under way.  Wavefront (sequence and key head, 4 slots and its own).
+template <int TYPE, int DP, bool EXACT>
+__global__ void __launch_bounds__(kScoreThreads, DP >= 128 && TYPE == CODEGEMM_KV_FP16 ? 2 : 3) score_few_kernel(const ScoreParams p)
+{
+    constexpr int TILES = score_tiles(DP), PARTS = DP / 32, BLOCK = 16 * TILES, VALUES = 4 * TILES;
+    const int D = EXACT ? DP : p.c.D, tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave), col = lane & 15, g = lane >> 4;
+    const int seq = blockIdx.x / p.c.Hk, head = blockIdx.x % p.c.Hk;
+    const Queries qs = queries_of(p, seq);
+    const int stride = p.slots * kScoreWaves * BLOCK;
+    int t0 = ((int)blockIdx.y * kScoreWaves + wave) * BLOCK;
+    if (t0 >= qs.len) return;
+    const int rows = qs.n * p.r, lowest = first_seen(p, qs.at), fresh = p.first ? p.first[seq] : qs.at;
+    const float* earlier = p.earlier ? p.earlier : p.scores;        // (where nothing says so: what lies in its place, which is not looked at)
+    const int tile_of = (col >> 2) & (TILES - 1), in_tile = 4 * g + (col & 3);
+    Codes<TYPE, DP, EXACT> codes;
+    size_t place_next;
+    float had_next;
+    auto ask = [&](int from) {
+        codes.load(p, seq, head, from, qs.len, col, g);
+        place_next = codes.token[0];
+#pragma unroll
+        for (int n = 1; n < TILES; ++n) place_next = tile_of == n ? codes.token[n] : place_next;
+        place_next += in_tile;
+        had_next = earlier[place_next];
+    };
+    ask(t0);
+    // The lane's row: its operands, where it stands, what its weights' logarithms lie below and 1 / their sum.
+    const int query = col / p.r, at = qs.at + (col < rows ? query : 0);
+    half8_t q[PARTS];
+#pragma unroll
+    for (int i = 0; i < PARTS; ++i) {
+        half8_t x = {0, 0, 0, 0, 0, 0, 0, 0};
+        const int d = operand_dim<TYPE, DP>(i, g);
+        if (col < rows && d < D) x = *reinterpret_cast<const half8_t*>(p.q + (size_t)(qs.row0 + query) * p.q_stride + (size_t)(head * p.r + col - query * p.r) * D + d);
+        q[i] = x;
+    }
+    Pair st = {0.0f, 0.0f};
+    if (col < rows) st = p.stats[(size_t)(qs.row0 + query) * (p.c.Hk * p.r) + head * p.r + col - query * p.r];
+    const int seen_from = first_seen(p, qs.at + (qs.n > 0 ? qs.n - 1 : 0));                 // by all rows, up to the first one's position
+    size_t place_last = 0;
+    float last = 0.0f;
+    bool to_store = false;
+    for (; t0 < qs.len; t0 += stride) {
+        const Codes<TYPE, DP, EXACT> now = codes;
+        const size_t place = place_next;
+        const float had = had_next;
+        const int t = t0 + 16 * tile_of + in_tile, ok = now.ok;
+        // (after the wait for the codes, so that it is not one for this store too)
+        if (to_store) p.scores[place_last] = last;
+        if (qs.len - t0 > stride) ask(t0 + stride);
+        float sum[VALUES];
+#pragma unroll
+        for (int i = 0; i < VALUES; ++i) sum[i] = 0.0f;
+        if (t0 + BLOCK > lowest && rows > 0) {
+            Keys<TYPE, DP, EXACT> keys;
+            keys.take(now, p, g);
+            float4_t s[TILES];
+#pragma unroll
+            for (int n = 0; n < TILES; ++n) s[n] = float4_t{0, 0, 0, 0};
+#pragma unroll
+            for (int i = 0; i < PARTS; ++i)
+#pragma unroll
+                for (int n = 0; n < TILES; ++n) s[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(keys.k[n][i], q[i], s[n], 0, 0, 0);
+            const bool whole = ok == (1 << TILES) - 1 && t0 + BLOCK - 1 <= qs.at && t0 >= seen_from;
+#pragma unroll
+            for (int n = 0; n < TILES; ++n)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) sum[4 * n + r] = __builtin_amdgcn_exp2f(s[n][r] * keys.by[n][r] - st.a) * st.b;
+            if (!whole) {
+                const Seen seen = Seen{first_seen(p, at) - t0, (at < qs.len ? at : qs.len - 1) - t0, ok};
+#pragma unroll
+                for (int n = 0; n < TILES; ++n)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) sum[4 * n + r] = seen(n, r, g) && st.b != 0.0f ? sum[4 * n + r] : 0.0f;
+            }
+        }
+        over_columns<VALUES>(sum, col);
+        to_store = t < qs.len && col < VALUES && (ok >> tile_of & 1);
+        place_last = place;
+        last = (p.earlier && t < fresh ? had : 0.0f) + sum[0];
+    }
+    if (to_store) p.scores[place_last] = last;
 }
 
 namespace {
 
 struct ScorePlan {
-    int slots, z, rows;
+    int slots, sum_slots, few_slots, z, rows;
+    int most;               // rows of a sequence and key head, at most
     size_t part, bytes;     // where parts begin (behind rows' stats), of workspace
 };
 
@@ -408,13 +629,18 @@ int score_plan(const codegemm_kv_cache* cache, const codegemm_attn_desc* d, bool
     if (too_many(items, kScoreThreads)) return CODEGEMM_UNSUPPORTED;
     const int held = cache->max_pages * cache->page_size, longest = d->max_kv < held ? d->max_kv : held;
     const int block = 16 * score_tiles(d->head_dim > 128 ? 256 : 128) * kScoreWaves;
+    const int dp = d->head_dim > 128 ? 256 : d->head_dim > 64 ? 128 : 64, at_once = rows_at_once(dp, true);
     const long long mean = (rows / d->kv_heads + d->num_seqs - 1) / d->num_seqs;           // rows of a sequence and key head
-    p->z = (int)((mean + kRowsAtOnce - 1) / kRowsAtOnce);
+    p->z = (int)((mean + at_once - 1) / at_once);
     p->z = p->z < 1 ? 1 : p->z > 256 ? 256 : p->z;
-    const long long blocks = ceil_div(longest, block), share = (kScoreGroups + items - 1) / items;
-    long long slots = blocks < share ? blocks : share;
+    const long long blocks = ceil_div(longest, block), most = single ? d->q_heads / d->kv_heads : rows / d->kv_heads;
+    auto share = [&](long long groups, long long of) { const long long n = (groups + of - 1) / of; return blocks < n ? blocks : n; };
+    long long slots = share(kStatsGroups, items * p->z);
     if (!single && (size_t)slots * rows * sizeof(Pair) > kMostParts) slots = kMostParts / (rows * sizeof(Pair));
     p->slots = slots < 1 ? 1 : (int)slots;
+    p->sum_slots = (int)share(kSumGroups, items);
+    p->few_slots = (int)share(kFewGroups, items);
+    p->most = most < 1024 ? (int)most : 1024;
     p->rows = (int)rows;
     p->part = kFixedArea + ((size_t)rows * sizeof(Pair) + 255) / 256 * 256;
     p->bytes = p->part + (single ? 0 : (size_t)p->slots * rows * sizeof(Pair));
@@ -444,27 +670,38 @@ ScoreParams score_params(const codegemm_kv_cache* cache, const codegemm_attn_des
     p.r = d->q_heads / d->kv_heads;
     p.q_stride = row_stride(d->q_stride, d->q_heads * d->head_dim);
     p.window = d->window;
-    p.slots = plan.slots;
     p.scale = log2_scale(d->scale);
     return p;
 }
 
 template <int TYPE, int DP, bool EXACT>
-int launch_scores_one(const ScoreParams& p, const ScorePlan& plan, bool stats, hipStream_t s)
+int launch_scores_one(ScoreParams p, const ScorePlan& plan, bool stats, hipStream_t s)
 {
-    const dim3 threads(kScoreThreads), items((unsigned)(p.c.seqs * p.c.Hk), (unsigned)plan.slots);
-    constexpr size_t lds = RowSpace<DP>::bytes;
+    const dim3 threads(kScoreThreads);
+    const unsigned items = (unsigned)(p.c.seqs * p.c.Hk);
+    const int rows = ceil_div(plan.most, kPairRows) * kPairRows;
     if (stats) {
+        p.slots = plan.slots;
+        p.many = rows < rows_at_once(DP, true) ? rows : rows_at_once(DP, true);
         auto fn = score_stats_kernel<TYPE, DP, EXACT>;
+        const size_t lds = RowSpace<DP>::bytes(p.many, kScoreWaves);
         const int st = set_max_lds(reinterpret_cast<const void*>(fn), lds);
         if (st) return st;
-        hipLaunchKernelGGL(fn, dim3(items.x, items.y, (unsigned)plan.z), threads, lds, s, p);
+        hipLaunchKernelGGL(fn, dim3(items, (unsigned)plan.slots, (unsigned)plan.z), threads, lds, s, p);
         hipLaunchKernelGGL(score_join_kernel, dim3((unsigned)ceil_div(p.rows, kScoreThreads)), threads, 0, s, p);
     }
+    if (plan.most <= 16) {
+        p.slots = plan.few_slots;
+        hipLaunchKernelGGL((score_few_kernel<TYPE, DP, EXACT>), dim3(items, (unsigned)p.slots), threads, 0, s, p);
+        return hipGetLastError() == hipSuccess ? CODEGEMM_OK : CODEGEMM_LAUNCH_FAILED;
+    }
+    p.slots = plan.sum_slots;
+    p.many = rows < rows_at_once(DP, false) ? rows : rows_at_once(DP, false);
     auto fn = score_sum_kernel<TYPE, DP, EXACT>;
+    const size_t lds = RowSpace<DP>::bytes(p.many, 1);
     const int st = set_max_lds(reinterpret_cast<const void*>(fn), lds);
     if (st) return st;
-    hipLaunchKernelGGL(fn, items, threads, lds, s, p);
+    hipLaunchKernelGGL(fn, dim3(items, (unsigned)plan.sum_slots), threads, lds, s, p);
     return hipGetLastError() == hipSuccess ? CODEGEMM_OK : CODEGEMM_LAUNCH_FAILED;
 }
 
