@@ -16,15 +16,7 @@ namespace cg {
 constexpr int kScoreWaves = 4;
 constexpr int kScoreThreads = kScoreWaves * kWave;
 constexpr int rows_at_once(int dp, bool stats) { return stats || dp == 256 ? 128 : 256; }       // in LDS, at most
-#ifndef SB4
-#define SB4 2
-#endif
-#ifndef GST
-#define GST 512
-#define GSU 512
-#define GSD 2048
-#endif
-constexpr int kStatsGroups = GST, kSumGroups = GSU, kFewGroups = GSD;          // workgroups that are worth sharing the keys, at least
+constexpr int kStatsGroups = 512, kSumGroups = 512, kFewGroups = 2048;        // workgroups that are worth sharing the keys, at least
 constexpr size_t kMostParts = 32u << 20;    // bytes of rows' parts
 
 // Tokens of a wavefront at once: what leaves room for four (two) wavefronts on a SIMD.
@@ -426,7 +418,7 @@ __global__ void __launch_bounds__(kScoreThreads) score_join_kernel(const ScorePa
 
 // Workgroup (sequence and key head, slot): every slots-th block of keys, all rows.  The next block's codes are on their way while one is worked on.
 template <int TYPE, int DP, bool EXACT>
-__global__ void __launch_bounds__(kScoreThreads, DP == 256 || (DP == 128 && TYPE != CODEGEMM_KV_INT4) ? 2 : SB4) score_sum_kernel(const ScoreParams p)
+__global__ void __launch_bounds__(kScoreThreads, 2) score_sum_kernel(const ScoreParams p)
 {
     constexpr int TILES = score_tiles(DP), BLOCK = 16 * TILES * kScoreWaves, VALUES = 4 * TILES;
     extern __shared__ __align__(16) unsigned char smem[];

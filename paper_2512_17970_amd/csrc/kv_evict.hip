@@ -11,9 +11,22 @@ namespace cg {
 
 constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / kWave;
 constexpr int kKeptKeys = 32768;            // 128 KB, at most
-constexpr int kBins = 2048;
+constexpr int kBins = 2048, kDigits = 3;    // two for each thread
+constexpr int kDigitAt[kDigits] = {21, 10, 0};
+constexpr int kLongKeys = 16384, kPartKeys = 8192, kSelectGroups = 256;      // more positions are shared by several workgroups, that many to each, where there are few heads
 constexpr int kMoveThreads = 256;
 constexpr int kMoveTokens = 64;
+
+// Between the launches of a selection by several workgroups.
+struct PartState {
+    unsigned always;        // tokens of the part that stay whatever they have
+    uint32_t kind;          // kSome, kAll or kNone of the others
+    uint32_t prefix;        // kSome: of the least key that stays, as far as it is known
+    unsigned room;          // how many stay of the keys that begin with it
+    unsigned before;        // tokens of the parts ahead that stay, as far as is known
+};
+
+enum { kSome = 0, kAll = 1, kNone = 2 };
 
 struct EvictParams {
     CacheView from, to;
@@ -25,6 +38,9 @@ struct EvictParams {
     int2* info;             // [sequence][head]: tokens that stay, the sequence's length
     int budget, first, last, most;
     int kept_keys;          // in LDS, a multiple of 4
+    int parts;              // workgroups of a sequence and key head that select
+    uint32_t* part_bins;    // [sequence][head][part][digit][kBins]
+    PartState* states;      // [sequence][head][part]
     int unit;               // places of a workgroup that moves
     int units;              // .. of a sequence
 };
@@ -37,161 +53,291 @@ __device__ __forceinline__ uint32_t key_of(float score)
     return score == score ? k : 1u;
 }
 
-__global__ void __launch_bounds__(kSelectThreads) kv_select_kernel(const EvictParams p)
-{
-    extern __shared__ __align__(16) unsigned char smem[];
-    uint32_t* kept_keys = reinterpret_cast<uint32_t*>(smem);                            // [p.kept_keys]
-    uint32_t* bins = kept_keys + p.kept_keys;                                           // [kBins]
-    uint32_t* shared = bins + kBins;                                                    // [2 kSelectWaves]
-    const CacheView& c = p.from;
-    const int seq = blockIdx.x / c.Hk, head = blockIdx.x % c.Hk;
-    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
-    const int held = c.max_pages << c.page_shift, given = c.lens[seq], len = given < 0 ? 0 : given, n = len < held ? len : held;
-    const int last = len > p.last ? len - p.last : 0;                                   // the last tokens' first position
-    int32_t* list = p.list + ((size_t)seq * c.Hk + head) * p.most;
+// What is common to the workgroups that select: positions begin .. end - 1 of a sequence and key head.
+struct Selector {
+    const EvictParams& p;
+    uint32_t *kept_keys, *bins, *shared;        // LDS: [p.kept_keys], [kBins], [2 kSelectWaves]
+    int seq, head, tid, lane, wave;
+    int len, n, last;                           // the sequence's length, positions there are, the last tokens' first one
+    int begin, end;
+
+    __device__ __forceinline__ Selector(const EvictParams& params, unsigned char* smem, int item) : p(params)
+    {
+        kept_keys = reinterpret_cast<uint32_t*>(smem);
+        bins = kept_keys + p.kept_keys;
+        shared = bins + kBins;
+        const CacheView& c = p.from;
+        seq = item / c.Hk; head = item % c.Hk;
+        tid = threadIdx.x; lane = tid & (kWave - 1); wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+        const int held = c.max_pages << c.page_shift, given = c.lens[seq];
+        len = given < 0 ? 0 : given;
+        n = len < held ? len : held;
+        last = len > p.last ? len - p.last : 0;
+        begin = 0;
+        end = n;
+    }
 
     // The four tokens from t on (a multiple of 4): their keys; ~0 for those that stay whatever they have, 0 for those that are none.
-    auto look = [&](int t) {
+    __device__ __forceinline__ u32x4_t look(int t) const
+    {
+        const CacheView& c = p.from;
         u32x4_t k = {0, 0, 0, 0};
-        if (t >= n) return k;
+        if (t >= end) return k;
         const int page = page_of(c, seq, t >> c.page_shift);
         if (page < 0) return k;
         const float4_t x = *reinterpret_cast<const float4_t*>(p.scores + ((((size_t)page * c.Hk + head) << c.page_shift) + (t & ((1 << c.page_shift) - 1))));
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const bool always = t + i < p.first || t + i >= last;
-            k[i] = t + i >= n ? 0u : always ? ~0u : key_of(x[i]);
+            k[i] = t + i >= end ? 0u : always ? ~0u : key_of(x[i]);
         }
         return k;
-    };
-    auto keys_at = [&](int t) {
-        if (t + 4 <= p.kept_keys) return *reinterpret_cast<const u32x4_t*>(kept_keys + t);
-        return look(t);
-    };
-    auto total = [&](unsigned x) {                                                      // over the workgroup
-        for (int o = 1; o < kWave; o <<= 1) x += (unsigned)__shfl_xor((int)x, o);
-        __syncthreads();
-        if (lane == 0) shared[wave] = x;
-        __syncthreads();
-        unsigned sum = 0;
-        for (int w = 0; w < kSelectWaves; ++w) sum += shared[w];
-        return sum;
-    };
-
-    // Those that stay anyhow, and those there are.
-    unsigned always = 0, there = 0;
-    for (int t = 4 * tid; t < n; t += 4 * kSelectThreads) {
-        const u32x4_t k = look(t);
-        if (t + 4 <= p.kept_keys) *reinterpret_cast<u32x4_t*>(kept_keys + t) = k;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { always += k[i] == ~0u; there += k[i] != 0u; }
     }
-    always = total(always);
-    there = total(there);
-    // The keys above `least` stay, and of those that are it the first `equal`.
-    uint32_t least = 0;
-    unsigned equal = 0;
-    if (there > (unsigned)p.budget) {
-        unsigned room = (unsigned)p.budget - always;
-        uint32_t prefix = 0, mask = 0;
-        if (room == 0) least = ~0u - 1;                                                 // (no candidate's key is that)
-        else {
-#pragma unroll
-            for (int digit = 0; digit < 3; ++digit) {
-                const int at = digit == 0 ? 21 : digit == 1 ? 10 : 0, width = digit == 2 ? 10 : 11;
-                __syncthreads();
-                for (int i = tid; i < kBins; i += kSelectThreads) bins[i] = 0;
-                __syncthreads();
-                for (int t = 4 * tid; t < n; t += 4 * kSelectThreads) {
-                    const u32x4_t k = keys_at(t);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (k[i] != 0u && k[i] != ~0u && (k[i] & mask) == prefix) atomicAdd(&bins[k[i] >> at & ((1u << width) - 1)], 1u);
-                }
-                __syncthreads();
-                // the bin in which the room ends, from the top: thread i has bins 2 i and 2 i + 1 from the top
-                const int b0 = kBins - 1 - 2 * tid;
-                const unsigned c0 = bins[b0], c1 = bins[b0 - 1];
-                unsigned upto = c0 + c1;
-                for (int o = 1; o < kWave; o <<= 1) {
-                    const unsigned x = (unsigned)__shfl_up((int)upto, o);
-                    upto += lane >= o ? x : 0u;
-                }
-                if (lane == kWave - 1) shared[wave] = upto;
-                __syncthreads();
-                for (int w = 0; w < wave; ++w) upto += shared[w];
-                const unsigned before = upto - c0 - c1;
-                if (before < room && room <= upto) {                                    // one thread
-                    const bool second = room > before + c0;
-                    shared[kSelectWaves] = (uint32_t)(second ? b0 - 1 : b0);
-                    shared[kSelectWaves + 1] = room - before - (second ? c0 : 0u);
-                }
-                __syncthreads();
-                prefix |= shared[kSelectWaves] << at;
-                room = shared[kSelectWaves + 1];
-                mask |= ((1u << width) - 1) << at;
-            }
-            least = prefix;
-            equal = room;
-        }
-    }
-    // Each wavefront's stretch: how many are above, and are, the least; then their places.
-    const int stretch = ceil_div(ceil_div(n, 4 * kWave), kSelectWaves) * 4 * kWave, begin = wave * stretch, end = begin + stretch < n ? begin + stretch : n;
-    unsigned above = 0, same = 0;
-    for (int t = begin + 4 * lane; t < end; t += 4 * kWave) {
-        const u32x4_t k = keys_at(t);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { above += k[i] > least; same += least != 0u && k[i] == least; }
-    }
-    for (int o = 1; o < kWave; o <<= 1) { above += (unsigned)__shfl_xor((int)above, o); same += (unsigned)__shfl_xor((int)same, o); }
-    __syncthreads();
-    if (lane == 0) { shared[wave] = above; shared[kSelectWaves + wave] = same; }
-    __syncthreads();
-    unsigned places = 0, sames = 0, all = 0;                                            // of the wavefronts before this one; of all
+    __device__ __forceinline__ u32x4_t keys_at(int t) const
     {
-        unsigned seen = 0;
+        if (t - begin + 4 <= p.kept_keys) return *reinterpret_cast<const u32x4_t*>(kept_keys + (t - begin));
+        return look(t);
+    }
+    __device__ __forceinline__ void clear_bins() const
+    {
+        for (int i = tid; i < kBins / 4; i += kSelectThreads) reinterpret_cast<u32x4_t*>(bins)[i] = u32x4_t{0, 0, 0, 0};
+    }
+    __device__ __forceinline__ static bool candidate(uint32_t k) { return k != 0u && k != ~0u; }
+
+    // Keys into LDS, the histogram of their first digit, and how many stay anyhow (to all threads).
+    __device__ __forceinline__ unsigned first_digit() const
+    {
+        clear_bins();
+        if (tid == 0) shared[0] = 0;
+        __syncthreads();
+        unsigned always = 0;
+        for (int t = begin + 4 * tid; t < end; t += 4 * kSelectThreads) {
+            const u32x4_t k = look(t);
+            if (t - begin + 4 <= p.kept_keys) *reinterpret_cast<u32x4_t*>(kept_keys + (t - begin)) = k;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                always += k[i] == ~0u;
+                if (candidate(k[i])) atomicAdd(&bins[k[i] >> kDigitAt[0]], 1u);
+            }
+        }
+        if (always) atomicAdd(&shared[0], always);
+        __syncthreads();
+        return shared[0];
+    }
+    // .. of a further one, among the keys that begin with `prefix`.
+    __device__ __forceinline__ void further_digit(int digit, uint32_t prefix) const
+    {
+        clear_bins();
+        __syncthreads();
+        const uint32_t mask = ~0u << kDigitAt[digit - 1];
+        for (int t = begin + 4 * tid; t < end; t += 4 * kSelectThreads) {
+            const u32x4_t k = keys_at(t);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (candidate(k[i]) && (k[i] & mask) == prefix) atomicAdd(&bins[k[i] >> kDigitAt[digit] & (kBins - 1)], 1u);
+        }
+        __syncthreads();
+    }
+
+    // The sum of x over the threads up to this one.
+    __device__ __forceinline__ unsigned upto(unsigned x) const
+    {
+        for (int o = 1; o < kWave; o <<= 1) {
+            const unsigned y = (unsigned)__shfl_up((int)x, o);
+            x += lane >= o ? y : 0u;
+        }
+        __syncthreads();
+        if (lane == kWave - 1) shared[wave] = x;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kSelectWaves - 1; ++w) x += w < wave ? shared[w] : 0u;
+        return x;
+    }
+    // Thread i has the numbers of keys in bins kBins - 1 - 2 i and the one below.  The bin in which the first `room` keys from the top end, and how many of its own are among them.
+    struct Found {
+        int bin;
+        unsigned room, all;     // all: in all bins
+    };
+    __device__ __forceinline__ Found find(unsigned c0, unsigned c1, unsigned room) const
+    {
+        const int b0 = kBins - 1 - 2 * tid;
+        const unsigned to = upto(c0 + c1), before = to - c0 - c1;
+        if (before < room && room <= to) {                                              // one thread
+            const bool second = room > before + c0;
+            shared[kSelectWaves] = (uint32_t)(second ? b0 - 1 : b0);
+            shared[kSelectWaves + 1] = room - before - (second ? c0 : 0u);
+        }
+        if (tid == kSelectThreads - 1) shared[kSelectWaves + 2] = to;
+        __syncthreads();
+        return Found{(int)shared[kSelectWaves], shared[kSelectWaves + 1], shared[kSelectWaves + 2]};
+    }
+
+    // Writes down the positions whose keys are above `least`, and of those that have it the first `equal` behind `sames` of others; the first as the `places`-th.
+    // The number of those that stay.
+    __device__ __forceinline__ unsigned write_down(uint32_t least, unsigned equal, unsigned places, unsigned sames) const
+    {
+        int32_t* list = p.list + ((size_t)seq * p.from.Hk + head) * p.most;
+        // each wavefront's stretch: how many are above, and are, the least; then their places
+        const int stretch = ceil_div(ceil_div(end - begin, 4 * kWave), kSelectWaves) * 4 * kWave, from = begin + wave * stretch, to = from + stretch < end ? from + stretch : end;
+        unsigned above = 0, same = 0;
+        for (int t = from + 4 * lane; t < to; t += 4 * kWave) {
+            const u32x4_t k = keys_at(t);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { above += k[i] > least; same += least != 0u && k[i] == least; }
+        }
+        for (int o = 1; o < kWave; o <<= 1) { above += (unsigned)__shfl_xor((int)above, o); same += (unsigned)__shfl_xor((int)same, o); }
+        __syncthreads();
+        if (lane == 0) { shared[wave] = above; shared[kSelectWaves + wave] = same; }
+        __syncthreads();
+        unsigned all = places, seen = sames;
+#pragma unroll
         for (int w = 0; w < kSelectWaves; ++w) {
             const unsigned a = shared[w], s = shared[kSelectWaves + w], taken = seen >= equal ? 0u : equal - seen < s ? equal - seen : s;
             if (w == wave) { places = all; sames = seen; }
             all += a + taken;
             seen += s;
         }
-    }
-    for (int t0 = begin; t0 < end; t0 += 4 * kWave) {
-        const int t = t0 + 4 * lane;
-        u32x4_t k = {0, 0, 0, 0};
-        if (t < end) k = keys_at(t);
-        unsigned s4 = 0;
+        for (int t0 = from; t0 < to; t0 += 4 * kWave) {
+            const int t = t0 + 4 * lane;
+            u32x4_t k = {0, 0, 0, 0};
+            if (t < to) k = keys_at(t);
+            unsigned s4 = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s4 += least != 0u && k[i] == least;
-        auto upto = [&](unsigned x) {                                                   // over the wavefront, up to the lane
+            for (int i = 0; i < 4; ++i) s4 += least != 0u && k[i] == least;
+            // (both counts of a wavefront's 256 tokens in one sum)
+            unsigned a4 = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) a4 += k[i] > least;
+            unsigned both = s4 << 16 | a4;
             for (int o = 1; o < kWave; o <<= 1) {
-                const unsigned y = (unsigned)__shfl_up((int)x, o);
-                x += lane >= o ? y : 0u;
+                const unsigned y = (unsigned)__shfl_up((int)both, o);
+                both += lane >= o ? y : 0u;
             }
-            return x;
-        };
-        const unsigned s_upto = upto(s4);
-        unsigned s_before = sames + s_upto - s4, stays = 0;
-        bool stay[4];
+            unsigned s_before = sames + (both >> 16) - s4, a_before = (both & 0xffffu) - a4;
+            auto taken_of = [&](unsigned upto_same) { return (upto_same < equal ? upto_same : equal) - (sames < equal ? sames : equal); };      // since the wavefront's first
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const bool is_same = least != 0u && k[i] == least;
-            stay[i] = k[i] > least || (is_same && s_before < equal);
-            s_before += is_same;
-            stays += stay[i];
+            for (int i = 0; i < 4; ++i) {
+                const bool is_above = k[i] > least, is_same = least != 0u && k[i] == least;
+                const unsigned at = places + a_before + taken_of(s_before);
+                if ((is_above || (is_same && s_before < equal)) && at < (unsigned)p.most) list[at] = t + i;
+                a_before += is_above;
+                s_before += is_same;
+            }
+            const unsigned whole = (unsigned)__builtin_amdgcn_readlane((int)both, kWave - 1);
+            places += (whole & 0xffffu) + taken_of(sames + (whole >> 16));
+            sames += whole >> 16;
         }
-        const unsigned p_upto = upto(stays);
-        unsigned at = places + p_upto - stays;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (stay[i] && at < (unsigned)p.most) list[at] = t + i;
-            at += stay[i];
-        }
-        places += (unsigned)__builtin_amdgcn_readlane((int)p_upto, kWave - 1);
-        sames += (unsigned)__builtin_amdgcn_readlane((int)s_upto, kWave - 1);
+        return all;
     }
-    if (tid == 0) p.info[(size_t)seq * c.Hk + head] = int2{(int)all, len};
+};
+
+// A sequence and key head by one workgroup.
+__global__ void __launch_bounds__(kSelectThreads) kv_select_kernel(const EvictParams p)
+{
+    extern __shared__ __align__(16) unsigned char smem[];
+    const Selector s(p, smem, blockIdx.x);
+    const unsigned always = s.first_digit();
+    unsigned room = (unsigned)p.budget - always;
+    const int b0 = kBins - 1 - 2 * s.tid;
+    Selector::Found f = s.find(s.bins[b0], s.bins[b0 - 1], room);
+    uint32_t least = 0;                                                                 // all stay
+    unsigned equal = 0;
+    if (always + f.all > (unsigned)p.budget) {
+        least = ~0u - 1;                                                                // (no candidate's key is that: none stays)
+        if (room != 0) {
+            least = (uint32_t)f.bin << kDigitAt[0];
+            equal = f.room;
+#pragma unroll
+            for (int digit = 1; digit < kDigits; ++digit) {
+                s.further_digit(digit, least);
+                f = s.find(s.bins[b0], s.bins[b0 - 1], equal);
+                least |= (uint32_t)f.bin << kDigitAt[digit];
+                equal = f.room;
+            }
+        }
+    }
+    const unsigned all = s.write_down(least, equal, 0, 0);
+    if (s.tid == 0) p.info[blockIdx.x] = int2{(int)all, s.len};
+}
+
+// .. by several, each with its part of the positions, in four launches: the histogram of the first digit, of the second, of the third, and what stays.  Every workgroup adds up
+// the histograms of the digit before, and of those of the parts ahead of its own what is above the bin that was found.
+template <int PASS>
+__global__ void __launch_bounds__(kSelectThreads) kv_select_part_kernel(const EvictParams p)
+{
+    extern __shared__ __align__(16) unsigned char smem[];
+    const int item = blockIdx.x / p.parts, part = blockIdx.x % p.parts;
+    Selector s(p, smem, item);
+    const int size = ceil_div(ceil_div(s.n, 4), p.parts) * 4;
+    s.begin = part * size < s.n ? part * size : s.n;
+    s.end = s.begin + size < s.n ? s.begin + size : s.n;
+    uint32_t* bins_of = p.part_bins + (size_t)item * p.parts * kDigits * kBins;         // [part][digit][kBins]
+    PartState* states = p.states + (size_t)item * p.parts;
+    if constexpr (PASS == 0) {
+        const unsigned always = s.first_digit();
+        for (int i = s.tid; i < kBins; i += kSelectThreads) bins_of[(size_t)part * kDigits * kBins + i] = s.bins[i];
+        if (s.tid == 0) states[part] = PartState{always, kSome, 0, 0, 0};
+        return;
+    }
+    // of the item: what came out of the digits before, the same in all parts
+    unsigned always = 0, always_before = 0;
+    for (int i = 0; i < p.parts; ++i) {
+        always += states[i].always;
+        always_before += i < part ? states[i].always : 0u;
+    }
+    const unsigned room = PASS == 1 ? (unsigned)p.budget - always : states[part].room;
+    uint32_t least = PASS == 1 ? 0u : states[part].prefix;
+    unsigned before = PASS == 1 ? always_before : states[part].before;                  // what stays ahead of this part, of what is known
+    const int b0 = kBins - 1 - 2 * s.tid;
+    unsigned c0 = 0, c1 = 0, ahead0 = 0, ahead1 = 0;
+#pragma unroll 4
+    for (int i = 0; i < p.parts; ++i) {
+        const u32x2_t x = *reinterpret_cast<const u32x2_t*>(bins_of + ((size_t)i * kDigits + PASS - 1) * kBins + b0 - 1);
+        c0 += x[1];
+        c1 += x[0];
+        ahead0 += i < part ? x[1] : 0u;
+        ahead1 += i < part ? x[0] : 0u;
+    }
+    const Selector::Found f = s.find(c0, c1, room);
+    const uint32_t kind = PASS != 1 ? states[part].kind : always + f.all <= (unsigned)p.budget ? kAll : room == 0u ? kNone : kSome;
+    const bool all_stay = kind == kAll, none = kind == kNone;
+    unsigned equal = 0, sames = 0;
+    {
+        const unsigned mine = all_stay ? (PASS == 1 ? ahead0 + ahead1 : 0u) : none ? 0u : (b0 > f.bin ? ahead0 : 0u) + (b0 - 1 > f.bin ? ahead1 : 0u);
+        const unsigned same = all_stay || none ? 0u : (b0 == f.bin ? ahead0 : 0u) + (b0 - 1 == f.bin ? ahead1 : 0u);
+        const unsigned sum = s.upto(mine);
+        __syncthreads();
+        if (s.tid == kSelectThreads - 1) s.shared[kSelectWaves] = sum;
+        if (s.tid == 0) s.shared[kSelectWaves + 1] = 0;
+        __syncthreads();
+        if (same) atomicAdd(&s.shared[kSelectWaves + 1], same);
+        __syncthreads();
+        before += s.shared[kSelectWaves];
+        sames = s.shared[kSelectWaves + 1];
+    }
+    if (all_stay) least = 0;
+    else if (none) least = ~0u - 1;
+    else {
+        least |= (uint32_t)f.bin << kDigitAt[PASS - 1];
+        equal = f.room;
+    }
+    if constexpr (PASS < kDigits) {
+        if (!all_stay && !none) {
+            s.further_digit(PASS, least);
+            for (int i = s.tid; i < kBins; i += kSelectThreads) bins_of[((size_t)part * kDigits + PASS) * kBins + i] = s.bins[i];
+        }
+        __syncthreads();
+        // (every part reads its own state only, but for `always`, which stays)
+        if (s.tid == 0) {
+            states[part].kind = kind;
+            states[part].prefix = least;
+            states[part].room = equal;
+            states[part].before = before;
+        }
+    } else {
+        const unsigned all = s.write_down(least, equal, before + (sames < equal ? sames : equal), sames);
+        if (part == p.parts - 1 && s.tid == 0) p.info[item] = int2{(int)all, s.len};
+    }
 }
 
 // 8 bits: a code in another scale.
@@ -373,8 +519,8 @@ namespace {
 constexpr size_t kFixedArea = (size_t)kCounterAreaWords * sizeof(uint32_t) + kPairAreaBytes;       // that other calls keep their counters in
 
 struct EvictPlan {
-    int most, unit, units, kept_keys;
-    size_t info, bytes;
+    int most, unit, units, kept_keys, parts;
+    size_t info, part_bins, states, bytes;
 };
 
 int evict_plan(const codegemm_kv_cache* from, const codegemm_evict_desc* d, EvictPlan* p)
@@ -394,8 +540,14 @@ int evict_plan(const codegemm_kv_cache* from, const codegemm_evict_desc* d, Evic
     const long long room = 0xffffffffll / kMoveThreads / items;
     if (p->units > room) p->units = (int)room;
     p->kept_keys = known < kKeptKeys ? ceil_div(known, 4) * 4 : kKeptKeys;
+    // Long sequences of few heads: several workgroups, which takes four launches.
+    const long long parts = known <= kLongKeys ? 1 : kSelectGroups / items < ceil_div(known, kPartKeys) ? kSelectGroups / items : ceil_div(known, kPartKeys);
+    p->parts = parts < 1 ? 1 : (int)parts;
     p->info = kFixedArea + ((size_t)items * p->most * sizeof(int32_t) + 255) / 256 * 256;
-    p->bytes = p->info + (size_t)items * sizeof(int2);
+    p->part_bins = p->info + ((size_t)items * sizeof(int2) + 255) / 256 * 256;
+    const size_t many = p->parts > 1 ? (size_t)items * p->parts : 0;
+    p->states = p->part_bins + many * kDigits * kBins * sizeof(uint32_t);
+    p->bytes = many ? p->states + many * sizeof(PartState) : p->info + (size_t)items * sizeof(int2);
     return CODEGEMM_OK;
 }
 
@@ -442,11 +594,25 @@ extern "C" int codegemm_kv_evict(const codegemm_kv_cache* from, const codegemm_k
     p.info = reinterpret_cast<int2*>(static_cast<unsigned char*>(workspace) + plan.info);
     p.budget = desc->budget; p.first = desc->keep_first; p.last = desc->keep_last;
     p.most = plan.most; p.kept_keys = plan.kept_keys; p.unit = plan.unit; p.units = plan.units;
+    p.parts = plan.parts;
+    p.part_bins = reinterpret_cast<uint32_t*>(static_cast<unsigned char*>(workspace) + plan.part_bins);
+    p.states = reinterpret_cast<PartState*>(static_cast<unsigned char*>(workspace) + plan.states);
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const size_t lds = ((size_t)plan.kept_keys + kBins + 2 * kSelectWaves) * sizeof(uint32_t);
-    st = set_max_lds(reinterpret_cast<const void*>(kv_select_kernel), lds);
-    if (st) return st;
-    hipLaunchKernelGGL(kv_select_kernel, dim3((unsigned)(p.from.seqs * p.from.Hk)), dim3(kSelectThreads), lds, s, p);
+    const unsigned items = (unsigned)(p.from.seqs * p.from.Hk);
+    if (plan.parts > 1) {
+        p.kept_keys = 0;
+        const size_t lds = ((size_t)kBins + 2 * kSelectWaves) * sizeof(uint32_t);
+        const dim3 grid(items * (unsigned)plan.parts), threads(kSelectThreads);
+        hipLaunchKernelGGL(kv_select_part_kernel<0>, grid, threads, lds, s, p);
+        hipLaunchKernelGGL(kv_select_part_kernel<1>, grid, threads, lds, s, p);
+        hipLaunchKernelGGL(kv_select_part_kernel<2>, grid, threads, lds, s, p);
+        hipLaunchKernelGGL(kv_select_part_kernel<3>, grid, threads, lds, s, p);
+    } else {
+        const size_t lds = ((size_t)plan.kept_keys + kBins + 2 * kSelectWaves) * sizeof(uint32_t);
+        st = set_max_lds(reinterpret_cast<const void*>(kv_select_kernel), lds);
+        if (st) return st;
+        hipLaunchKernelGGL(kv_select_kernel, dim3(items), dim3(kSelectThreads), lds, s, p);
+    }
     if (from->dtype == CODEGEMM_KV_FP16) launch_move<CODEGEMM_KV_FP16>(p, s);
     else if (from->dtype == CODEGEMM_KV_INT8) launch_move<CODEGEMM_KV_INT8>(p, s);
     else if (from->dtype == CODEGEMM_KV_INT4) launch_move<CODEGEMM_KV_INT4>(p, s);
