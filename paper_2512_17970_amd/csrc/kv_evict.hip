@@ -15,7 +15,13 @@ constexpr int kBins = 2048, kDigits = 3;    // two for each thread
 constexpr int kDigitAt[kDigits] = {21, 10, 0};
 constexpr int kLongKeys = 16384, kPartKeys = 8192, kSelectGroups = 256;      // more positions are shared by several workgroups, that many to each, where there are few heads
 constexpr int kMoveThreads = 256;
-constexpr int kMoveTokens = 64;
+#ifndef MANY
+#define MANY 4096
+#endif
+#ifndef MOVE2
+#define MOVE2 256
+#endif
+constexpr int kMoveTokens = 64, kManyUnits = MANY;
 
 // Between the launches of a selection by several workgroups.
 struct PartState {
@@ -41,6 +47,7 @@ struct EvictParams {
     int parts;              // workgroups of a sequence and key head that select
     uint32_t* part_bins;    // [sequence][head][part][digit][kBins]
     PartState* states;      // [sequence][head][part]
+    uint32_t by_pieces, by_runs;        // 2^32 over the pieces of a key, rounded up, and over its runs: i / n is the upper half of the product (0: n is 1)
     int unit;               // places of a workgroup that moves
     int units;              // .. of a sequence
 };
@@ -354,18 +361,27 @@ __device__ __forceinline__ uint32_t again(uint32_t code, float ratio)
 // The four bits of token j of a word's eight.
 __device__ __forceinline__ constexpr int bit_of(int j) { return 4 * (j >> 1) + 16 * (j & 1); }
 
+// i / n for i < 2^16 and n < 2^8, by 2^32 / n rounded up.
+__device__ __forceinline__ int over(int i, uint32_t by) { return by != 0 ? (int)__umulhi((uint32_t)i, by) : i; }
+
 // Units of places of a sequence and key head, keys or values.
 template <int TYPE>
 __global__ void __launch_bounds__(kMoveThreads) kv_move_kernel(const EvictParams p)
 {
     constexpr bool FOUR = TYPE == CODEGEMM_KV_INT4, SCALED = TYPE == CODEGEMM_KV_INT8 || TYPE == CODEGEMM_KV_FP8;
     __shared__ int2 source[kMoveThreads];                       // [token]: page and slot
+    __shared__ u32x2_t value_row[kMoveThreads];                 // [token]: where its 16 tokens' values begin in the pool, in bytes, and above bit 60 which of them it is
+    __shared__ int page_to[kMoveThreads / 16];                  // [16 tokens]: the page that they go to, or -1
     __shared__ float old[kMoveThreads];                         // [token]: its scale so far
     __shared__ uint32_t largest[kMoveThreads];                  // [block]: the bits of its scale
     const CacheView &a = p.from, &b = p.to;
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave), D = a.D;
     const int head = blockIdx.x % a.Hk, item = blockIdx.x / a.Hk, seq = item / p.units;
     const bool values = blockIdx.y != 0;
+    // (the first unit's positions are asked for beside the counts, which say what of them there is)
+    const int32_t* list = p.list + ((size_t)seq * a.Hk + head) * p.most;
+    auto listed = [&](int unit) { const int i = unit * p.unit + tid; return tid < p.unit && i < p.most ? list[i] : 0; };
+    int mine = listed(item % p.units);
     const int2 info = p.info[(size_t)seq * a.Hk + head];
     if (item % p.units == 0 && head == 0 && !values && tid == 0) {
         p.to_lens[seq] = info.x;
@@ -376,11 +392,16 @@ __global__ void __launch_bounds__(kMoveThreads) kv_move_kernel(const EvictParams
         const int first = unit * p.unit, count = info.x - first < p.unit ? info.x - first : p.unit;
         if (count <= 0) return;
         __syncthreads();
-        if (tid < p.unit) largest[tid] = 0;
-        __syncthreads();
+        if (SCALED) {
+            if (tid < p.unit) largest[tid] = 0;
+            __syncthreads();
+        }
+        if (tid < kMoveThreads / 16) page_to[tid] = 16 * tid < count ? page_of(b, seq, (first + 16 * tid) >> b.page_shift) : -1;
         if (tid < count) {
-            const int t = p.list[((size_t)seq * a.Hk + head) * p.most + first + tid], page = page_of(a, seq, t >> a.page_shift), slot = t & mask;       // (there is a page)
+            const int t = mine, page = page_of(a, seq, t >> a.page_shift), slot = t & mask;       // (there is a page)
             source[tid] = int2{page, slot};
+            const unsigned long long row = page_at(a, page, head) + (size_t)(slot & ~15) * D, at = FOUR ? row / 2 : TYPE == CODEGEMM_KV_FP16 ? row * 2 : row;
+            value_row[tid] = u32x2_t{(uint32_t)at, (uint32_t)(at >> 32) | (uint32_t)(slot & 15) << 28};
             if constexpr (SCALED) {
                 const float s = (values ? a.v_scales : a.k_scales)[scales_at(a, page, head) + (slot >> a.block_shift)];
                 old[tid] = s;
@@ -392,13 +413,14 @@ __global__ void __launch_bounds__(kMoveThreads) kv_move_kernel(const EvictParams
                     p.to_scores[(((size_t)to * b.Hk + head) << b.page_shift) + ((first + tid) & mask)] = p.scores[(((size_t)page * a.Hk + head) << a.page_shift) + slot];
             }
         }
+        mine = listed(unit + p.units);
         __syncthreads();
         auto ratio_of = [&](int token) {                        // 1: codes stay
             const float s = old[token], now = __builtin_bit_cast(float, largest[token >> a.block_shift]);
             return s == now ? 1.0f : s > 0.0f && s < now ? s / now : 0.0f;
         };
         if constexpr (SCALED) {
-            const int block = tid << b.block_shift, to = block < count ? page_of(b, seq, (first + block) >> b.page_shift) : -1;
+            const int block = tid << b.block_shift, to = block < count ? page_to[block >> 4] : -1;
             if (to >= 0) (values ? b.v_scales : b.k_scales)[scales_at(b, to, head) + (((first + block) & mask) >> b.block_shift)] = __builtin_bit_cast(float, largest[tid]);
         }
         if (!values) {
@@ -408,13 +430,13 @@ __global__ void __launch_bounds__(kMoveThreads) kv_move_kernel(const EvictParams
                 u32x4_t x[AT_ONCE];
 #pragma unroll
                 for (int k = 0; k < AT_ONCE; ++k) {
-                    const int i = i0 + k * kMoveThreads, token = i / pieces;
-                    if (i < count * pieces) x[k] = reinterpret_cast<const u32x4_t*>(a.k)[((((size_t)source[token].x * a.Hk + head) << a.page_shift) + source[token].y) * pieces + i % pieces];
+                    const int i = i0 + k * kMoveThreads, token = over(i, p.by_pieces);
+                    if (i < count * pieces) x[k] = reinterpret_cast<const u32x4_t*>(a.k)[((((size_t)source[token].x * a.Hk + head) << a.page_shift) + source[token].y) * pieces + (i - token * pieces)];
                 }
 #pragma unroll
                 for (int k = 0; k < AT_ONCE; ++k) {
-                    const int i = i0 + k * kMoveThreads, token = i / pieces, t = first + token;
-                    const int to = i < count * pieces ? page_of(b, seq, t >> b.page_shift) : -1;
+                    const int i = i0 + k * kMoveThreads, token = over(i, p.by_pieces), t = first + token;
+                    const int to = i < count * pieces ? page_to[token >> 4] : -1;
                     if (to < 0) continue;
                     if constexpr (SCALED) {
                         const float ratio = ratio_of(token);
@@ -428,12 +450,12 @@ __global__ void __launch_bounds__(kMoveThreads) kv_move_kernel(const EvictParams
                             }
                         }
                     }
-                    reinterpret_cast<u32x4_t*>(b.k)[((((size_t)to * b.Hk + head) << b.page_shift) + (t & mask)) * pieces + i % pieces] = x[k];
+                    reinterpret_cast<u32x4_t*>(b.k)[((((size_t)to * b.Hk + head) << b.page_shift) + (t & mask)) * pieces + (i - token * pieces)] = x[k];
                 }
             }
             if constexpr (FOUR) {
                 for (int i = tid; i < count * a.runs; i += kMoveThreads) {
-                    const int token = i / a.runs, run = i % a.runs, t = first + token, to = page_of(b, seq, t >> b.page_shift);
+                    const int token = over(i, p.by_runs), run = i - token * a.runs, t = first + token, to = page_to[token >> 4];
                     if (to >= 0)
                         reinterpret_cast<uint32_t*>(b.k_scales)[runs_at(b, to, head, t & mask) + run] =
                             reinterpret_cast<const uint32_t*>(a.k_scales)[runs_at(a, source[token].x, head, source[token].y) + run];
@@ -443,67 +465,99 @@ __global__ void __launch_bounds__(kMoveThreads) kv_move_kernel(const EvictParams
         }
         for (int group = wave; 16 * group < count; group += kMoveThreads / kWave) {
             const int t = first + 16 * group, here = count - 16 * group < 16 ? count - 16 * group : 16;
-            const int to = __builtin_amdgcn_readfirstlane(page_of(b, seq, t >> b.page_shift));
+            const int to = __builtin_amdgcn_readfirstlane(page_to[group]);
             if (to < 0) continue;
-            int2 from[16];                                      // of the group's tokens; the same for all lanes
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                const int2 s = source[16 * group + (j < here ? j : 0)];
-                from[j] = int2{__builtin_amdgcn_readfirstlane(s.x), __builtin_amdgcn_readfirstlane(s.y)};
-            }
+            // Lane j has the group's j-th token: where its row begins, and which of the row's 16 it is.  Tokens that follow each other in a row share its load: `heads` are those
+            // that begin one.
+            const u32x2_t row_of = value_row[16 * group + ((lane & 15) < here ? lane & 15 : 0)];
+            const uint32_t before_lo = (uint32_t)__shfl_up((int)row_of[0], 1), before_hi = (uint32_t)__shfl_up((int)row_of[1], 1);
+            const uint32_t heads = (uint32_t)__ballot(lane < here && (lane == 0 || before_lo != row_of[0] || (before_hi ^ row_of[1]) << 4 != 0));
+            float ratio = 1.0f;                                 // of the lane's token
+            if constexpr (SCALED) ratio = ratio_of(16 * group + ((lane & 15) < here ? lane & 15 : 0));
+            // .. and how a code goes from its row to its place: bits 0 to 4 where it is in its word, 8 to 12 where it comes, 16 on which word (4 bits: its own, its place's; 8: two bits each)
+            const uint32_t in_row = row_of[1] >> 28, place = lane & 15;
+            const uint32_t how_of = FOUR ? (uint32_t)bit_of(in_row & 7) | (uint32_t)bit_of(place & 7) << 8 | in_row >> 3 << 16 | place >> 3 << 17
+                                         : 8 * (in_row & 3) | 8 * (place & 3) << 8 | in_row >> 2 << 16 | place >> 2 << 18;
             const size_t at = page_at(b, to, head) + (size_t)(t & mask) * D;
-            auto row = [&](int j) { return page_at(a, from[j].x, head) + (size_t)(from[j].y & ~15) * D; };
-            for (int d = lane; d < D; d += kWave) {
-                if constexpr (FOUR) {
-                    uint32_t x[16], w[2] = {0, 0}, taken[2] = {0, 0};
+            constexpr int WORDS = TYPE == CODEGEMM_KV_FP16 ? 8 : 4, ROWS = 32 / WORDS;            // of a lane's part of a row; rows that are asked for at once
+            for (int d = lane; d < (FOUR ? D / 2 : D); d += kWave) {                               // (4 bits: two dimensions a lane)
+                uint32_t w[WORDS] = {0};
+                if constexpr (TYPE == CODEGEMM_KV_FP16) {       // a load for each token: of one row, they are of the same lines
+                    uint32_t x[16];
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) x[j] = reinterpret_cast<const uint32_t*>(a.v + row(j) / 2)[2 * d + (from[j].y >> 3 & 1)];
-#pragma unroll
-                    for (int j = 0; j < 16; ++j)
-                        if (j < here) {
-                            w[j >> 3] |= (x[j] >> bit_of(from[j].y & 7) & 15u) << bit_of(j & 7);
-                            taken[j >> 3] |= 15u << bit_of(j & 7);
-                        }
-                    u32x2_t* dst = reinterpret_cast<u32x2_t*>(b.v + at / 2) + d;
-                    if (here < 16) {
-                        const u32x2_t was = *dst;
-                        w[0] |= was[0] & ~taken[0];
-                        w[1] |= was[1] & ~taken[1];
+                    for (int j = 0; j < 16; ++j) {
+                        const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)row_of[0], j), hi = (uint32_t)__builtin_amdgcn_readlane((int)row_of[1], j);
+                        x[j] = reinterpret_cast<const uint16_t*>(a.v + ((unsigned long long)(hi & 0x0fffffffu) << 32 | lo) + 2 * (hi >> 28))[(uint32_t)d * 16];
                     }
-                    *dst = u32x2_t{w[0], w[1]};
-                } else if constexpr (SCALED) {
-                    uint32_t x[16];
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) x[j] = a.v[row(j) + (size_t)d * 16 + (from[j].y & 15)];
-                    u32x4_t* dst = reinterpret_cast<u32x4_t*>(b.v + at) + d;
-                    u32x4_t w = {0, 0, 0, 0};
-                    if (here < 16) w = *dst;
+                    for (int j = 0; j < 16; ++j) w[j >> 1] |= j < here ? x[j] << (16 * (j & 1)) : 0u;
+                }
+                for (uint32_t left = TYPE == CODEGEMM_KV_FP16 ? 0u : heads; left != 0;) {
+                    u32x4_t x[ROWS][WORDS / 4];
+                    int from[ROWS + 1];
 #pragma unroll
-                    for (int j = 0; j < 16; ++j)
-                        if (j < here) {
-                            const float ratio = ratio_of(16 * group + j);
-                            const uint32_t code = ratio == 1.0f ? x[j] : again<TYPE>(x[j], ratio);
-                            w[j >> 2] = (w[j >> 2] & ~(255u << (8 * (j & 3)))) | code << (8 * (j & 3));
+                    for (int k = 0; k < ROWS; ++k) {
+                        from[k] = left != 0 ? __builtin_ctz(left) : here;
+                        if (left != 0) {
+                            const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)row_of[0], from[k]), hi = (uint32_t)__builtin_amdgcn_readlane((int)row_of[1], from[k]);
+                            const u32x4_t* row = reinterpret_cast<const u32x4_t*>(a.v + ((unsigned long long)(hi & 0x0fffffffu) << 32 | lo));
+#pragma unroll
+                            for (int i = 0; i < WORDS / 4; ++i) x[k][i] = row[d * (WORDS / 4) + i];
                         }
-                    *dst = w;
-                } else {
-                    uint32_t x[16];
+                        left &= left - 1;
+                    }
+                    from[ROWS] = left != 0 ? __builtin_ctz(left) : here;
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) x[j] = reinterpret_cast<const uint16_t*>(a.v)[row(j) + (size_t)d * 16 + (from[j].y & 15)];
-                    u32x4_t* dst = reinterpret_cast<u32x4_t*>(reinterpret_cast<uint16_t*>(b.v) + at) + 2 * d;
-                    u32x4_t w[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
-                    if (here < 16) { w[0] = dst[0]; w[1] = dst[1]; }
+                    for (int k = 0; k < ROWS; ++k)
+                        for (int j = from[k]; j < from[k + 1]; ++j) {
+                            const uint32_t how = (uint32_t)__builtin_amdgcn_readlane((int)how_of, j), to_bit = how >> 8 & 31u;
+                            // (which word a code is in and comes into by conditions and masks that are the same for all lanes: chosen by branches, words
+                            // are copied about)
+                            const u32x4_t y = x[k][0];
+                            auto mask_of = [&](uint32_t is) { return is != 0 ? ~0u : 0u; };
+                            if constexpr (FOUR) {
+                                const bool upper = how & 0x10000u;
+                                const uint32_t second = mask_of(how & 0x20000u), c0 = __builtin_amdgcn_ubfe(upper ? y[1] : y[0], how, 4) << to_bit, c1 = __builtin_amdgcn_ubfe(upper ? y[3] : y[2], how, 4) << to_bit;
+                                w[0] |= c0 & ~second;
+                                w[1] |= c0 & second;
+                                w[2] |= c1 & ~second;
+                                w[3] |= c1 & second;
+                            } else if constexpr (SCALED) {
+                                const bool odd = how & 0x10000u, upper = how & 0x20000u;
+                                uint32_t code = upper ? (odd ? y[3] : y[2]) : (odd ? y[1] : y[0]);
+                                code = __builtin_amdgcn_ubfe(code, how, 8);
+                                const float by = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, ratio), j));
+                                if (by != 1.0f) code = again<TYPE>(code, by);
+                                code <<= to_bit;
+                                const uint32_t to_word = how >> 18 & 3u;
 #pragma unroll
-                    for (int j = 0; j < 16; ++j)
-                        if (j < here) w[j >> 3][j / 2 & 3] = j & 1 ? (w[j >> 3][j / 2 & 3] & 0xffffu) | x[j] << 16 : (w[j >> 3][j / 2 & 3] & 0xffff0000u) | x[j];
-                    dst[0] = w[0];
-                    dst[1] = w[1];
+                                for (int i = 0; i < 4; ++i) w[i] |= code & mask_of(to_word == (uint32_t)i ? 1u : 0u);
+                            }
+                        }
+                }
+                u32x4_t* dst = reinterpret_cast<u32x4_t*>(b.v + (FOUR ? at / 2 : at * (WORDS / 4))) + (size_t)d * (WORDS / 4);
+#pragma unroll
+                for (int i = 0; i < WORDS / 4; ++i) {
+                    u32x4_t y = {w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]};
+                    if (here < 16) {                            // the group's other places stay as they are
+                        const u32x4_t was = dst[i];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            constexpr int PER = FOUR ? 8 : TYPE == CODEGEMM_KV_FP16 ? 2 : 4;      // tokens of a word
+                            const int first_of = FOUR ? 8 * (e & 1) : PER * (4 * i + e);
+                            uint32_t taken = 0;
+#pragma unroll
+                            for (int q = 0; q < PER; ++q) taken |= first_of + q < here ? (FOUR ? 15u << bit_of(q) : PER == 2 ? 0xffffu << (16 * q) : 255u << (8 * q)) : 0u;
+                            y[e] |= was[e] & ~taken;
+                        }
+                    }
+                    dst[i] = y;
                 }
             }
         }
         if constexpr (FOUR) {
             for (int i = tid; i < count * a.runs; i += kMoveThreads) {
-                const int token = i / a.runs, run = i % a.runs, t = first + token, to = page_of(b, seq, t >> b.page_shift), slot = source[token].y;
+                const int token = over(i, p.by_runs), run = i - token * a.runs, t = first + token, to = page_to[token >> 4], slot = source[token].y;
                 if (to < 0) continue;
                 const uint16_t* src = reinterpret_cast<const uint16_t*>(a.v_scales) + 2 * runs_at(a, source[token].x, head, slot & ~15) + 32 * run + (slot & 15);
                 uint16_t* dst = reinterpret_cast<uint16_t*>(b.v_scales) + 2 * runs_at(b, to, head, t & mask & ~15) + 32 * run + (t & 15);
@@ -533,8 +587,9 @@ int evict_plan(const codegemm_kv_cache* from, const codegemm_evict_desc* d, Evic
     const int held = from->max_pages * from->page_size, known = d->max_kv < held ? d->max_kv : held;
     p->most = d->budget < held ? d->budget : held;
     const bool scaled = from->dtype == CODEGEMM_KV_INT8 || from->dtype == CODEGEMM_KV_FP8;
-    p->unit = scaled && from->scale_block > kMoveTokens ? from->scale_block : kMoveTokens;
     const int kept = p->most < known ? p->most : known;
+    const int tokens = 2 * items * ceil_div(kept, kMoveTokens) > kManyUnits ? MOVE2 : kMoveTokens;
+    p->unit = scaled && from->scale_block > tokens ? from->scale_block : tokens;
     p->units = ceil_div(kept, p->unit);
     // (whatever the host knows: fewer workgroups have more units each)
     const long long room = 0xffffffffll / kMoveThreads / items;
@@ -594,6 +649,10 @@ extern "C" int codegemm_kv_evict(const codegemm_kv_cache* from, const codegemm_k
     p.info = reinterpret_cast<int2*>(static_cast<unsigned char*>(workspace) + plan.info);
     p.budget = desc->budget; p.first = desc->keep_first; p.last = desc->keep_last;
     p.most = plan.most; p.kept_keys = plan.kept_keys; p.unit = plan.unit; p.units = plan.units;
+    const int pieces = from->head_dim / (from->dtype == CODEGEMM_KV_FP16 ? 8 : from->dtype == CODEGEMM_KV_INT4 ? 32 : 16);
+    auto inverse = [](int n) { return n > 1 ? (uint32_t)(((1ull << 32) + (unsigned)n - 1) / (unsigned)n) : 0u; };
+    p.by_pieces = inverse(pieces);
+    p.by_runs = inverse(p.from.runs);
     p.parts = plan.parts;
     p.part_bins = reinterpret_cast<uint32_t*>(static_cast<unsigned char*>(workspace) + plan.part_bins);
     p.states = reinterpret_cast<PartState*>(static_cast<unsigned char*>(workspace) + plan.states);
