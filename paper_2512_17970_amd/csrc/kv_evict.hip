@@ -13,7 +13,7 @@ constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / kWave;
 constexpr int kKeptKeys = 32768;            // 128 KB, at most
 constexpr int kBins = 2048, kDigits = 3;    // two for each thread
 constexpr int kDigitAt[kDigits] = {21, 10, 0};
-constexpr int kLongKeys = 16384, kPartKeys = 8192, kSelectGroups = 256;      // more positions are shared by several workgroups, that many to each, where there are few heads
+constexpr int kLongKeys = 16384, kPartKeys = 8192, kPartKept = 12288, kSelectGroups = 256;      // more positions are shared by several workgroups, that many to each, where there are few heads
 constexpr int kMoveThreads = 256;
 #ifndef MANY
 #define MANY 4096
@@ -88,15 +88,13 @@ struct Selector {
     __device__ __forceinline__ u32x4_t look(int t) const
     {
         const CacheView& c = p.from;
-        u32x4_t k = {0, 0, 0, 0};
-        if (t >= end) return k;
-        const int page = page_of(c, seq, t >> c.page_shift);
-        if (page < 0) return k;
-        const float4_t x = *reinterpret_cast<const float4_t*>(p.scores + ((((size_t)page * c.Hk + head) << c.page_shift) + (t & ((1 << c.page_shift) - 1))));
+        const int at = t < end ? t : begin, page = page_of(c, seq, at >> c.page_shift);         // (no branches: loads of several places are under way together)
+        const float4_t x = *reinterpret_cast<const float4_t*>(p.scores + ((((size_t)(page < 0 ? 0 : page) * c.Hk + head) << c.page_shift) + (at & ((1 << c.page_shift) - 1))));
+        u32x4_t k;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const bool always = t + i < p.first || t + i >= last;
-            k[i] = t + i >= end ? 0u : always ? ~0u : key_of(x[i]);
+            k[i] = page < 0 || t + i >= end ? 0u : always ? ~0u : key_of(x[i]);
         }
         return k;
     }
@@ -111,6 +109,21 @@ struct Selector {
     }
     __device__ __forceinline__ static bool candidate(uint32_t k) { return k != 0u && k != ~0u; }
 
+    // take(t, get(t)) for the thread's places t, several of which are under way at once.
+    template <class Get, class Take>
+    __device__ __forceinline__ void each(Get get, Take take) const
+    {
+        constexpr int AT_ONCE = 4;
+        for (int t0 = begin + 4 * tid; t0 < end; t0 += 4 * AT_ONCE * kSelectThreads) {
+            u32x4_t k[AT_ONCE];
+#pragma unroll
+            for (int i = 0; i < AT_ONCE; ++i) k[i] = t0 + 4 * i * kSelectThreads < end ? get(t0 + 4 * i * kSelectThreads) : u32x4_t{0, 0, 0, 0};
+#pragma unroll
+            for (int i = 0; i < AT_ONCE; ++i)
+                if (t0 + 4 * i * kSelectThreads < end) take(t0 + 4 * i * kSelectThreads, k[i]);
+        }
+    }
+
     // Keys into LDS, the histogram of their first digit, and how many stay anyhow (to all threads).
     __device__ __forceinline__ unsigned first_digit() const
     {
@@ -118,15 +131,14 @@ struct Selector {
         if (tid == 0) shared[0] = 0;
         __syncthreads();
         unsigned always = 0;
-        for (int t = begin + 4 * tid; t < end; t += 4 * kSelectThreads) {
-            const u32x4_t k = look(t);
+        each([&](int t) { return look(t); }, [&](int t, const u32x4_t& k) {
             if (t - begin + 4 <= p.kept_keys) *reinterpret_cast<u32x4_t*>(kept_keys + (t - begin)) = k;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 always += k[i] == ~0u;
                 if (candidate(k[i])) atomicAdd(&bins[k[i] >> kDigitAt[0]], 1u);
             }
-        }
+        });
         if (always) atomicAdd(&shared[0], always);
         __syncthreads();
         return shared[0];
@@ -137,12 +149,11 @@ struct Selector {
         clear_bins();
         __syncthreads();
         const uint32_t mask = ~0u << kDigitAt[digit - 1];
-        for (int t = begin + 4 * tid; t < end; t += 4 * kSelectThreads) {
-            const u32x4_t k = keys_at(t);
+        each([&](int t) { return keys_at(t); }, [&](int, const u32x4_t& k) {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 if (candidate(k[i]) && (k[i] & mask) == prefix) atomicAdd(&bins[k[i] >> kDigitAt[digit] & (kBins - 1)], 1u);
-        }
+        });
         __syncthreads();
     }
 
@@ -164,6 +175,7 @@ struct Selector {
     struct Found {
         int bin;
         unsigned room, all;     // all: in all bins
+        unsigned count;         // in that bin
     };
     __device__ __forceinline__ Found find(unsigned c0, unsigned c1, unsigned room) const
     {
@@ -173,10 +185,11 @@ struct Selector {
             const bool second = room > before + c0;
             shared[kSelectWaves] = (uint32_t)(second ? b0 - 1 : b0);
             shared[kSelectWaves + 1] = room - before - (second ? c0 : 0u);
+            shared[kSelectWaves + 3] = second ? c1 : c0;
         }
         if (tid == kSelectThreads - 1) shared[kSelectWaves + 2] = to;
         __syncthreads();
-        return Found{(int)shared[kSelectWaves], shared[kSelectWaves + 1], shared[kSelectWaves + 2]};
+        return Found{(int)shared[kSelectWaves], shared[kSelectWaves + 1], shared[kSelectWaves + 2], shared[kSelectWaves + 3]};
     }
 
     // Writes down the positions whose keys are above `least`, and of those that have it the first `equal` behind `sames` of others; the first as the `places`-th.
@@ -254,13 +267,17 @@ __global__ void __launch_bounds__(kSelectThreads) kv_select_kernel(const EvictPa
         if (room != 0) {
             least = (uint32_t)f.bin << kDigitAt[0];
             equal = f.room;
+            bool all_of_bin = f.room == f.count;
 #pragma unroll
             for (int digit = 1; digit < kDigits; ++digit) {
+                if (all_of_bin) continue;                                               // (uniform) what is left to find out makes no difference
                 s.further_digit(digit, least);
                 f = s.find(s.bins[b0], s.bins[b0 - 1], equal);
                 least |= (uint32_t)f.bin << kDigitAt[digit];
                 equal = f.room;
+                all_of_bin = f.room == f.count;
             }
+            if (all_of_bin && least != 0u) { least -= 1; equal = 0; }                     // all keys from the bin on
         }
     }
     const unsigned all = s.write_down(least, equal, 0, 0);
@@ -288,16 +305,22 @@ __global__ void __launch_bounds__(kSelectThreads) kv_select_part_kernel(const Ev
     }
     // of the item: what came out of the digits before, the same in all parts
     unsigned always = 0, always_before = 0;
-    for (int i = 0; i < p.parts; ++i) {
-        always += states[i].always;
-        always_before += i < part ? states[i].always : 0u;
+    for (int i = s.lane; i < p.parts; i += kWave) {
+        const unsigned x = states[i].always;
+        always += x;
+        always_before += i < part ? x : 0u;
     }
+    for (int o = 1; o < kWave; o <<= 1) { always += (unsigned)__shfl_xor((int)always, o); always_before += (unsigned)__shfl_xor((int)always_before, o); }
+    if constexpr (PASS == kDigits)                                                      // the part's keys, for what follows
+        s.each([&](int t) { return s.look(t); }, [&](int t, const u32x4_t& k) {
+            if (t - s.begin + 4 <= p.kept_keys) *reinterpret_cast<u32x4_t*>(s.kept_keys + (t - s.begin)) = k;
+        });
     const unsigned room = PASS == 1 ? (unsigned)p.budget - always : states[part].room;
     uint32_t least = PASS == 1 ? 0u : states[part].prefix;
     unsigned before = PASS == 1 ? always_before : states[part].before;                  // what stays ahead of this part, of what is known
     const int b0 = kBins - 1 - 2 * s.tid;
     unsigned c0 = 0, c1 = 0, ahead0 = 0, ahead1 = 0;
-#pragma unroll 4
+#pragma unroll 8
     for (int i = 0; i < p.parts; ++i) {
         const u32x2_t x = *reinterpret_cast<const u32x2_t*>(bins_of + ((size_t)i * kDigits + PASS - 1) * kBins + b0 - 1);
         c0 += x[1];
@@ -665,7 +688,8 @@ extern "C" int codegemm_kv_evict(const codegemm_kv_cache* from, const codegemm_k
         hipLaunchKernelGGL(kv_select_part_kernel<0>, grid, threads, lds, s, p);
         hipLaunchKernelGGL(kv_select_part_kernel<1>, grid, threads, lds, s, p);
         hipLaunchKernelGGL(kv_select_part_kernel<2>, grid, threads, lds, s, p);
-        hipLaunchKernelGGL(kv_select_part_kernel<3>, grid, threads, lds, s, p);
+        p.kept_keys = kPartKept;
+        hipLaunchKernelGGL(kv_select_part_kernel<3>, grid, threads, lds + (size_t)p.kept_keys * sizeof(uint32_t), s, p);
     } else {
         const size_t lds = ((size_t)plan.kept_keys + kBins + 2 * kSelectWaves) * sizeof(uint32_t);
         st = set_max_lds(reinterpret_cast<const void*>(kv_select_kernel), lds);
