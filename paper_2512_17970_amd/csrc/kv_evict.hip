@@ -502,7 +502,7 @@ __global__ void __launch_bounds__(kMoveThreads) kv_move_kernel(const EvictParams
             const uint32_t how_of = FOUR ? (uint32_t)bit_of(in_row & 7) | (uint32_t)bit_of(place & 7) << 8 | in_row >> 3 << 16 | place >> 3 << 17
                                          : 8 * (in_row & 3) | 8 * (place & 3) << 8 | in_row >> 2 << 16 | place >> 2 << 18;
             const size_t at = page_at(b, to, head) + (size_t)(t & mask) * D;
-            constexpr int WORDS = TYPE == CODEGEMM_KV_FP16 ? 8 : 4, ROWS = 32 / WORDS;            // of a lane's part of a row; rows that are asked for at once
+            constexpr int WORDS = TYPE == CODEGEMM_KV_FP16 ? 8 : 4, ROWS = 4;            // of a lane's part of a row; rows that are asked for at once
             for (int d = lane; d < (FOUR ? D / 2 : D); d += kWave) {                               // (4 bits: two dimensions a lane)
                 uint32_t w[WORDS] = {0};
                 if constexpr (TYPE == CODEGEMM_KV_FP16) {       // a load for each token: of one row, they are of the same lines
