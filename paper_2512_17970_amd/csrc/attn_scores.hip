@@ -178,6 +178,9 @@ struct Keys {
     }
 };
 
+// Scores below kFine are taken off each other before they are rounded.  A row's sum of exp2(score) within these limits needs no maximum.
+constexpr float kFine = 1048576.0f, kLeastSum = 1.0e-18f, kMostSum = 1.0e30f;
+
 // Rows are worked on 32 at a time: two tiles, so that one's instructions fill the other's waits.
 constexpr int kPair = 2, kPairRows = 16 * kPair;
 
@@ -203,22 +206,32 @@ __device__ __forceinline__ void load_rows(const ScoreParams& p, const Queries& q
     const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), col = lane & 15, g = lane >> 4;
     const int tile0 = wave / PARTS, step = 16 * TILES;
     Row row(from + 16 * tile0 + col, p.r);
-    for (int i = 16 * tile0 + col; i < ceil_div(count, kPairRows) * kPairRows; i += step) {
-        const _Float16* q = p.q + (size_t)(qs.row0 + row.query) * p.q_stride + (size_t)(head * p.r + row.head) * D;
+    const int end = ceil_div(count, kPairRows) * kPairRows, rows_q = step / p.r, rows_h = step % p.r;
+    constexpr int EACH = (PARTS + kScoreWaves - 1) / kScoreWaves, AT_ONCE = 8 / EACH;                       // all of them under way before the first is put down
+    for (int i0 = 16 * tile0 + col; i0 < end; i0 += AT_ONCE * step) {
+        half8_t x[AT_ONCE][EACH];
 #pragma unroll
-        for (int k = 0; k < (PARTS + kScoreWaves - 1) / kScoreWaves; ++k) {
-            const int part = wave % PARTS + k * kScoreWaves;
-            const int d = type_is_four ? operand_dim<CODEGEMM_KV_INT4, DP>(part, g) : operand_dim<CODEGEMM_KV_FP16, DP>(part, g);
-            half8_t x = {0, 0, 0, 0, 0, 0, 0, 0};
-            if (i < count && d < D) x = *reinterpret_cast<const half8_t*>(q + d);
-            *reinterpret_cast<half8_t*>(to + ((size_t)(i / 16 * PARTS + part) * kWave + lane) * 8) = x;
+        for (int t = 0; t < AT_ONCE; ++t) {
+            const bool in = i0 + t * step < count;
+            const _Float16* q = p.q + (in ? (size_t)(qs.row0 + row.query) * p.q_stride + (size_t)(head * p.r + row.head) * D : 0);
+#pragma unroll
+            for (int k = 0; k < EACH; ++k) {
+                const int part = wave % PARTS + k * kScoreWaves, d = type_is_four ? operand_dim<CODEGEMM_KV_INT4, DP>(part, g) : operand_dim<CODEGEMM_KV_FP16, DP>(part, g);
+                x[t][k] = *reinterpret_cast<const half8_t*>(q + (d < D ? d : 0));
+                if (!in || d >= D) x[t][k] = half8_t{0, 0, 0, 0, 0, 0, 0, 0};
+            }
+            row.next(rows_q, rows_h, p.r);
         }
-        row.next(step / p.r, step % p.r, p.r);
+#pragma unroll
+        for (int t = 0; t < AT_ONCE; ++t)
+#pragma unroll
+            for (int k = 0; k < EACH; ++k)
+                if (i0 + t * step < end) *reinterpret_cast<half8_t*>(to + ((size_t)((i0 + t * step) / 16 * PARTS + wave % PARTS + k * kScoreWaves) * kWave + lane) * 8) = x[t][k];
     }
 }
 
-// 32 rows against the wavefront's keys; a lane's scores are those of rows `col` and 16 + `col` for tokens 4 g + r of every tile of keys, before they are scaled.  (Scaled scores are
-// rounded before a maximum is taken off, everywhere alike: fused, the largest score's own weight would be off by what large scores are rounded by.)
+// 32 rows against the wavefront's keys; a lane's scores are those of rows `col` and 16 + `col` for tokens 4 g + r of every tile of keys, before they are scaled.  (Where they are
+// large, scaled scores are rounded before a maximum is taken off: fused, the largest score's own weight would be off by what they are rounded by.)
 template <int TYPE, int DP, bool EXACT>
 __device__ __forceinline__ void score_pair(const Keys<TYPE, DP, EXACT>& keys, const _Float16* rows, int lane, float4_t (&s)[kPair][score_tiles(DP)])
 {
@@ -235,6 +248,21 @@ __device__ __forceinline__ void score_pair(const Keys<TYPE, DP, EXACT>& keys, co
 #pragma unroll
             for (int n = 0; n < TILES; ++n) s[k][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(keys.k[n][i], q, s[k][n], 0, 0, 0);
         }
+}
+
+// .. and 16 rows.
+template <int TYPE, int DP, bool EXACT>
+__device__ __forceinline__ void score_tile(const Keys<TYPE, DP, EXACT>& keys, const _Float16* rows, int lane, float4_t (&s)[score_tiles(DP)])
+{
+    constexpr int TILES = score_tiles(DP), PARTS = DP / 32;
+#pragma unroll
+    for (int n = 0; n < TILES; ++n) s[n] = float4_t{0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < PARTS; ++i) {
+        const half8_t q = *reinterpret_cast<const half8_t*>(rows + (size_t)(i * kWave + lane) * 8);
+#pragma unroll
+        for (int n = 0; n < TILES; ++n) s[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(keys.k[n][i], q, s[n], 0, 0, 0);
+    }
 }
 
 // Which tokens of its row a lane sees: t - t0 in lo .. hi, in tiles that have a page.
@@ -261,11 +289,13 @@ struct RowSpace {
     _Float16* rows;         // [tile][part][lane][8]
     Pair* sums;
     int* at;
+    float* lanes;           // (stats) [wavefront][tile][lane]: what a lane has added up itself
     __device__ __forceinline__ RowSpace(unsigned char* smem, int many, int copies)
-        : rows(reinterpret_cast<_Float16*>(smem)), sums(reinterpret_cast<Pair*>(smem + (size_t)many * DP * 2)), at(reinterpret_cast<int*>(sums + many * copies))
+        : rows(reinterpret_cast<_Float16*>(smem)), sums(reinterpret_cast<Pair*>(smem + (size_t)many * DP * 2)), at(reinterpret_cast<int*>(sums + many * copies)), lanes(reinterpret_cast<float*>(at + many))
     {
     }
     static size_t bytes(int many, int copies) { return (size_t)many * (DP * 2 + copies * sizeof(Pair) + sizeof(int)); }
+    static size_t lane_bytes(int many) { return (size_t)many * kScoreWaves * (kWave / 16) * sizeof(float); }
 };
 __device__ __forceinline__ void load_positions(const ScoreParams& p, const Queries& qs, int from, int count, int* at)
 {
@@ -287,78 +317,122 @@ __global__ void __launch_bounds__(kScoreThreads, 2) score_stats_kernel(const Sco
     const int count_all = qs.n * p.r, lowest = first_seen(p, qs.at) / BLOCK * BLOCK;   // of the first query's keys
     for (int from = blockIdx.z * many; from < count_all; from += gridDim.z * many) {
         const int count = count_all - from < many ? count_all - from : many;
-        int b = lowest + blockIdx.y * BLOCK;
+        const int begin = lowest + blockIdx.y * BLOCK;
         Codes<TYPE, DP, EXACT> codes;
-        if (b < qs.len) codes.load(p, seq, head, b + wave * 16 * TILES, qs.len, col, g);
+        if (begin < qs.len) codes.load(p, seq, head, begin + wave * 16 * TILES, qs.len, col, g);
         __syncthreads();
         load_rows<DP>(p, qs, head, from, count, D, TYPE == CODEGEMM_KV_INT4, space.rows);
         load_positions(p, qs, from, count, space.at);
-        for (int i = tid; i < kScoreWaves * many; i += kScoreThreads) space.sums[i] = Pair{-INFINITY, 0.0f};
+        for (int i = tid; i < kScoreWaves * many; i += kScoreThreads) space.sums[i] = Pair{0.0f, 0.0f};
+        for (int i = tid; i < kScoreWaves * many * (kWave / 16); i += kScoreThreads) space.lanes[i] = 0.0f;
         __syncthreads();
-        for (; b < qs.len; b += p.slots * BLOCK) {
-            const int t0 = b + wave * 16 * TILES;
-            Keys<TYPE, DP, EXACT> keys;
-            if (!AHEAD && b != lowest + (int)blockIdx.y * BLOCK) codes.load(p, seq, head, t0, qs.len, col, g);
-            keys.take(codes, p, g);
-            if (AHEAD) {
-                __builtin_amdgcn_sched_barrier(0);                                     // (the next codes come into the same registers)
-                if (qs.len - b > p.slots * BLOCK) codes.load(p, seq, head, t0 + p.slots * BLOCK, qs.len, col, g);
-                __builtin_amdgcn_sched_barrier(0);
+        // work(keys, t0, row) for the wavefront's blocks and pairs of tiles
+        auto all_blocks = [&](auto work) {
+            for (int b = begin; b < qs.len; b += p.slots * BLOCK) {
+                const int t0 = b + wave * 16 * TILES;
+                Keys<TYPE, DP, EXACT> keys;
+                if (!AHEAD && b != begin) codes.load(p, seq, head, t0, qs.len, col, g);
+                keys.take(codes, p, g);
+                if (AHEAD) {
+                    __builtin_amdgcn_sched_barrier(0);                                 // (the next codes come into the same registers)
+                    if (qs.len - b > p.slots * BLOCK) codes.load(p, seq, head, t0 + p.slots * BLOCK, qs.len, col, g);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                if (t0 >= qs.len) continue;
+                for (int row = 0; row < count; row += kPairRows) work(keys, t0, row);
             }
-            if (t0 >= qs.len) continue;
-            for (int row = 0; row < count; row += kPairRows) {
-                float4_t s[kPair][TILES];
-                score_pair<TYPE, DP, EXACT>(keys, space.rows + (size_t)row * DP, lane, s);
-                Pair* mine = space.sums + wave * many + row + col;
-                const Pair old[kPair] = {mine[0], mine[16]};
-                auto add = [&](auto is_whole) {
-                    constexpr bool whole = decltype(is_whole)::value;
-                    float most[kPair], sum[kPair], base[kPair], m[kPair];
+        };
+        // At first weights are exp2(score) as they are, which needs no maximum, and a lane adds up its own.  Sums that come out between kLeastSum and kMostSum are as
+        // good as any: what is lost below 2^-126 is nothing beside them.
+        all_blocks([&](const Keys<TYPE, DP, EXACT>& keys, int t0, int row) {
+            float4_t s[kPair][TILES];
+            score_pair<TYPE, DP, EXACT>(keys, space.rows + (size_t)row * DP, lane, s);
+            float* lanes = space.lanes + (wave * many + row) * (kWave / 16) + lane;
+            float sum[kPair] = {lanes[0], lanes[kWave]};
+            if (see_all(p, qs, space.at + row, t0, keys)) {
 #pragma unroll
-                    for (int k = 0; k < kPair; ++k) {
-                        const Seen seen = whole ? Seen{} : seen_of(p, qs, space.at[row + 16 * k + col], t0, keys);
-                        most[k] = -INFINITY;
+                for (int n = 0; n < TILES; ++n)
 #pragma unroll
-                        for (int n = 0; n < TILES; ++n)
+                    for (int r = 0; r < 4; ++r)
 #pragma unroll
-                            for (int r = 0; r < 4; ++r) {
-                                s[k][n][r] *= keys.by[n][r];
-                                if (!whole) s[k][n][r] = seen(n, r, g) ? s[k][n][r] : -INFINITY;
-                                most[k] = fmaxf(most[k], s[k][n][r]);
-                            }
-                    }
+                        for (int k = 0; k < kPair; ++k) sum[k] += __builtin_amdgcn_exp2f(s[k][n][r] * keys.by[n][r]);
+            } else {
 #pragma unroll
-                    for (int k = 0; k < kPair; ++k) {
-                        most[k] = over_groups(most[k], [](float a, float c) { return fmaxf(a, c); });
-                        m[k] = fmaxf(old[k].a, most[k]);
-                        base[k] = m[k] == -INFINITY ? 0.0f : m[k];
-                        sum[k] = 0.0f;
-                    }
+                for (int k = 0; k < kPair; ++k) {
+                    const Seen seen = seen_of(p, qs, space.at[row + 16 * k + col], t0, keys);
 #pragma unroll
                     for (int n = 0; n < TILES; ++n)
 #pragma unroll
-                        for (int r = 0; r < 4; ++r)
-#pragma unroll
-                            for (int k = 0; k < kPair; ++k) sum[k] += __builtin_amdgcn_exp2f(s[k][n][r] - base[k]);
-#pragma unroll
-                    for (int k = 0; k < kPair; ++k) {
-                        sum[k] = over_groups(sum[k], [](float a, float c) { return a + c; });
-                        if (g == 0) mine[16 * k] = Pair{m[k], __builtin_fmaf(old[k].b, __builtin_amdgcn_exp2f(old[k].a - base[k]), sum[k])};
-                    }
-                };
-                if (see_all(p, qs, space.at + row, t0, keys)) add(std::true_type());
-                else add(std::false_type());
+                        for (int r = 0; r < 4; ++r) sum[k] += seen(n, r, g) ? __builtin_amdgcn_exp2f(s[k][n][r] * keys.by[n][r]) : 0.0f;
+                }
             }
+            lanes[0] = sum[0];
+            lanes[kWave] = sum[1];
+        });
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");                              // (its own sums, by other lanes)
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        bool fine = true;
+        if (begin + wave * 16 * TILES < qs.len)
+            for (int row = lane; row < count; row += kWave) {
+                const float* lanes = space.lanes + (wave * many + row / 16 * 16) * (kWave / 16) + row % 16;
+                const float sum = (lanes[0] + lanes[16]) + (lanes[32] + lanes[48]);
+                fine = fine && sum > kLeastSum && sum < kMostSum;
+            }
+        // Where they do not (or a row sees nothing of the wavefront's keys, which looks the same), once more with every maximum followed.
+        if (!__all(fine)) {
+            if (!AHEAD || begin + p.slots * BLOCK < qs.len) codes.load(p, seq, head, begin + wave * 16 * TILES, qs.len, col, g);
+            for (int row = lane; row < count; row += kWave) space.sums[wave * many + row] = Pair{-INFINITY, 0.0f};
+            for (int i = lane; i < many * (kWave / 16); i += kWave) space.lanes[wave * many * (kWave / 16) + i] = 0.0f;
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+            all_blocks([&](const Keys<TYPE, DP, EXACT>& keys, int t0, int row) {
+#pragma unroll 1
+                for (int k = 0; k < kPair; ++k) {
+                    if (row + 16 * k >= count) break;
+                    float4_t s[TILES];
+                    score_tile<TYPE, DP, EXACT>(keys, space.rows + (size_t)(row + 16 * k) * DP, lane, s);
+                    Pair* mine = space.sums + wave * many + row + 16 * k + col;
+                    const bool is_row = row + 16 * k + col < count;
+                    const Pair old = is_row ? *mine : Pair{-INFINITY, 0.0f};
+                    const Seen seen = seen_of(p, qs, space.at[row + 16 * k + col], t0, keys);
+                    float most = -INFINITY;
+#pragma unroll
+                    for (int n = 0; n < TILES; ++n)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) most = fmaxf(most, seen(n, r, g) ? s[n][r] * keys.by[n][r] : -INFINITY);
+                    most = over_groups(most, [](float a, float c) { return fmaxf(a, c); });
+                    const float m = fmaxf(old.a, most), base = m == -INFINITY ? 0.0f : m;
+                    float sum = 0.0f;
+#pragma unroll
+                    for (int n = 0; n < TILES; ++n)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const float w = __builtin_amdgcn_exp2f(fabsf(base) < kFine ? __builtin_fmaf(s[n][r], keys.by[n][r], -base) : s[n][r] * keys.by[n][r] - base);
+                            sum += seen(n, r, g) ? w : 0.0f;
+                        }
+                    sum = over_groups(sum, [](float a, float c) { return a + c; });
+                    if (g == 0 && is_row) *mine = Pair{m, __builtin_fmaf(old.b, __builtin_amdgcn_exp2f(old.a - base), sum)};
+                }
+            });
         }
         __syncthreads();
         for (int i = tid; i < count; i += kScoreThreads) {
-            const Pair* state = space.sums + i;
+            // of a wavefront; one that has nothing says nothing about the maximum
+            Pair state[kScoreWaves];
             float m = -INFINITY, sum = 0.0f;
 #pragma unroll
-            for (int w = 0; w < kScoreWaves; ++w) m = fmaxf(m, state[w * many].a);
+            for (int w = 0; w < kScoreWaves; ++w) {
+                const float* lanes = space.lanes + (w * many + i / 16 * 16) * (kWave / 16) + i % 16;
+                const Pair x = space.sums[w * many + i];
+                state[w].b = x.b + ((lanes[0] + lanes[16]) + (lanes[32] + lanes[48]));
+                state[w].a = state[w].b == 0.0f ? -INFINITY : x.a;
+                m = fmaxf(m, state[w].a);
+            }
             const float base = m == -INFINITY ? 0.0f : m;
 #pragma unroll
-            for (int w = 0; w < kScoreWaves; ++w) sum += state[w * many].b * __builtin_amdgcn_exp2f(state[w * many].a - base);
+            for (int w = 0; w < kScoreWaves; ++w) sum += state[w].b * __builtin_amdgcn_exp2f(state[w].a - base);
             const int row = from + i;
             p.part[(size_t)blockIdx.y * p.rows + (size_t)(qs.row0 + row / p.r) * (p.c.Hk * p.r) + head * p.r + row % p.r] = Pair{m, sum};
         }
@@ -486,8 +560,8 @@ __global__ void __launch_bounds__(kScoreThreads, 2) score_sum_kernel(const Score
                     float4_t s[kPair][TILES];
                     score_pair<TYPE, DP, EXACT>(keys, space.rows + (size_t)row * DP, lane, s);
                     const Pair st[kPair] = {space.sums[row + col], space.sums[row + 16 + col]};
-                    auto add = [&](auto is_whole) {
-                        constexpr bool whole = decltype(is_whole)::value;
+                    auto add = [&](auto is_whole, auto is_fine) {
+                        constexpr bool whole = decltype(is_whole)::value, fine = decltype(is_fine)::value;
 #pragma unroll
                         for (int k = 0; k < kPair; ++k) {
                             const Seen seen = whole ? Seen{} : seen_of(p, qs, space.at[row + 16 * k + col], t0, keys);
@@ -495,14 +569,17 @@ __global__ void __launch_bounds__(kScoreThreads, 2) score_sum_kernel(const Score
                             for (int n = 0; n < TILES; ++n)
 #pragma unroll
                                 for (int r = 0; r < 4; ++r) {
-                                    const float w = __builtin_amdgcn_exp2f(s[k][n][r] * keys.by[n][r] - st[k].a), more = __builtin_fmaf(w, st[k].b, sum[4 * n + r]);
+                                    const float w = __builtin_amdgcn_exp2f(fine ? __builtin_fmaf(s[k][n][r], keys.by[n][r], -st[k].a) : s[k][n][r] * keys.by[n][r] - st[k].a);
+                                    const float more = __builtin_fmaf(w, st[k].b, sum[4 * n + r]);
                                     sum[4 * n + r] = whole || (seen(n, r, g) && st[k].b != 0.0f) ? more : sum[4 * n + r];
                                 }
                         }
                     };
                     // (rows that are none have no weight in the first form either: a score of 0, and 1 / sum 0)
-                    if (see_all(p, qs, space.at + row, t0, keys)) add(std::true_type());
-                    else add(std::false_type());
+                    const bool fine = __all(fabsf(st[0].a) < kFine && fabsf(st[1].a) < kFine);
+                    if (fine && see_all(p, qs, space.at + row, t0, keys)) add(std::true_type(), std::true_type());
+                    else if (fine) add(std::false_type(), std::true_type());
+                    else add(std::false_type(), std::false_type());
                 }
             }
         }
@@ -676,7 +753,7 @@ int launch_scores_one(ScoreParams p, const ScorePlan& plan, bool stats, hipStrea
         p.slots = plan.slots;
         p.many = rows < rows_at_once(DP, true) ? rows : rows_at_once(DP, true);
         auto fn = score_stats_kernel<TYPE, DP, EXACT>;
-        const size_t lds = RowSpace<DP>::bytes(p.many, kScoreWaves);
+        const size_t lds = RowSpace<DP>::bytes(p.many, kScoreWaves) + RowSpace<DP>::lane_bytes(p.many);
         const int st = set_max_lds(reinterpret_cast<const void*>(fn), lds);
         if (st) return st;
         hipLaunchKernelGGL(fn, dim3(items, (unsigned)plan.slots, (unsigned)plan.z), threads, lds, s, p);

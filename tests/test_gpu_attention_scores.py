@@ -216,6 +216,23 @@ def test_sums_are_what_was_given_out():
             assert bool(((got - 4).abs() <= 4 * (c.lens[i] + 64) * 2.0 ** -24).all())
 
 
+@pytest.mark.parametrize("size", [1e-3, 1.0, 8.0, 40.0, 600.0])
+@pytest.mark.parametrize("sign", [-1, 1])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_rows_whose_scores_are_all_far_from_zero(size, sign, dim):
+    """Keys that point one way, queries along it and against it: all scores of a row lie near sign * size * 8 (up to 4800 and more), on one side of what exp2 holds as on the
+    other; some rows small beside them."""
+    for new in ([40, 3], [1, 1]):
+        c = make([700, 90], FP16, heads=1, dim=dim, page=64)
+        g = torch.Generator().manual_seed(2)
+        c.k.copy_((1 + 0.02 * torch.randn(c.k.shape, generator=g)).half().cuda())
+        q = (sign * size * 8 / dim ** 0.5 * (1 + 0.1 * torch.rand(sum(new), 4, dim, generator=g))).half().cuda()
+        q[::3] *= 0.01
+        run(c, q, new)
+        if max(new) == 1:
+            run(c, q, new, single=True)
+
+
 @pytest.mark.parametrize("dtype,block", TYPES)
 def test_the_attention_beside_them(dtype, block):
     lens = [700, 3, 0, 64, 257]
