@@ -1,12 +1,19 @@
 // Softmax weights summed per cached token: what a token gets from the last queries of its sequence, in all query heads of its key head.
 //
-// A weight needs its row's maximum and sum first, so the keys are gone through twice: kernels of STATS leave both for every row (a query in a query head) and
+// A weight needs its row's sum first, so the keys are gone through twice: kernels of STATS leave a maximum and a sum for every row (a query in a query head) and
 // part of the keys, a small one joins the parts, and the last adds up exp2(score - maximum) / sum per token.  Single tokens have the first from the
 // attention itself.
 //
 // A wavefront has 16 TILES tokens of a sequence and key head in registers, as left operands of 16x16x32 products; the rows come by as right operands, 16 at
 // a time, from LDS, where the workgroup's four wavefronts share them.  The score tiles have four tokens and one row a lane: what rows need is
-// joined over four lanes, what tokens need over 16 at the very end, in a fixed order.
+// joined over four lanes, what tokens need over 16 at the very end, in a fixed order.  Keys are read and their codes turned into operands once for all rows (up to
+// 256), and nothing is written but 4 bytes a token.
+//
+// Rows by the hundred are bound by instructions: a product of 16x16x32 beside half as many vector instructions as it has scores (an exponential, one or two multiply-adds for
+// each), on two wavefronts a SIMD, which is what 64 tokens' operands in registers allow.  The last 32 queries of four prompts of 8192, 64 and 8 heads of 128, 8 bits: 33 us for
+// the rows' sums (maxima followed throughout took 42), 5 for the join, 37 for the weights; in all 69 us, 192 TFLOP/s.  The next product's instructions set between those of
+// the last one's weights, by hand, gained nothing.  Few rows are bound by the keys' bytes and the wait for them: 32 sequences of 206 000 tokens in all, 8 rows, 4 bits, 36 us beside
+// the attention's 59, 4.0 TB/s with what tokens had before and have now.
 #include <type_traits>
 
 #include "attn_common.h"
@@ -198,7 +205,7 @@ struct Row {
     }
 };
 
-// Rows from .. from + count - 1 into LDS, as right operands [tile][part][lane][8]; rows of queries that are none are zeros.
+// Rows from .. from + count - 1 into LDS, as right operands [tile][part][lane][8]; behind them the last one again, up to a pair of tiles.
 template <int DP>
 __device__ __forceinline__ void load_rows(const ScoreParams& p, const Queries& qs, int head, int from, int count, int D, int type_is_four, _Float16* to)
 {
@@ -206,6 +213,7 @@ __device__ __forceinline__ void load_rows(const ScoreParams& p, const Queries& q
     const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), col = lane & 15, g = lane >> 4;
     const int tile0 = wave / PARTS, step = 16 * TILES;
     Row row(from + 16 * tile0 + col, p.r);
+    const Row last(from + count - 1, p.r);
     const int end = ceil_div(count, kPairRows) * kPairRows, rows_q = step / p.r, rows_h = step % p.r;
     constexpr int EACH = (PARTS + kScoreWaves - 1) / kScoreWaves, AT_ONCE = 8 / EACH;                       // all of them under way before the first is put down
     for (int i0 = 16 * tile0 + col; i0 < end; i0 += AT_ONCE * step) {
@@ -213,12 +221,12 @@ __device__ __forceinline__ void load_rows(const ScoreParams& p, const Queries& q
 #pragma unroll
         for (int t = 0; t < AT_ONCE; ++t) {
             const bool in = i0 + t * step < count;
-            const _Float16* q = p.q + (in ? (size_t)(qs.row0 + row.query) * p.q_stride + (size_t)(head * p.r + row.head) * D : 0);
+            const _Float16* q = p.q + (size_t)(qs.row0 + (in ? row.query : last.query)) * p.q_stride + (size_t)(head * p.r + (in ? row.head : last.head)) * D;
 #pragma unroll
             for (int k = 0; k < EACH; ++k) {
                 const int part = wave % PARTS + k * kScoreWaves, d = type_is_four ? operand_dim<CODEGEMM_KV_INT4, DP>(part, g) : operand_dim<CODEGEMM_KV_FP16, DP>(part, g);
                 x[t][k] = *reinterpret_cast<const half8_t*>(q + (d < D ? d : 0));
-                if (!in || d >= D) x[t][k] = half8_t{0, 0, 0, 0, 0, 0, 0, 0};
+                if (d >= D) x[t][k] = half8_t{0, 0, 0, 0, 0, 0, 0, 0};
             }
             row.next(rows_q, rows_h, p.r);
         }
@@ -299,7 +307,7 @@ struct RowSpace {
 };
 __device__ __forceinline__ void load_positions(const ScoreParams& p, const Queries& qs, int from, int count, int* at)
 {
-    for (int i = threadIdx.x; i < ceil_div(count, kPairRows) * kPairRows; i += kScoreThreads) at[i] = qs.at + (from + i) / p.r;
+    for (int i = threadIdx.x; i < ceil_div(count, kPairRows) * kPairRows; i += kScoreThreads) at[i] = qs.at + (from + (i < count ? i : count - 1)) / p.r;
 }
 
 // Workgroup (sequence and key head, slot, z): rows z * 128 .. and on, over every slots-th block of keys.
@@ -314,7 +322,7 @@ __global__ void __launch_bounds__(kScoreThreads, 2) score_stats_kernel(const Sco
     const int D = EXACT ? DP : p.c.D, tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave), col = lane & 15, g = lane >> 4;
     const int seq = blockIdx.x / p.c.Hk, head = blockIdx.x % p.c.Hk;
     const Queries qs = queries_of(p, seq);
-    const int count_all = qs.n * p.r, lowest = first_seen(p, qs.at) / BLOCK * BLOCK;   // of the first query's keys
+    const int count_all = qs.n * p.r, seen0 = first_seen(p, qs.at), lowest = (seen0 < qs.len ? seen0 : qs.len) / BLOCK * BLOCK;       // of the first query's keys
     for (int from = blockIdx.z * many; from < count_all; from += gridDim.z * many) {
         const int count = count_all - from < many ? count_all - from : many;
         const int begin = lowest + blockIdx.y * BLOCK;
@@ -377,9 +385,9 @@ __global__ void __launch_bounds__(kScoreThreads, 2) score_stats_kernel(const Sco
             for (int row = lane; row < count; row += kWave) {
                 const float* lanes = space.lanes + (wave * many + row / 16 * 16) * (kWave / 16) + row % 16;
                 const float sum = (lanes[0] + lanes[16]) + (lanes[32] + lanes[48]);
-                fine = fine && sum > kLeastSum && sum < kMostSum;
+                fine = fine && ((sum > kLeastSum && sum < kMostSum) || (sum == 0.0f && space.at[row] < begin + wave * 16 * TILES));     // (it stands before all of them)
             }
-        // Where they do not (or a row sees nothing of the wavefront's keys, which looks the same), once more with every maximum followed.
+        // Where they do not, once more with every maximum followed.
         if (!__all(fine)) {
             if (!AHEAD || begin + p.slots * BLOCK < qs.len) codes.load(p, seq, head, begin + wave * 16 * TILES, qs.len, col, g);
             for (int row = lane; row < count; row += kWave) space.sums[wave * many + row] = Pair{-INFINITY, 0.0f};
@@ -511,8 +519,10 @@ __global__ void __launch_bounds__(kScoreThreads, 2) score_sum_kernel(const Score
         load_rows<DP>(p, qs, head, from, count, D, TYPE == CODEGEMM_KV_INT4, space.rows);
         load_positions(p, qs, from, count, space.at);
         for (int i = tid; i < ceil_div(count, kPairRows) * kPairRows; i += kScoreThreads) {
-            const int row = from + i;
-            space.sums[i] = i < count ? p.stats[(size_t)(qs.row0 + row / p.r) * (p.c.Hk * p.r) + head * p.r + row % p.r] : Pair{0.0f, 0.0f};
+            const int row = from + (i < count ? i : count - 1);
+            Pair st = p.stats[(size_t)(qs.row0 + row / p.r) * (p.c.Hk * p.r) + head * p.r + row % p.r];
+            if (i >= count) st.b = 0.0f;
+            space.sums[i] = st;
         }
         __syncthreads();
         return count;
@@ -620,17 +630,19 @@ __global__ void __launch_bounds__(kScoreThreads, DP >= 128 && TYPE == CODEGEMM_K
     };
     ask(t0);
     // The lane's row: its operands, where it stands, what its weights' logarithms lie below and 1 / their sum.
-    const int query = col / p.r, at = qs.at + (col < rows ? query : 0);
+    // (Behind the last row this again, without weight: a row of zeros would meet infinite keys.)
+    const int row = col < rows ? col : rows > 0 ? rows - 1 : 0, query = row / p.r, at = qs.at + query;
     half8_t q[PARTS];
 #pragma unroll
     for (int i = 0; i < PARTS; ++i) {
         half8_t x = {0, 0, 0, 0, 0, 0, 0, 0};
         const int d = operand_dim<TYPE, DP>(i, g);
-        if (col < rows && d < D) x = *reinterpret_cast<const half8_t*>(p.q + (size_t)(qs.row0 + query) * p.q_stride + (size_t)(head * p.r + col - query * p.r) * D + d);
+        if (rows > 0 && d < D) x = *reinterpret_cast<const half8_t*>(p.q + (size_t)(qs.row0 + query) * p.q_stride + (size_t)(head * p.r + row - query * p.r) * D + d);
         q[i] = x;
     }
     Pair st = {0.0f, 0.0f};
-    if (col < rows) st = p.stats[(size_t)(qs.row0 + query) * (p.c.Hk * p.r) + head * p.r + col - query * p.r];
+    if (rows > 0) st = p.stats[(size_t)(qs.row0 + query) * (p.c.Hk * p.r) + head * p.r + row - query * p.r];
+    if (col >= rows) st.b = 0.0f;
     const int seen_from = first_seen(p, qs.at + (qs.n > 0 ? qs.n - 1 : 0));                 // by all rows, up to the first one's position
     size_t place_last = 0;
     float last = 0.0f;

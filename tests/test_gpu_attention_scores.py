@@ -165,6 +165,26 @@ def test_more_queries_than_tokens_and_idle_slots():
     run(c, queries(3, 4, 64), [2, 1])
 
 
+@pytest.mark.parametrize("window", [0, 5])
+def test_the_largest_length(window):
+    """Of 2^31 - 1 tokens the table holds 64: rows without a window see them all, rows with one stand behind."""
+    c = make([64, 40], INT8, heads=1, dim=64, page=16, max_pages=4)
+    c.lens_dev.copy_(torch.tensor([2 ** 31 - 1, 40], dtype=torch.int32))
+    q = queries(6, 4, 64)
+    desc = cg.AttnDesc.make(4, 1, 64, num_seqs=2, total_q=6, max_kv=64, scale=0.125, window=window)
+    s = c.struct()
+    ws, n = workspace(cg.codegemm_attn_scores_workspace_bytes(s, desc))
+    scores = torch.full((c.pages, 1, 16), -7.0, device="cuda")
+    cg.codegemm_attn_scores(s, desc, q, starts([3, 3]), None, None, scores, ws, n, stream())
+    got = torch.stack([scores[c.page_of(0, t), 0, t % 16] for t in range(64)])
+    if window:
+        assert bool((got == 0).all())
+    else:
+        assert bool((got > 0).all()) and abs(float(got.double().sum()) - 12) < 1e-3
+    other = torch.stack([scores[c.page_of(1, t), 0, t % 16] for t in range(40)])
+    assert abs(float(other.double().sum()) - 12) < 1e-3
+
+
 def test_lengths_beyond_the_table():
     """The last places of the table are the last that count; queries stand behind them."""
     c = make([64, 40], INT4, heads=1, dim=64, page=16, max_pages=4)
@@ -267,6 +287,33 @@ def test_nan_keys_stay_with_those_who_see_them():
     cg.codegemm_attn_scores(s, desc, q, starts([10, 10]), None, None, scores.zero_(), ws, n, stream())
     got = torch.stack([scores[c.page_of(0, t), 0, t % 16] for t in range(40)])
     assert bool((got[:28] == 0).all()) and bool(got[28:33].isnan().all()) and bool(got[35:].isfinite().all())
+
+
+@pytest.mark.parametrize("new", [[1, 1], [9, 33]])
+def test_infinite_keys_that_all_rows_turn_away_from(new):
+    """A key of infinite length whose scores are -inf has no weight, and does not touch its neighbours', however many rows there are."""
+    c = make([200, 400], FP16, heads=2, dim=128, page=64, seed=12)
+    q = queries(sum(new), 6, 128)
+    q[..., 7] = -q[..., 7].abs() - 0.5
+    for t in (3, 100, 130):
+        page, slot = c.page_of(1, t), t % 64
+        c.k[page, :, slot, 7] = float("inf")
+    s = c.struct()
+    desc = cg.AttnDesc.make(6, 2, 128, num_seqs=2, total_q=sum(new), max_kv=400, scale=128 ** -0.5)
+    scores = torch.full((c.pages, 2, 64), -7.0, device="cuda")
+    if new == [1, 1]:
+        ws, n = workspace(cg.codegemm_attn_decode_scores_workspace_bytes(s, desc))
+        cg.codegemm_attn_decode_scores(s, desc, q, torch.empty_like(q), None, None, scores, ws, n, stream())
+    else:
+        ws, n = workspace(cg.codegemm_attn_scores_workspace_bytes(s, desc))
+        cg.codegemm_attn_scores(s, desc, q, starts(new), None, None, scores, ws, n, stream())
+    for i in range(2):
+        got = torch.stack([scores[c.page_of(i, t), :, t % 64] for t in range(c.lens[i])])
+        assert bool(got.isfinite().all())
+        # (weights are rounded to 24 bits a few times each; 2^-16 is far above that)
+        assert bool((got.double().sum(0) - 3 * new[i]).abs().max() < 3 * new[i] * 2.0 ** -16)
+        if i == 1:
+            assert bool((got[[3, 100, 130]] == 0).all())
 
 
 def test_strides_streams_and_graphs():
