@@ -20,6 +20,11 @@
 // Farthest from the bytes: long sequences with few key heads, whose pieces are as many as there are workgroups and are added up by one of them, 8 at a time:
 // 100 000 tokens with 8, 2 and 1 key heads take 45.7, 33.2 and 44.0 us for 205, 51 and 26 MB, 32 000 tokens 23.6, 26.6 and 25.7.
 // Heads of 80 are worked on as 128: 32 sequences of 206 376 tokens take 70 us for 265 MB, 3.8 TB/s; of 256, one wavefront a SIMD: 240 us for 848 MB, 3.5 TB/s.
+// 4 bits: a code is (code + 16) scale + offset in fp16 on the way into the matrix cores, two instructions for a pair of codes and one multiply-add, which is exact to
+// the cached value's one rounding; scales and offsets come with the codes into the ring.  The running maximum is not followed from step to step, but only where a
+// weight would pass 2^15.5: the largest lies between 2^10 and that.  Bound by the codes' way into operands as much as by bytes: 32 sequences of 206 000 tokens,
+// 58.7 us, 4.1 TB/s (of loads alone 52, of what is computed alone 55); three of 250 000 70.7 us, 4.5 TB/s; 13 of twenty heads of 64 with a window of 1500 19.2 us;
+// one of 701 9.3.
 #include <cmath>
 #include <type_traits>
 
