@@ -1,6 +1,8 @@
 // What the kernels around the paged cache share: its layout on the device, host checks, and the search for the sequence of a row.
 #pragma once
 
+#include <type_traits>
+
 #include "cg_common.h"
 
 namespace cg {
@@ -56,6 +58,21 @@ __device__ __forceinline__ int last_at_most(int n, int x, First first)
     }
     return __builtin_amdgcn_readfirstlane(base);
 }
+
+// The sum of the values up to the lane's own; all lanes' in the last lane.
+__device__ __forceinline__ unsigned wave_scan(unsigned x)
+{
+    auto add = [&](auto ctrl, auto rows) { x += (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, decltype(ctrl)::value, decltype(rows)::value, 0xf, false); };
+    typedef std::integral_constant<int, 0xf> all;
+    add(std::integral_constant<int, 0x111>(), all());      // row_shr 1, 2, 4, 8
+    add(std::integral_constant<int, 0x112>(), all());
+    add(std::integral_constant<int, 0x114>(), all());
+    add(std::integral_constant<int, 0x118>(), all());
+    add(std::integral_constant<int, 0x142>(), std::integral_constant<int, 0xa>());     // row_bcast 15 into rows 1 and 3
+    add(std::integral_constant<int, 0x143>(), std::integral_constant<int, 0xc>());     // row_bcast 31 into rows 2 and 3
+    return x;
+}
+__device__ __forceinline__ unsigned wave_sum(unsigned x) { return (unsigned)__builtin_amdgcn_readlane((int)wave_scan(x), kWave - 1); }
 
 // 8 codes to fp16, exactly.
 template <int TYPE>

@@ -92,19 +92,6 @@ struct DecodeStep {
     static_assert(kStages * kBytes >= kDecodeRows * DP * 4, "a wavefront's sums fit into its part of the ring");
 };
 
-// The sum of the values up to the lane's own; all lanes' in the last lane.
-__device__ __forceinline__ unsigned wave_scan(unsigned x)
-{
-    auto add = [&](auto ctrl, auto rows) { x += (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, decltype(ctrl)::value, decltype(rows)::value, 0xf, false); };
-    typedef std::integral_constant<int, 0xf> all;
-    add(std::integral_constant<int, 0x111>(), all());      // row_shr 1, 2, 4, 8
-    add(std::integral_constant<int, 0x112>(), all());
-    add(std::integral_constant<int, 0x114>(), all());
-    add(std::integral_constant<int, 0x118>(), all());
-    add(std::integral_constant<int, 0x142>(), std::integral_constant<int, 0xa>());     // row_bcast 15 into rows 1 and 3
-    add(std::integral_constant<int, 0x143>(), std::integral_constant<int, 0xc>());     // row_bcast 31 into rows 2 and 3
-    return x;
-}
 __device__ __forceinline__ unsigned wave_max(unsigned x)
 {
     for (int o = 1; o < kWave; o <<= 1) {
@@ -113,7 +100,6 @@ __device__ __forceinline__ unsigned wave_max(unsigned x)
     }
     return (unsigned)__builtin_amdgcn_readfirstlane((int)x);
 }
-__device__ __forceinline__ unsigned wave_sum(unsigned x) { return (unsigned)__builtin_amdgcn_readlane((int)wave_scan(x), kWave - 1); }
 
 // A sequence's tokens lo .. len - 1; its steps start at multiples of their length.  One without tokens has a step all the same, in
 // which nothing counts, and so gets its zeros.

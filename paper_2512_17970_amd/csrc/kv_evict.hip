@@ -164,10 +164,7 @@ struct Selector {
     // The sum of x over the threads up to this one.
     __device__ __forceinline__ unsigned upto(unsigned x) const
     {
-        for (int o = 1; o < kWave; o <<= 1) {
-            const unsigned y = (unsigned)__shfl_up((int)x, o);
-            x += lane >= o ? y : 0u;
-        }
+        x = wave_scan(x);
         __syncthreads();
         if (lane == kWave - 1) shared[wave] = x;
         __syncthreads();
@@ -209,7 +206,8 @@ struct Selector {
 #pragma unroll
             for (int i = 0; i < 4; ++i) { above += k[i] > least; same += least != 0u && k[i] == least; }
         }
-        for (int o = 1; o < kWave; o <<= 1) { above += (unsigned)__shfl_xor((int)above, o); same += (unsigned)__shfl_xor((int)same, o); }
+        above = wave_sum(above);
+        same = wave_sum(same);
         __syncthreads();
         if (lane == 0) { shared[wave] = above; shared[kSelectWaves + wave] = same; }
         __syncthreads();
@@ -232,11 +230,7 @@ struct Selector {
             unsigned a4 = 0;
 #pragma unroll
             for (int i = 0; i < 4; ++i) a4 += k[i] > least;
-            unsigned both = s4 << 16 | a4;
-            for (int o = 1; o < kWave; o <<= 1) {
-                const unsigned y = (unsigned)__shfl_up((int)both, o);
-                both += lane >= o ? y : 0u;
-            }
+            const unsigned both = wave_scan(s4 << 16 | a4);
             unsigned s_before = sames + (both >> 16) - s4, a_before = (both & 0xffffu) - a4;
             auto taken_of = [&](unsigned upto_same) { return (upto_same < equal ? upto_same : equal) - (sames < equal ? sames : equal); };      // since the wavefront's first
 #pragma unroll
@@ -314,7 +308,8 @@ __global__ void __launch_bounds__(kSelectThreads) kv_select_part_kernel(const Ev
         always += x;
         always_before += i < part ? x : 0u;
     }
-    for (int o = 1; o < kWave; o <<= 1) { always += (unsigned)__shfl_xor((int)always, o); always_before += (unsigned)__shfl_xor((int)always_before, o); }
+    always = wave_sum(always);
+    always_before = wave_sum(always_before);
     if constexpr (PASS == kDigits)                                                      // the part's keys, for what follows
         s.each([&](int t) { return s.look(t); }, [&](int t, const u32x4_t& k) {
             if (t - s.begin + 4 <= p.kept_keys) *reinterpret_cast<u32x4_t*>(s.kept_keys + (t - s.begin)) = k;
