@@ -537,7 +537,7 @@ int codegemm_attn_decode(const codegemm_kv_cache *cache, const codegemm_attn_des
  * sequence only.  cu_q NULL: one query each, total_q = num_seqs.  Queries at negative
  * positions see nothing.  In fp32, in a fixed order.  total_kv, k_stride, v_stride and
  * out_stride of desc are not read; kv_heads, head_dim and num_seqs are those of the cache.
- * workspace: as for codegemm_attn_decode.  num_seqs * kv_heads < 2^24, total_q * q_heads < 2^31.
+ * workspace: as for codegemm_attn_decode.  num_seqs * kv_heads < 2^24, total_q * q_heads <= 2^30.
  */
 size_t codegemm_attn_scores_workspace_bytes(const codegemm_kv_cache *cache, const codegemm_attn_desc *desc);
 int codegemm_attn_scores(const codegemm_kv_cache *cache, const codegemm_attn_desc *desc,

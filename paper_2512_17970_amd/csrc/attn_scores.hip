@@ -706,7 +706,7 @@ int score_plan(const codegemm_kv_cache* cache, const codegemm_attn_desc* d, bool
     if (st) return st;
     if (d->kv_heads != cache->kv_heads || d->head_dim != cache->head_dim || d->num_seqs != cache->num_seqs) return CODEGEMM_INVALID_ARG;
     const long long rows = (long long)d->total_q * d->q_heads, items = (long long)d->num_seqs * d->kv_heads;
-    if (rows >= 1ll << 31) return CODEGEMM_UNSUPPORTED;
+    if (rows > 1ll << 30) return CODEGEMM_UNSUPPORTED;                                     // (a workgroup steps on from row to row in 32 bits)
     if (too_many(items, kScoreThreads)) return CODEGEMM_UNSUPPORTED;
     const int held = cache->max_pages * cache->page_size, longest = d->max_kv < held ? d->max_kv : held;
     const int block = 16 * score_tiles(d->head_dim > 128 ? 256 : 128) * kScoreWaves;

@@ -121,5 +121,7 @@ def test_launches_that_are_too_large():
     assert status(cg.codegemm_kv_evict, c, c, cg.EvictDesc.make(5, max_kv=9), AT, None, None, AT, None, AT, 1 << 60) == UNSUPPORTED
     d = attn(q_heads=1024, kv_heads=1024, num_seqs=65535, total_q=65535)
     assert cg.codegemm_attn_scores_workspace_bytes(c, d) == 0 and status(cg.codegemm_attn_scores, c, d, AT, None, None, None, AT, AT, 1 << 60) == UNSUPPORTED
+    assert cg.codegemm_attn_scores_workspace_bytes(cache(), attn(q_heads=64, kv_heads=2, total_q=1 << 24)) > 0
+    assert cg.codegemm_attn_scores_workspace_bytes(cache(), attn(q_heads=66, kv_heads=2, total_q=1 << 24)) == 0
     d = attn(q_heads=1024, kv_heads=2, total_q=1 << 24)
     assert cg.codegemm_attn_scores_workspace_bytes(cache(), d) == 0 and status(cg.codegemm_attn_scores, cache(), d, AT, AT, None, None, AT, AT, 1 << 60) == UNSUPPORTED
