@@ -273,15 +273,25 @@ __device__ __forceinline__ void score_tile(const Keys<TYPE, DP, EXACT>& keys, co
     }
 }
 
-// Which tokens of its row a lane sees: t - t0 in lo .. hi, in tiles that have a page.
+// Which of the tokens t0 + 16 n + 4 g + r a lane's row sees: those that lie `span` at most behind the first one, in tiles that have a page.  (One compare each, nothing
+// through the scalar unit.)
+constexpr int kNowhere = 0x40000000;        // a span is less
+template <int TILES>
 struct Seen {
-    int lo, hi, ok;
-    __device__ __forceinline__ bool operator()(int n, int r, int g) const { const int t = 16 * n + 4 * g + r; return (ok >> n & 1) && t >= lo && t <= hi; }
+    int from[TILES];
+    unsigned span;
+    __device__ __forceinline__ bool operator()(int n, int r) const { return (unsigned)(from[n] + r) <= span; }
 };
-template <class T>
-__device__ __forceinline__ Seen seen_of(const ScoreParams& p, const Queries& qs, int at, int t0, const T& keys)
+template <int TILES>
+__device__ __forceinline__ Seen<TILES> seen_of(const ScoreParams& p, const Queries& qs, int at, int t0, int ok, int g)
 {
-    return Seen{first_seen(p, at) - t0, (at < qs.len ? at : qs.len - 1) - t0, keys.ok};
+    const int lo = first_seen(p, at) - t0, hi = (at < qs.len ? at : qs.len - 1) - t0;
+    Seen<TILES> s;
+    s.span = (unsigned)(hi - lo);
+#pragma unroll
+    for (int n = 0; n < TILES; ++n) s.from[n] = (ok >> n & 1) && hi >= lo ? 16 * n + 4 * g - lo : kNowhere;
+    if (hi < lo) s.span = 0;
+    return s;
 }
 // Whether 32 rows all see all of a wavefront's tokens.
 template <class T>
@@ -367,11 +377,11 @@ __global__ void __launch_bounds__(kScoreThreads, 2) score_stats_kernel(const Sco
             } else {
 #pragma unroll
                 for (int k = 0; k < kPair; ++k) {
-                    const Seen seen = seen_of(p, qs, space.at[row + 16 * k + col], t0, keys);
+                    const Seen<TILES> seen = seen_of<TILES>(p, qs, space.at[row + 16 * k + col], t0, keys.ok, g);
 #pragma unroll
                     for (int n = 0; n < TILES; ++n)
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) sum[k] += seen(n, r, g) ? __builtin_amdgcn_exp2f(s[k][n][r] * keys.by[n][r]) : 0.0f;
+                        for (int r = 0; r < 4; ++r) sum[k] += seen(n, r) ? __builtin_amdgcn_exp2f(s[k][n][r] * keys.by[n][r]) : 0.0f;
                 }
             }
             lanes[0] = sum[0];
@@ -404,12 +414,12 @@ __global__ void __launch_bounds__(kScoreThreads, 2) score_stats_kernel(const Sco
                     Pair* mine = space.sums + wave * many + row + 16 * k + col;
                     const bool is_row = row + 16 * k + col < count;
                     const Pair old = is_row ? *mine : Pair{-INFINITY, 0.0f};
-                    const Seen seen = seen_of(p, qs, space.at[row + 16 * k + col], t0, keys);
+                    const Seen<TILES> seen = seen_of<TILES>(p, qs, space.at[row + 16 * k + col], t0, keys.ok, g);
                     float most = -INFINITY;
 #pragma unroll
                     for (int n = 0; n < TILES; ++n)
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) most = fmaxf(most, seen(n, r, g) ? s[n][r] * keys.by[n][r] : -INFINITY);
+                        for (int r = 0; r < 4; ++r) most = fmaxf(most, seen(n, r) ? s[n][r] * keys.by[n][r] : -INFINITY);
                     most = over_groups(most, [](float a, float c) { return fmaxf(a, c); });
                     const float m = fmaxf(old.a, most), base = m == -INFINITY ? 0.0f : m;
                     float sum = 0.0f;
@@ -418,7 +428,7 @@ __global__ void __launch_bounds__(kScoreThreads, 2) score_stats_kernel(const Sco
 #pragma unroll
                         for (int r = 0; r < 4; ++r) {
                             const float w = __builtin_amdgcn_exp2f(fabsf(base) < kFine ? __builtin_fmaf(s[n][r], keys.by[n][r], -base) : s[n][r] * keys.by[n][r] - base);
-                            sum += seen(n, r, g) ? w : 0.0f;
+                            sum += seen(n, r) ? w : 0.0f;
                         }
                     sum = over_groups(sum, [](float a, float c) { return a + c; });
                     if (g == 0 && is_row) *mine = Pair{m, __builtin_fmaf(old.b, __builtin_amdgcn_exp2f(old.a - base), sum)};
@@ -574,14 +584,14 @@ __global__ void __launch_bounds__(kScoreThreads, 2) score_sum_kernel(const Score
                         constexpr bool whole = decltype(is_whole)::value, fine = decltype(is_fine)::value;
 #pragma unroll
                         for (int k = 0; k < kPair; ++k) {
-                            const Seen seen = whole ? Seen{} : seen_of(p, qs, space.at[row + 16 * k + col], t0, keys);
+                            const Seen<TILES> seen = whole ? Seen<TILES>{} : seen_of<TILES>(p, qs, space.at[row + 16 * k + col], t0, keys.ok, g);
 #pragma unroll
                             for (int n = 0; n < TILES; ++n)
 #pragma unroll
                                 for (int r = 0; r < 4; ++r) {
                                     const float w = __builtin_amdgcn_exp2f(fine ? __builtin_fmaf(s[k][n][r], keys.by[n][r], -st[k].a) : s[k][n][r] * keys.by[n][r] - st[k].a);
                                     const float more = __builtin_fmaf(w, st[k].b, sum[4 * n + r]);
-                                    sum[4 * n + r] = whole || (seen(n, r, g) && st[k].b != 0.0f) ? more : sum[4 * n + r];
+                                    sum[4 * n + r] = whole || (seen(n, r) && st[k].b != 0.0f) ? more : sum[4 * n + r];
                                 }
                         }
                     };
@@ -674,11 +684,11 @@ __global__ void __launch_bounds__(kScoreThreads, DP >= 128 && TYPE == CODEGEMM_K
 #pragma unroll
                 for (int r = 0; r < 4; ++r) sum[4 * n + r] = __builtin_amdgcn_exp2f(s[n][r] * keys.by[n][r] - st.a) * st.b;
             if (!whole) {
-                const Seen seen = Seen{first_seen(p, at) - t0, (at < qs.len ? at : qs.len - 1) - t0, ok};
+                const Seen<TILES> seen = seen_of<TILES>(p, qs, at, t0, ok, g);
 #pragma unroll
                 for (int n = 0; n < TILES; ++n)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) sum[4 * n + r] = seen(n, r, g) && st.b != 0.0f ? sum[4 * n + r] : 0.0f;
+                    for (int r = 0; r < 4; ++r) sum[4 * n + r] = seen(n, r) && st.b != 0.0f ? sum[4 * n + r] : 0.0f;
             }
         }
         over_columns<VALUES>(sum, col);
