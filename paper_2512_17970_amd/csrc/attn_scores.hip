@@ -283,14 +283,14 @@ struct Seen {
     __device__ __forceinline__ bool operator()(int n, int r) const { return (unsigned)(from[n] + r) <= span; }
 };
 template <int TILES>
-__device__ __forceinline__ Seen<TILES> seen_of(const ScoreParams& p, const Queries& qs, int at, int t0, int ok, int g)
+__device__ __forceinline__ Seen<TILES> seen_of(const ScoreParams& p, const Queries& qs, int at, int t0, int ok, int g, bool weighs = true)
 {
     const int lo = first_seen(p, at) - t0, hi = (at < qs.len ? at : qs.len - 1) - t0;
+    const bool any = hi >= lo && weighs;
     Seen<TILES> s;
-    s.span = (unsigned)(hi - lo);
+    s.span = any ? (unsigned)(hi - lo) : 0u;
 #pragma unroll
-    for (int n = 0; n < TILES; ++n) s.from[n] = (ok >> n & 1) && hi >= lo ? 16 * n + 4 * g - lo : kNowhere;
-    if (hi < lo) s.span = 0;
+    for (int n = 0; n < TILES; ++n) s.from[n] = (ok >> n & 1) && any ? 16 * n + 4 * g - lo : kNowhere;
     return s;
 }
 // Whether 32 rows all see all of a wavefront's tokens.
@@ -584,14 +584,14 @@ __global__ void __launch_bounds__(kScoreThreads, 2) score_sum_kernel(const Score
                         constexpr bool whole = decltype(is_whole)::value, fine = decltype(is_fine)::value;
 #pragma unroll
                         for (int k = 0; k < kPair; ++k) {
-                            const Seen<TILES> seen = whole ? Seen<TILES>{} : seen_of<TILES>(p, qs, space.at[row + 16 * k + col], t0, keys.ok, g);
+                            const Seen<TILES> seen = whole ? Seen<TILES>{} : seen_of<TILES>(p, qs, space.at[row + 16 * k + col], t0, keys.ok, g, st[k].b != 0.0f);
 #pragma unroll
                             for (int n = 0; n < TILES; ++n)
 #pragma unroll
                                 for (int r = 0; r < 4; ++r) {
                                     const float w = __builtin_amdgcn_exp2f(fine ? __builtin_fmaf(s[k][n][r], keys.by[n][r], -st[k].a) : s[k][n][r] * keys.by[n][r] - st[k].a);
                                     const float more = __builtin_fmaf(w, st[k].b, sum[4 * n + r]);
-                                    sum[4 * n + r] = whole || (seen(n, r) && st[k].b != 0.0f) ? more : sum[4 * n + r];
+                                    sum[4 * n + r] = whole || seen(n, r) ? more : sum[4 * n + r];
                                 }
                         }
                     };
@@ -684,11 +684,11 @@ __global__ void __launch_bounds__(kScoreThreads, DP >= 128 && TYPE == CODEGEMM_K
 #pragma unroll
                 for (int r = 0; r < 4; ++r) sum[4 * n + r] = __builtin_amdgcn_exp2f(s[n][r] * keys.by[n][r] - st.a) * st.b;
             if (!whole) {
-                const Seen<TILES> seen = seen_of<TILES>(p, qs, at, t0, ok, g);
+                const Seen<TILES> seen = seen_of<TILES>(p, qs, at, t0, ok, g, st.b != 0.0f);
 #pragma unroll
                 for (int n = 0; n < TILES; ++n)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) sum[4 * n + r] = seen(n, r) && st.b != 0.0f ? sum[4 * n + r] : 0.0f;
+                    for (int r = 0; r < 4; ++r) sum[4 * n + r] = seen(n, r) ? sum[4 * n + r] : 0.0f;
             }
         }
         over_columns<VALUES>(sum, col);
