@@ -9,11 +9,11 @@
 // joined over four lanes, what tokens need over 16 at the very end, in a fixed order.  Keys are read and their codes turned into operands once for all rows (up to
 // 256), and nothing is written but 4 bytes a token.
 //
-// Rows by the hundred are bound by instructions: a product of 16x16x32 beside half as many vector instructions as it has scores (an exponential, one or two multiply-adds for
-// each), on two wavefronts a SIMD, which is what 64 tokens' operands in registers allow.  The last 32 queries of four prompts of 8192, 64 and 8 heads of 128, 8 bits: 33 us for
-// the rows' sums (maxima followed throughout took 42), 5 for the join, 37 for the weights; in all 69 us, 192 TFLOP/s.  The next product's instructions set between those of
-// the last one's weights, by hand, gained nothing.  Few rows are bound by the keys' bytes and the wait for them: 32 sequences of 206 000 tokens in all, 8 rows, 4 bits, 36 us beside
-// the attention's 59, 4.0 TB/s with what tokens had before and have now.
+// Rows by the hundred are bound by instructions: for every four products of 16x16x32 (a head of 128) a lane has four scores, an exponential and one or two multiply-adds
+// each, beside what turns codes into operands, on the two wavefronts a SIMD that 64 tokens' operands in registers allow.  The last 32 queries of four prompts of 8192,
+// 64 and 8 heads of 128, 8 bits: 32 us for the rows' sums (maxima followed throughout: 42), 5 for the join, 34 for the weights; in all 63 us, 212 TFLOP/s.  The next product's
+// instructions set between those of the last one's weights, by hand, gained nothing.  Few rows are bound by the keys' bytes and the wait for them: 32 sequences of 206 000
+// tokens in all, 8 rows, 4 bits, 36 us beside the attention's 59, 4.0 TB/s with what tokens had before and have now.
 #include <type_traits>
 
 #include "attn_common.h"
@@ -273,8 +273,9 @@ __device__ __forceinline__ void score_tile(const Keys<TYPE, DP, EXACT>& keys, co
     }
 }
 
-// Which of the tokens t0 + 16 n + 4 g + r a lane's row sees: those that lie `span` at most behind the first one, in tiles that have a page.  (One compare each, nothing
-// through the scalar unit.)
+// Which of the tokens t0 + 16 n + 4 g + r a lane's row sees: those that lie `span` at most behind the first one, in tiles that have a page; rows that are not to have
+// weight see none.  One compare each, nothing through the scalar unit: few blocks need it, but the workgroups that all others wait for have them (two compares and a bit
+// joined there: 69.5 us for the 63 above; a loop of one body for all tiles 90, tiles that are seen as a whole told apart 72).
 constexpr int kNowhere = 0x40000000;        // a span is less
 template <int TILES>
 struct Seen {
