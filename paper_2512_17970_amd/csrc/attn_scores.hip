@@ -185,8 +185,8 @@ struct Keys {
     }
 };
 
-// Scores below kFine are taken off each other before they are rounded.  A row's sum of exp2(score) within these limits needs no maximum.
-constexpr float kFine = 1048576.0f, kLeastSum = 1.0e-18f, kMostSum = 1.0e30f;
+// A row's sum of exp2(score) within these limits needs no maximum.
+constexpr float kLeastSum = 1.0e-18f, kMostSum = 1.0e30f;
 
 // Rows are worked on 32 at a time: two tiles, so that one's instructions fill the other's waits.
 constexpr int kPair = 2, kPairRows = 16 * kPair;
@@ -238,8 +238,9 @@ __device__ __forceinline__ void load_rows(const ScoreParams& p, const Queries& q
     }
 }
 
-// 32 rows against the wavefront's keys; a lane's scores are those of rows `col` and 16 + `col` for tokens 4 g + r of every tile of keys, before they are scaled.  (Where they are
-// large, scaled scores are rounded before a maximum is taken off: fused, the largest score's own weight would be off by what they are rounded by.)
+// 32 rows against the wavefront's keys; a lane's scores are those of rows `col` and 16 + `col` for tokens 4 g + r of every tile of keys, before they are scaled.  (Scaled scores are
+// rounded to 32 bits before a maximum is taken off, in every kernel that makes a row's sum, the attention among them, and in every one that makes its weights: were it fused in some, a
+// row would give out 2^(half of the last place of its scores) times 1, 2 % from scores of 2^20 on.)
 template <int TYPE, int DP, bool EXACT>
 __device__ __forceinline__ void score_pair(const Keys<TYPE, DP, EXACT>& keys, const _Float16* rows, int lane, float4_t (&s)[kPair][score_tiles(DP)])
 {
@@ -428,7 +429,7 @@ __global__ void __launch_bounds__(kScoreThreads, 2) score_stats_kernel(const Sco
                     for (int n = 0; n < TILES; ++n)
 #pragma unroll
                         for (int r = 0; r < 4; ++r) {
-                            const float w = __builtin_amdgcn_exp2f(fabsf(base) < kFine ? __builtin_fmaf(s[n][r], keys.by[n][r], -base) : s[n][r] * keys.by[n][r] - base);
+                            const float w = __builtin_amdgcn_exp2f(s[n][r] * keys.by[n][r] - base);
                             sum += seen(n, r) ? w : 0.0f;
                         }
                     sum = over_groups(sum, [](float a, float c) { return a + c; });
@@ -581,26 +582,26 @@ __global__ void __launch_bounds__(kScoreThreads, 2) score_sum_kernel(const Score
                     float4_t s[kPair][TILES];
                     score_pair<TYPE, DP, EXACT>(keys, space.rows + (size_t)row * DP, lane, s);
                     const Pair st[kPair] = {space.sums[row + col], space.sums[row + 16 + col]};
-                    auto add = [&](auto is_whole, auto is_fine) {
-                        constexpr bool whole = decltype(is_whole)::value, fine = decltype(is_fine)::value;
+                    auto add = [&](auto is_plain) {
+                        constexpr bool plain = decltype(is_plain)::value;
 #pragma unroll
                         for (int k = 0; k < kPair; ++k) {
-                            const Seen<TILES> seen = whole ? Seen<TILES>{} : seen_of<TILES>(p, qs, space.at[row + 16 * k + col], t0, keys.ok, g, st[k].b != 0.0f);
+                            const Seen<TILES> seen = plain ? Seen<TILES>{} : seen_of<TILES>(p, qs, space.at[row + 16 * k + col], t0, keys.ok, g, st[k].b != 0.0f);
 #pragma unroll
                             for (int n = 0; n < TILES; ++n)
 #pragma unroll
                                 for (int r = 0; r < 4; ++r) {
-                                    const float w = __builtin_amdgcn_exp2f(fine ? __builtin_fmaf(s[k][n][r], keys.by[n][r], -st[k].a) : s[k][n][r] * keys.by[n][r] - st[k].a);
+                                    const float score = s[k][n][r] * keys.by[n][r];
+                                    const float w = __builtin_amdgcn_exp2f(plain ? score : score - st[k].a);
                                     const float more = __builtin_fmaf(w, st[k].b, sum[4 * n + r]);
-                                    sum[4 * n + r] = whole || seen(n, r) ? more : sum[4 * n + r];
+                                    sum[4 * n + r] = plain || seen(n, r) ? more : sum[4 * n + r];
                                 }
                         }
                     };
-                    // (rows that are none have no weight in the first form either: a score of 0, and 1 / sum 0)
-                    const bool fine = __all(fabsf(st[0].a) < kFine && fabsf(st[1].a) < kFine);
-                    if (fine && see_all(p, qs, space.at + row, t0, keys)) add(std::true_type(), std::true_type());
-                    else if (fine) add(std::false_type(), std::true_type());
-                    else add(std::false_type(), std::false_type());
+                    // Nearly always: rows whose sums needed no maximum, which is 0 then, and keys that all of them see.  (Rows that are none have no weight here either: scores of
+                    // one that is, and 1 / sum 0.)
+                    if (__all(st[0].a == 0.0f && st[1].a == 0.0f) && see_all(p, qs, space.at + row, t0, keys)) add(std::true_type());
+                    else add(std::false_type());
                 }
             }
         }
