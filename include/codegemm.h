@@ -494,7 +494,7 @@ typedef struct codegemm_attn_desc {
     int32_t head_dim;           /* D: a multiple of 16, 16..256                                         */
     int32_t num_seqs;           /* 1..65535                                                             */
     int32_t total_q;            /* rows of q, 1..2^24; codegemm_attn_decode: num_seqs                   */
-    int32_t total_kv;           /* rows of k and v, 0..2^24 (codegemm_attn_decode: not read)            */
+    int32_t total_kv;           /* rows of k and v, 0..2^24 (0 will do where keys are in a cache)       */
     int32_t max_kv;             /* keys of the longest sequence as far as the host knows, >= 1: chooses */
                                 /* how keys are split; longer ones are right all the same               */
     int32_t window;             /* 0, or keys that a query sees: the last `window` up to its position   */
@@ -536,7 +536,8 @@ int codegemm_attn_decode(const codegemm_kv_cache *cache, const codegemm_attn_des
  * earlier may be NULL.  Other places of scores stay as they are.  A page may belong to one
  * sequence only.  cu_q NULL: one query each, total_q = num_seqs.  Queries at negative
  * positions see nothing.  In fp32, in a fixed order.  total_kv, k_stride, v_stride and
- * out_stride of desc are not read; kv_heads, head_dim and num_seqs are those of the cache.
+ * out_stride of desc have no effect, but are refused outside their ranges as everywhere;
+ * kv_heads, head_dim and num_seqs are those of the cache.
  * workspace: as for codegemm_attn_decode.  num_seqs * kv_heads < 2^24, total_q * q_heads <= 2^30.
  */
 size_t codegemm_attn_scores_workspace_bytes(const codegemm_kv_cache *cache, const codegemm_attn_desc *desc);
