@@ -43,7 +43,9 @@ constexpr float kLeastLog = -40.0f;         // of a scale's logarithm in the run
 // the weight and values near zero, thousands of others with little weight each make the result.  (With 1 for the largest, the weights of the keys that share
 // a wavefront with such a key were off by 2.6 % at 15 nats below it, by 44 % at 17, and zero at 18.)  Not from scores of kFine on, which may have no place for it.
 constexpr float kLift = 14.0f, kFine = 1048576.0f;
-constexpr float kLowLift = 10.0f, kReach = 5.5f;       // 4 bits: the largest weight lies between 2^10 and 2^15.5
+// 4 bits: the largest weight lies between 2^10 and 2^15.5, so that sums are seldom rescaled (below).  In the worst case fp16 holds weights with all their places down to 2^-24 of it, 16.6
+// nats below the largest score instead of 19.4, and at all down to 2^-34.
+constexpr float kLowLift = 10.0f, kReach = 5.5f;
 
 struct DecodeParams {
     CacheView c;
@@ -587,8 +589,8 @@ attn_decode_kernel(const DecodeParams p)
         }
         l = over_groups(l, [](float a, float b) { return a + b; });
 
-        // Every wavefront leaves its sums in its own first stage, then takes some blocks of 16 dimensions and adds up all wavefronts' sums of
-        // them, each lane those of its own place.
+        // Every wavefront leaves its sums in its own part of the ring (its first stage; 4 bits: the beginning of its second too), whose last step has been read, then takes
+        // some blocks of 16 dimensions and adds up all wavefronts' sums of them, each lane those of its own place.
 #pragma unroll
         for (int b = 0; b < DP / 16; ++b) *(lds_float4*)(uintptr_t)(ring + (uint32_t)(b * 1024 + lane * 16)) = o[b];
         if (g == 0) {

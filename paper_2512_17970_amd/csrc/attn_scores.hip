@@ -9,10 +9,12 @@
 // joined over four lanes, what tokens need over 16 at the very end, in a fixed order.  Keys are read and their codes turned into operands once for all rows (up to
 // 256), and nothing is written but 4 bytes a token.
 //
-// Rows by the hundred are bound by instructions: for every four products of 16x16x32 (a head of 128) a lane has four scores, an exponential and one or two multiply-adds
-// each, beside what turns codes into operands, on the two wavefronts a SIMD that 64 tokens' operands in registers allow.  The last 32 queries of four prompts of 8192,
-// 64 and 8 heads of 128, 8 bits: 32 us for the rows' sums (maxima followed throughout: 42), 5 for the join, 34 for the weights; in all 63 us, 212 TFLOP/s.  The next product's
-// instructions set between those of the last one's weights, by hand, gained nothing.  Few rows are bound by the keys' bytes and the wait for them: 32 sequences of 206 000
+// Rows by the hundred are bound by waits, on the two wavefronts a SIMD that 64 tokens' operands in registers allow: for every four products of 16x16x32 (a head of 128) a lane has
+// four scores, an exponential and two or three instructions more each, beside what turns codes into operands, and of a pass's cycles matrix cores are busy for a sixth and vector
+// instructions for two fifths; wavefronts wait for half of theirs.  The last 32 queries of four prompts of 8192, 64 and 8 heads of 128, 8 bits: 32 us for the rows' sums (maxima followed
+// throughout: 42), 5 for the join, 34 for the weights; in all 63 us, 211 TFLOP/s; scores far from zero, whose maxima are followed, 99.  The next product's instructions set between
+// those of the last one's weights, by hand, gained nothing.  Every block of keys is multiplied with every row, whether these see it or not, and with a window the weights' kernels load
+// keys that no row sees: all queries of a prompt of 2048 take 900 us, the 32 queries above with a window of 500 48.  Few rows are bound by the keys' bytes and the wait for them: 32 sequences of 206 000
 // tokens in all, 8 rows, 4 bits, 36 us beside the attention's 59, 4.0 TB/s with what tokens had before and have now.
 #include <type_traits>
 
@@ -399,7 +401,8 @@ __global__ void __launch_bounds__(kScoreThreads, 2) score_stats_kernel(const Sco
                 const float sum = (lanes[0] + lanes[16]) + (lanes[32] + lanes[48]);
                 fine = fine && ((sum > kLeastSum && sum < kMostSum) || (sum == 0.0f && space.at[row] < begin + wave * 16 * TILES));     // (it stands before all of them)
             }
-        // Where they do not, once more with every maximum followed.
+        // Where they do not, once more with every maximum followed.  (Also where a row sees none of the wavefront's keys for another reason: its window begins behind them, or they
+        // have no page.  The sum is zero again then.)
         if (!__all(fine)) {
             if (!AHEAD || begin + p.slots * BLOCK < qs.len) codes.load(p, seq, head, begin + wave * 16 * TILES, qs.len, col, g);
             for (int row = lane; row < count; row += kWave) space.sums[wave * many + row] = Pair{-INFINITY, 0.0f};
